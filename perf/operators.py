@@ -89,9 +89,10 @@ def _draw_rotary(rng):
     dims = rng.choice([D, D, D // 2, D // 4 * 3, D - 2 * rng.randint(1, 20)])
     S = _log_int(rng, 1, 4096)
     B = max(1, min(_log_int(rng, 1, 64), 16384 // S))
-    while B * S * (Hq + Hkv) * D > 4 * 2048 * 40 * 128:
+    dtype = rng.choice(["bf16", "bf16", "f16", "f32"])
+    while B * S * (Hq + Hkv) * D > (40 << 20) // (2 if dtype == "f32" else 1):
         B, S = max(1, B // 2), (S + 1) // 2
-    return _rotary(rng.choice(["bf16", "bf16", "f16", "f32"]), B, Hq + Hkv, S, D, dims, rng.choice(["half", "interleaved"]),
+    return _rotary(dtype, B, Hq + Hkv, S, D, dims, rng.choice(["half", "interleaved"]),
                    _log_int(rng, 16, 1 << 20), rng.random() < 0.3)
 
 
@@ -99,7 +100,7 @@ def _draw_append(rng):
     Hq, Hkv = rng.choice(_HEADS)
     D = 64 if Hq == 12 else rng.choice([64, 80, 128, 128])
     S = rng.choice([1, _log_int(rng, 1, 2048)])
-    B = max(1, min(_log_int(rng, 1, 64), 8192 // S))
+    B = max(1, min(_log_int(rng, 1, 64), 7000 // S))
     dtype = rng.choice(["bf16", "f16"])
     return _append(dtype, rng.choice(["int8", "e4m3", dtype]), B, Hq, Hkv, S, S + _log_int(rng, 1, 2048), D,
                    rng.choice([D, D, D // 2, D // 4 * 3]), rng.choice(["half", "interleaved"]), ragged=rng.random() < 0.4)
@@ -129,7 +130,7 @@ def _draw_tree(rng):
     Hq, Hkv = rng.choice(_HEADS)
     D = 64 if Hq == 12 else rng.choice([64, 96, 128, 128])
     T = _log_int(rng, 2, 64)
-    Smax = T + min(_log_int(rng, 64, 8192), (1 << 17) // (B * Hkv))
+    Smax = T + min(_log_int(rng, 64, 8192), (1 << 17) // (B * Hkv), (30 << 20) // (B * Hq * T))
     dtype = rng.choice(["bf16", "f16"])
     return _tree(dtype, rng.choice(["int8", "e4m3", dtype, dtype]), B, Hq, Hkv, T, Smax, D, (Smax - T) // 4,
                  chain=rng.random() < 0.2)
