@@ -266,6 +266,144 @@ int forge_linear_swiglu(const void* x, const void* w_gate, const void* w_up, voi
                         int M, int N, int K, int w_layout, void* stream);
 
 /*
+ * ---- The serving step around the KV cache -------------------------------------------------------------
+ * Rotary positions, writing a cache of 16-bit or 8-bit rows, reading rows back, and attention of one token
+ * per sequence or of a tree of drafted tokens over such a cache.  The cache of the decode step above is one
+ * of these (FORGE_KV_BF16 / FORGE_KV_F16).  Where a tensor's strides are given, they count elements for
+ * {batch, head, token}, as in forge_attn_fused_strided: positive multiples of 8, the D elements of a row
+ * contiguous; NULL is the dense layout {H S D, S D, D}.
+ *
+ * forge_kv_cache: k and v [B, Hkv, Smax, D].  8-bit formats keep a row x (one token and KV head) as D codes
+ * and one fp32 scale in k_scale / v_scale [B, Hkv, Smax]; the row stands for scale * code:
+ *     FORGE_KV_INT8   scale = max|x| / 127    code = rint(x * (127 / max|x|))        (symmetric; -128 is never written)
+ *     FORGE_KV_E4M3   scale = max|x| / 448    code = e4m3(x * (448 / max|x|))        (to nearest even; NaN codes are never
+ *                     written, and what reads a cache takes them for +-480)
+ * computed in fp32 from the unrounded row.  A row whose largest magnitude is below 2^-100 is kept as scale 0
+ * and codes 0; one with a NaN or an infinity as scale NaN and codes 0, so that it stands for NaN.  D: a
+ * multiple of 8 (16-bit formats) or 16 (8-bit formats), up to 128.  Pointers 16-byte aligned.  The struct is
+ * HOST memory and is read during the call only.
+ */
+enum { FORGE_DTYPE_BF16 = 0, FORGE_DTYPE_F16 = 1, FORGE_DTYPE_F32 = 2 };
+enum { FORGE_KV_BF16 = 0, FORGE_KV_F16 = 1, FORGE_KV_INT8 = 2, FORGE_KV_E4M3 = 3 };
+typedef struct forge_kv_cache {
+    void *k, *v;
+    float *k_scale, *v_scale; /* 8-bit formats only */
+    int B, Hkv, Smax, D;
+    int format;               /* FORGE_KV_* */
+} forge_kv_cache;
+
+/*
+ * Rotary positions: the first `dims` elements of a head (dims even, 2 .. D) are rotated in pairs by the angle
+ * position * inv_freq[i], i < dims / 2; the others are left as they are.
+ *     FORGE_ROTARY_HALF         pairs (x[i], x[i + dims/2])      FORGE_ROTARY_INTERLEAVED   pairs (x[2i], x[2i+1])
+ *     (a, b) -> amplitude * (a cos - b sin, b cos + a sin)
+ * inv_freq: DEVICE, fp32 [dims/2], radians per position.  The angle is the exact product, reduced to a turn in
+ * 64-bit fixed point: positions up to 2^20 are as accurate as small ones (cos and sin to a few 2^-24), 2^31 to about 1e-6.
+ *
+ * forge_rotary_frequencies fills inv_freq (HOST) with base^(-2i/dims), scaled for contexts longer than those
+ * of the training (scaling NULL or kind NONE: not at all), and *amplitude:
+ *     LINEAR            f / factor                                             (positions interpolated)
+ *     BASE              base * factor^(dims / (dims - 2)) for base             (dims > 2)
+ *     RAMP_ROTATIONS    f (1 - r) + f / factor * r,  r = clamp((i - lo) / (hi - lo), 0, 1), where lo and hi are the indices
+ *                       whose pairs make `fast` and `slow` turns over original_len positions (rounded down and up,
+ *                       within 0 .. dims - 1); amplitude 0.1 ln(factor) + 1 (1 for factor <= 1)
+ *     RAMP_WAVELENGTH   by the turns t = original_len f / 2 pi of a pair: f where t > fast, f / factor where t < slow,
+ *                       in between f (s + (1 - s) / factor) with s = (t - slow) / (fast - slow)
+ * Computed in fp64, host code only.
+ */
+enum { FORGE_ROTARY_HALF = 0, FORGE_ROTARY_INTERLEAVED = 1 };
+enum {
+    FORGE_ROTARY_SCALE_NONE = 0,
+    FORGE_ROTARY_SCALE_LINEAR = 1,
+    FORGE_ROTARY_SCALE_BASE = 2,
+    FORGE_ROTARY_SCALE_RAMP_ROTATIONS = 3,
+    FORGE_ROTARY_SCALE_RAMP_WAVELENGTH = 4
+};
+typedef struct forge_rotary_scaling {
+    int kind;
+    double factor;       /* >= 1 */
+    double fast, slow;   /* the ramps' bounds in turns, fast > slow > 0 */
+    int original_len;    /* positions of the training (ramps) */
+} forge_rotary_scaling;
+typedef struct forge_rotary {
+    const float* inv_freq;
+    int dims;
+    int layout;          /* FORGE_ROTARY_* */
+    float amplitude;     /* 1 unless the scaling says otherwise */
+} forge_rotary;
+int forge_rotary_frequencies(int dims, double base, const forge_rotary_scaling* scaling, float* inv_freq, float* amplitude);
+
+/*
+ * y = x rotated (inverse != 0: by the negative angles, which undoes the rotation and is its gradient; the amplitude
+ * multiplies in either case).  x, y: [B, H, S, D] views of dtype FORGE_DTYPE_*; y may be x itself with the same
+ * strides, but may not overlap it otherwise.  D: a multiple of 8 up to 256.  The position of token s of sequence b is
+ * positions[b S + s] if positions is given (int32 [B, S]), else first[b] + s (int32 [B]), else s.  So the query
+ * and key heads of a fused projection [B, S, heads, D], which lie side by side, take one call.
+ */
+int forge_rotary_apply(const void* x, void* y, int dtype, int B, int H, int S, int D, const int64_t* x_strides,
+                       const int64_t* y_strides, const int32_t* positions, const int32_t* first,
+                       const forge_rotary* rotary, int inverse, void* stream);
+
+/*
+ * Appends new rows to a cache: for i < counts[b] (counts NULL: S; clamped to 0 .. S) row lens[b] + i of sequence b becomes
+ * token i of k and v, for every KV head; with `rotary`, k is rotated first (and kept in fp32 until it is rounded to the
+ * cache's format).  Rows that would lie at or beyond Smax are dropped; nothing else of the cache is touched, and lens
+ * (clamped to 0 .. Smax) is not changed.  In the same launch q, if given, is rotated into q_out (q_out = q allowed with the
+ * same strides; tokens i >= counts[b] are not written), so that one call stands between the QKV projection and the attention.
+ *   k, v [B, Hkv, S, D], q, q_out [B, Hq, S, D]: views, all of `dtype`: FORGE_DTYPE_BF16 or FORGE_DTYPE_F16; a 16-bit cache
+ *   has the same type.  q needs `rotary`.
+ *   positions: int32 [B, S_src], the positions of the tokens of k (and q); NULL: that of a row is its place lens[b] + i.
+ *   rows: int32 [B, S] or NULL: row lens[b] + i is taken from token rows[b S + i] of k and v, which have S_src tokens then
+ *   (without rows S_src is not read and counts as S).  A value outside 0 .. S_src - 1 leaves its row as it is.  This is what follows a tree of drafted
+ *   tokens: the accepted path is appended once more, to its final rows.  Not together with q.
+ */
+typedef struct forge_kv_append_desc {
+    const void *k, *v, *q;
+    void* q_out;
+    const int64_t *k_strides, *v_strides, *q_strides, *q_out_strides;
+    const int32_t *lens, *counts, *positions, *rows;
+    const forge_rotary* rotary;
+    int dtype, Hq, S, S_src;
+} forge_kv_append_desc;
+int forge_kv_append(const forge_kv_cache* cache, const forge_kv_append_desc* desc, void* stream);
+
+/*
+ * Reads rows back as 16-bit tensors: k_out, v_out [B, Hkv, S, D] (views of dtype FORGE_DTYPE_BF16 or _F16; that of the cache
+ * if it is a 16-bit one) receive rows first[b] + i (first NULL: 0) for i < counts[b] (NULL: S; clamped to 0 .. S), rounded
+ * once; rows outside the cache and those from counts[b] on are left as they were.  So a chunk of a prompt attends a cached
+ * prefix through forge_attn_fused.
+ */
+int forge_kv_read(const forge_kv_cache* cache, void* k_out, void* v_out, int dtype, int S, const int64_t* k_strides,
+                  const int64_t* v_strides, const int32_t* first, const int32_t* counts, void* stream);
+
+/*
+ * Attention of one token per sequence over a cache of any format (the operator of forge_attn_decode_splitkv):
+ *     out[b,h,:] = sum_j softmax_j(scale * q[b,h,:].k[b,h/G,j,:]) v[b,h/G,j,:]   over rows j < lens[b]
+ * q, out: [B, Hq, D] of `dtype` FORGE_DTYPE_BF16 or _F16 (that of a 16-bit cache); lens clamped to 0 .. Smax; a sequence
+ * without rows gives zeros; rows at and beyond lens[b] may hold anything.  Any finite scale.  Hq / Hkv: any whole number.
+ *
+ * forge_attn_tree: T tokens per sequence (1 .. 64) whose own rows are in the cache behind the lens[b] rows of their common
+ * past, at lens[b] .. lens[b] + T - 1 (as forge_kv_append leaves them, with the same lens).  Token t sees all rows before
+ * lens[b], and row lens[b] + u if bit u of tree[b, t] is set (int64 bit masks [tree_B, T], tree_B = B, or 1 for all
+ * sequences; bits from T on are ignored).  tree NULL: a chain, u <= t.  A token that sees no row gives zeros; rows that lie
+ * beyond Smax are not there.  q, out: [B, Hq, T, D] views.  A row of the cache that a token does not see has no part in
+ * its output, whatever the row holds.
+ *
+ * workspace: at least forge_attn_kv_workspace_bytes(B, Hq, Hkv, T, D) bytes, 16-byte aligned; T = 1 for the single token.  Its
+ * arrival counters (the first max(256 KiB, 4 B Hkv ceil(G T / 128)) bytes) must be ZERO when a call starts and are zero when it
+ * has completed: clear a new workspace once with forge_attn_kv_workspace_init; every shape with up to 65536 counters can
+ * use it then.  After a call that ended in FORGE_ERR_TIMEOUT clear it again.  Two calls that may overlap on the GPU must not share it.
+ * The same inputs give the same bits, call after call (on GPUs with the same number of SMs).
+ */
+size_t forge_attn_kv_workspace_bytes(int B, int Hq, int Hkv, int T, int D);
+int forge_attn_kv_workspace_init(void* workspace, size_t workspace_bytes, void* stream);
+int forge_attn_decode_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, const int32_t* lens,
+                         float scale, void* workspace, size_t workspace_bytes, void* stream);
+int forge_attn_tree(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, const int64_t* q_strides,
+                    const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Buffer planning for a fixed sequence of operators (Section 4.5, "Liveness Analysis" and "Linear-Scan
  * Buffer Allocation").  Host code only; nothing is launched.
  *

@@ -80,6 +80,47 @@ SIGNATURES.update({
     "forge_decoder_layer": (_i, [ctypes.POINTER(LayerDesc), _vp, _vp, _vp, _sz, _vp]),
 })
 
+
+class KVCacheDesc(ctypes.Structure):
+    """forge_kv_cache"""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("B", _i), ("Hkv", _i), ("Smax", _i), ("D", _i),
+                ("format", _i)]
+
+
+class RotaryScaling(ctypes.Structure):
+    """forge_rotary_scaling: kind ROTARY_SCALE_*, factor, the ramps' bounds fast and slow in turns, original_len."""
+    _fields_ = [("kind", _i), ("factor", ctypes.c_double), ("fast", ctypes.c_double), ("slow", ctypes.c_double),
+                ("original_len", _i)]
+
+
+class RotaryDesc(ctypes.Structure):
+    """forge_rotary"""
+    _fields_ = [("inv_freq", _vp), ("dims", _i), ("layout", _i), ("amplitude", _f)]
+
+
+_i64x3 = ctypes.c_int64 * 3
+
+
+class KVAppendDesc(ctypes.Structure):
+    """forge_kv_append_desc"""
+    _fields_ = [("k", _vp), ("v", _vp), ("q", _vp), ("q_out", _vp),
+                ("k_strides", ctypes.POINTER(ctypes.c_int64)), ("v_strides", ctypes.POINTER(ctypes.c_int64)),
+                ("q_strides", ctypes.POINTER(ctypes.c_int64)), ("q_out_strides", ctypes.POINTER(ctypes.c_int64)),
+                ("lens", _vp), ("counts", _vp), ("positions", _vp), ("rows", _vp), ("rotary", ctypes.POINTER(RotaryDesc)),
+                ("dtype", _i), ("Hq", _i), ("S", _i), ("S_src", _i)]
+
+
+SIGNATURES.update({
+    "forge_rotary_frequencies": (_i, [_i, ctypes.c_double, ctypes.POINTER(RotaryScaling), _vp, _vp]),
+    "forge_rotary_apply": (_i, [_vp, _vp, _i, _i, _i, _i, _i, _vp, _vp, _vp, _vp, ctypes.POINTER(RotaryDesc), _i, _vp]),
+    "forge_kv_append": (_i, [ctypes.POINTER(KVCacheDesc), ctypes.POINTER(KVAppendDesc), _vp]),
+    "forge_kv_read": (_i, [ctypes.POINTER(KVCacheDesc), _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp]),
+    "forge_attn_kv_workspace_bytes": (_sz, [_i, _i, _i, _i, _i]),
+    "forge_attn_kv_workspace_init": (_i, [_vp, _sz, _vp]),
+    "forge_attn_decode_kv": (_i, [ctypes.POINTER(KVCacheDesc), _vp, _vp, _i, _i, _vp, _f, _vp, _sz, _vp]),
+    "forge_attn_tree": (_i, [ctypes.POINTER(KVCacheDesc), _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _f, _vp, _sz, _vp]),
+})
+
 _lib = None
 # host_calls.cpp: the frequent calls' marshalling in native code.  Its functions return -1 where a call is not plain (anything but
 # dense, contiguous CUDA tensors of matching shapes with the output given); then the Python below does it, with every check.
@@ -400,6 +441,228 @@ def linear_swiglu(x, w_gate, w_up, w_layout=W_KN, out=None):
     _check("forge_linear_swiglu", load().forge_linear_swiglu(
         _dev(x, bf, "x"), _dev(w_gate, bf, "w_gate"), _dev(w_up, bf, "w_up"), _dev(out, bf, "out"),
         M, N, K, int(w_layout), _stream()))
+    return out
+
+
+# ---- the serving step around the KV cache ----
+DTYPE_BF16, DTYPE_F16, DTYPE_F32 = range(3)
+KV_BF16, KV_F16, KV_INT8, KV_E4M3 = range(4)
+ROTARY_HALF, ROTARY_INTERLEAVED = range(2)
+(ROTARY_SCALE_NONE, ROTARY_SCALE_LINEAR, ROTARY_SCALE_BASE, ROTARY_SCALE_RAMP_ROTATIONS, ROTARY_SCALE_RAMP_WAVELENGTH) = range(5)
+_DTYPES = {torch.bfloat16: DTYPE_BF16, torch.float16: DTYPE_F16, torch.float32: DTYPE_F32}
+_KV_TYPES = (torch.bfloat16, torch.float16, torch.int8, torch.float8_e4m3fn)
+
+
+def _find_current_device():
+    return getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+_current_device = _find_current_device()
+
+
+def _on_current(*tensors) -> None:
+    """The library launches on the current device: a tensor of another one is refused."""
+    dev = _current_device()
+    for t in tensors:
+        if t is not None and t.device.index != dev:
+            raise ValueError(f"tensors on the current device (cuda:{dev}) expected, got one on {t.device}")
+
+
+def _dev_or_none(t, dtype, name: str, shape):
+    if t is None:
+        return None
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name}: shape {list(shape)} expected")
+    return _dev(t, dtype, name)
+
+
+def _view(t: torch.Tensor, dtype, name: str, shape):
+    """Address and {batch, head, token} strides of a [B, H, S, D] view with contiguous rows; a dimension of size 1 has no
+    stride of its own and gets one that the library takes."""
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 4 and tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{name}: expected a CUDA tensor {list(shape)} of {dtype}")
+    B, H, S, D = shape
+    st = t.stride()
+    if st[3] != 1 and D != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return t.data_ptr(), _i64x3(st[0] if B > 1 else 8, st[1] if H > 1 else 8, st[2] if S > 1 else 8)
+
+
+def rotary_frequencies(dims, base=10000.0, scaling=None):
+    """forge_rotary_frequencies: (inverse frequencies as an fp32 host tensor [dims / 2], amplitude); scaling: a RotaryScaling."""
+    inv_freq = torch.empty((max(int(dims), 2) // 2,), dtype=torch.float32)
+    amplitude = ctypes.c_float(1.0)
+    _check("forge_rotary_frequencies", load().forge_rotary_frequencies(
+        int(dims), float(base), None if scaling is None else ctypes.byref(scaling), inv_freq.data_ptr(), ctypes.byref(amplitude)))
+    return inv_freq, amplitude.value
+
+
+class Rotary:
+    """forge_rotary: inv_freq, an fp32 CUDA tensor [dims / 2] (kept), the layout of the pairs and the amplitude."""
+
+    def __init__(self, inv_freq, layout=ROTARY_HALF, amplitude=1.0):
+        if inv_freq.dim() != 1:
+            raise ValueError("inv_freq [dims / 2] expected")
+        self.inv_freq = inv_freq
+        self.desc = RotaryDesc(inv_freq=_dev(inv_freq, torch.float32, "inv_freq"), dims=2 * inv_freq.numel(), layout=int(layout),
+                               amplitude=float(amplitude))
+
+
+class KVCache:
+    """forge_kv_cache: k, v [B, Hkv, Smax, D] in bf16, fp16, int8 or float8_e4m3fn; 8-bit ones with k_scale, v_scale
+    [B, Hkv, Smax] in fp32.  The tensors are kept and belong to the caller."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4 or tuple(v.shape) != tuple(k.shape):
+            raise ValueError("k, v [B,Hkv,Smax,D] expected")
+        if k.dtype not in _KV_TYPES:
+            raise ValueError(f"k: expected one of {_KV_TYPES}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.format = _KV_TYPES.index(k.dtype)
+        self.B, self.Hkv, self.Smax, self.D = k.shape
+        eight = self.format in (KV_INT8, KV_E4M3)
+        if eight != (k_scale is not None) or eight != (v_scale is not None):
+            raise ValueError("k_scale and v_scale [B,Hkv,Smax] belong to 8-bit caches, and to no others")
+        kp, vp = _dev(k, k.dtype, "k"), _dev(v, k.dtype, "v")
+        shape = (self.B, self.Hkv, self.Smax)
+        self.desc = KVCacheDesc(k=kp, v=vp, k_scale=_dev_or_none(k_scale, torch.float32, "k_scale", shape),
+                                v_scale=_dev_or_none(v_scale, torch.float32, "v_scale", shape),
+                                B=self.B, Hkv=self.Hkv, Smax=self.Smax, D=self.D, format=self.format)
+        if len({t.device for t in (k, v, k_scale, v_scale) if t is not None}) != 1:
+            raise ValueError("the tensors of a cache must be on one device")
+
+    @classmethod
+    def empty(cls, B, Hkv, Smax, D, format=KV_BF16, device="cuda"):
+        """A new cache (of zeros: 8-bit rows that were never written stand for zeros)."""
+        kv = [torch.zeros((B, Hkv, Smax, D), dtype=_KV_TYPES[format], device=device) for _ in range(2)]
+        scales = [torch.zeros((B, Hkv, Smax), dtype=torch.float32, device=device) for _ in range(2)] if format in (KV_INT8, KV_E4M3) else []
+        return cls(*kv, *scales)
+
+
+def rotary_apply(x, rotary, positions=None, first=None, inverse=False, out=None):
+    """forge_rotary_apply: x [B,H,S,D] view (bf16, fp16 or fp32) rotated at positions int32 [B,S], or first int32 [B] + s, or s;
+    inverse: rotated back.  out may be x itself."""
+    B, H, S, D = x.shape
+    if x.dtype not in _DTYPES:
+        raise ValueError("x: bf16, fp16 or fp32 expected")
+    out = torch.empty_like(x) if out is None else out
+    xp, xs = _view(x, x.dtype, "x", (B, H, S, D))
+    op, os_ = _view(out, x.dtype, "out", (B, H, S, D))
+    pp, fp = _dev_or_none(positions, torch.int32, "positions", (B, S)), _dev_or_none(first, torch.int32, "first", (B,))
+    _on_current(x, out, rotary.inv_freq, positions, first)
+    _check("forge_rotary_apply", load().forge_rotary_apply(
+        xp, op, _DTYPES[x.dtype], B, H, S, D, xs, os_, pp, fp, rotary.desc, int(bool(inverse)), _stream()))
+    return out
+
+
+def kv_append(cache, k, v, lens, counts=None, positions=None, rows=None, rotary=None, q=None, q_out=None):
+    """forge_kv_append: k, v [B,Hkv,S,D] views (bf16 or fp16) become rows lens[b] .. of the cache, k rotated first if `rotary` is
+    given; q [B,Hq,S,D] is rotated into q_out in the same launch.  counts int32 [B]: how many tokens of each sequence; positions
+    int32 [B,S]; rows int32 [B,n]: which tokens of k and v, and in which order.  Returns q_out (None without q)."""
+    B, H, S_src, D = k.shape
+    if (B, H, D) != (cache.B, cache.Hkv, cache.D):
+        raise ValueError("k, v [B,Hkv,S,D] of the cache's B, Hkv and D expected")
+    if k.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("k: bf16 or fp16 expected")
+    if rows is not None and rows.dim() != 2:
+        raise ValueError("rows [B,n] expected")
+    S = S_src if rows is None else rows.shape[1]
+    d = KVAppendDesc(dtype=_DTYPES[k.dtype], S=S, S_src=S_src)
+    d.k, ks = _view(k, k.dtype, "k", (B, H, S_src, D))
+    d.v, vs = _view(v, k.dtype, "v", (B, H, S_src, D))
+    d.k_strides, d.v_strides = ks, vs
+    if q is not None:
+        q_out = torch.empty_like(q) if q_out is None else q_out
+        d.Hq = q.shape[1]
+        d.q, qs = _view(q, k.dtype, "q", (B, d.Hq, S, D))
+        d.q_out, qos = _view(q_out, k.dtype, "q_out", (B, d.Hq, S, D))
+        d.q_strides, d.q_out_strides = qs, qos
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    d.lens = _dev_or_none(lens, torch.int32, "lens", (B,))
+    d.counts = _dev_or_none(counts, torch.int32, "counts", (B,))
+    d.positions = _dev_or_none(positions, torch.int32, "positions", (B, S_src))
+    d.rows = _dev_or_none(rows, torch.int32, "rows", (B, S))
+    if rotary is not None:
+        d.rotary = ctypes.pointer(rotary.desc)
+    _on_current(cache.k, k, v, q, q_out, lens, counts, positions, rows, None if rotary is None else rotary.inv_freq)
+    _check("forge_kv_append", load().forge_kv_append(cache.desc, d, _stream()))
+    return q_out
+
+
+def kv_read(cache, k_out, v_out, first=None, counts=None):
+    """forge_kv_read: rows first[b] + i (first int32 [B] or None: 0) of the cache, for i < counts[b] (None: all), into
+    k_out, v_out [B,Hkv,S,D] views (bf16 or fp16); other rows of these are left as they were.  Returns (k_out, v_out)."""
+    if k_out.dim() != 4 or k_out.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("k_out [B,Hkv,S,D] in bf16 or fp16 expected")
+    shape = (cache.B, cache.Hkv, k_out.shape[2], cache.D)
+    kp, ks = _view(k_out, k_out.dtype, "k_out", shape)
+    vp, vs = _view(v_out, k_out.dtype, "v_out", shape)
+    fp, cp = _dev_or_none(first, torch.int32, "first", (cache.B,)), _dev_or_none(counts, torch.int32, "counts", (cache.B,))
+    _on_current(cache.k, k_out, v_out, first, counts)
+    _check("forge_kv_read", load().forge_kv_read(cache.desc, kp, vp, _DTYPES[k_out.dtype], shape[2], ks, vs, fp, cp, _stream()))
+    return k_out, v_out
+
+
+def attn_kv_workspace_bytes(B, Hq, Hkv, T=1, D=128) -> int:
+    return int(load().forge_attn_kv_workspace_bytes(B, Hq, Hkv, T, D))
+
+
+def attn_kv_workspace_init(workspace) -> None:
+    """forge_attn_kv_workspace_init: clears a new workspace (its arrival counters must start at zero)."""
+    _check("forge_attn_kv_workspace_init", load().forge_attn_kv_workspace_init(
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+
+
+def _kv_workspace(workspace, cache, Hq, T, device):
+    if workspace is None:
+        need = attn_kv_workspace_bytes(cache.B, Hq, cache.Hkv, T, cache.D)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=device)
+        attn_kv_workspace_init(workspace)
+    return workspace
+
+
+def attn_decode_kv(q, cache, lens, scale=None, out=None, workspace=None):
+    """forge_attn_decode_kv: q [B,Hq,D] (bf16 or fp16) over the first lens[b] rows of a KVCache.  A workspace passed in must have
+    been cleared once (attn_kv_workspace_init); without one, a fresh cleared workspace is allocated."""
+    B, Hq, D = q.shape
+    if (B, D) != (cache.B, cache.D):
+        raise ValueError("q [B,Hq,D] of the cache's B and D expected")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("q: bf16 or fp16 expected")
+    out = torch.empty_like(q) if out is None else out
+    if tuple(out.shape) != tuple(q.shape):
+        raise ValueError("out: the shape of q expected")
+    qp, op, lp = _dev(q, q.dtype, "q"), _dev(out, q.dtype, "out"), _dev_or_none(lens, torch.int32, "lens", (B,))
+    _on_current(cache.k, q, out, lens, workspace)
+    workspace = _kv_workspace(workspace, cache, Hq, 1, q.device)
+    _check("forge_attn_decode_kv", load().forge_attn_decode_kv(
+        cache.desc, qp, op, _DTYPES[q.dtype], Hq, lp, float(D ** -0.5 if scale is None else scale),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return out
+
+
+def attn_tree(q, cache, lens, tree=None, scale=None, out=None, workspace=None):
+    """forge_attn_tree: q [B,Hq,T,D] view (bf16 or fp16), T tokens whose own rows are rows lens[b] .. lens[b] + T - 1 of the cache; tree
+    int64 [B or 1, T]: bit u of tree[b, t] says whether token t sees token u (None: those up to itself).  Workspace as in
+    attn_decode_kv."""
+    B, Hq, T, D = q.shape
+    if (B, D) != (cache.B, cache.D):
+        raise ValueError("q [B,Hq,T,D] of the cache's B and D expected")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("q: bf16 or fp16 expected")
+    if tree is not None and (tree.dim() != 2 or tree.shape[0] not in (1, B)):
+        raise ValueError("tree [B or 1, T] expected")
+    out = torch.empty_like(q) if out is None else out
+    qp, qs = _view(q, q.dtype, "q", (B, Hq, T, D))
+    op, os_ = _view(out, q.dtype, "out", (B, Hq, T, D))
+    tree_B = 1 if tree is None else tree.shape[0]
+    lp, tp = _dev_or_none(lens, torch.int32, "lens", (B,)), _dev_or_none(tree, torch.int64, "tree", (tree_B, T))
+    _on_current(cache.k, q, out, lens, tree, workspace)
+    workspace = _kv_workspace(workspace, cache, Hq, T, q.device)
+    _check("forge_attn_tree", load().forge_attn_tree(
+        cache.desc, qp, op, _DTYPES[q.dtype], Hq, T, qs, os_, lp, tp, tree_B, float(D ** -0.5 if scale is None else scale),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
     return out
 
 

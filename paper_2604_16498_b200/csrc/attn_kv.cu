@@ -1,0 +1,102 @@
+// C entry points of the attention over a KV cache of any format.  The kernel is in attn_kv.cuh.
+#include "attn_kv.cuh"
+
+namespace forge {
+template <> int run_attn_kv<FORGE_KV_BF16>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
+template <> int run_attn_kv<FORGE_KV_F16>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
+template <> int run_attn_kv<FORGE_KV_INT8>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
+template <> int run_attn_kv<FORGE_KV_E4M3>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
+
+namespace {
+
+// How the G T rows of a KV head go over warps: row groups of at most 128 rows, and RG warps of 16 rows for each.
+struct RowSplit { int tiles, tile_rows, RG; };
+RowSplit split_rows(int rows) {
+    RowSplit s;
+    s.tiles = (rows + kKvMaxRows - 1) / kKvMaxRows;
+    s.tile_rows = (rows + s.tiles - 1) / s.tiles;
+    s.RG = 1;
+    while (16 * s.RG < s.tile_rows) s.RG *= 2;
+    return s;
+}
+size_t counter_bytes(size_t items) {
+    const size_t n = items > kKvMinCounters ? items : kKvMinCounters;
+    return (n * sizeof(unsigned int) + 255) & ~(size_t)255;
+}
+
+int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, bool own_rows, const int64_t* q_strides,
+            const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale, void* workspace,
+            size_t workspace_bytes, void* stream) {
+    int st = check_cache(cache, dtype);
+    if (st != FORGE_OK) return st;
+    if (!q || !out || !lens || Hq <= 0 || T <= 0 || Hq % cache->Hkv != 0) return FORGE_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lens) & 3u)) return FORGE_ERR_INVALID_ARG;
+    if (tree && ((reinterpret_cast<uintptr_t>(tree) & 7u) || (tree_B != 1 && tree_B != cache->B))) return FORGE_ERR_INVALID_ARG;
+    if (!workspace || !aligned16(workspace)) return FORGE_ERR_INVALID_ARG;
+    if (T > kKvMaxTokens || Hq > 65535 || !(scale - scale == 0.f)) return FORGE_ERR_UNSUPPORTED;
+    KvAttnArgs a = {};
+    if ((st = check_strides(q_strides, Hq, T, cache->D, &a.qs)) != FORGE_OK) return st;
+    if ((st = check_strides(out_strides, Hq, T, cache->D, &a.os)) != FORGE_OK) return st;
+    if (workspace_bytes < forge_attn_kv_workspace_bytes(cache->B, Hq, cache->Hkv, T, cache->D)) return FORGE_ERR_WORKSPACE;
+    const int G = Hq / cache->Hkv;
+    const RowSplit rs = split_rows(G * T);
+    const long long items = (long long)cache->B * cache->Hkv * rs.tiles;
+    const long long tiles = items * (((long long)cache->Smax + 127) / 128);
+    if (tiles >= (1LL << 31)) return FORGE_ERR_UNSUPPORTED;  // counted in 32 bits
+    a.q = q;
+    a.out = out;
+    a.lens = lens;
+    a.tree = reinterpret_cast<const unsigned long long*>(tree);
+    a.tree_stride = tree_B == 1 ? 0 : T;
+    a.T = own_rows ? T : 0;
+    a.B = cache->B; a.Hkv = cache->Hkv; a.G = G; a.Smax = cache->Smax; a.D = cache->D;
+    a.rows = G * T;
+    a.row_tiles = rs.tiles;
+    a.tile_rows = rs.tile_rows;
+    a.RG = rs.RG;
+    a.q_f16 = dtype == FORGE_DTYPE_F16;
+    a.scale_log2 = scale * 1.4426950408889634f;
+    a.counters = static_cast<unsigned int*>(workspace);
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes((size_t)items));
+    a.status = device_status_word();
+    const int sms = sm_count();
+    if (!a.status || sms <= 0) return FORGE_ERR_CUDA;
+    int ctas = sms < kKvMaxCtas ? sms : kKvMaxCtas;
+    if (tiles < ctas) ctas = (int)tiles;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    switch (cache->format) {
+        case FORGE_KV_BF16: return run_attn_kv<FORGE_KV_BF16>(*cache, a, ctas, s);
+        case FORGE_KV_F16: return run_attn_kv<FORGE_KV_F16>(*cache, a, ctas, s);
+        case FORGE_KV_INT8: return run_attn_kv<FORGE_KV_INT8>(*cache, a, ctas, s);
+        default: return run_attn_kv<FORGE_KV_E4M3>(*cache, a, ctas, s);
+    }
+}
+
+}  // namespace
+}  // namespace forge
+
+extern "C" size_t forge_attn_kv_workspace_bytes(int B, int Hq, int Hkv, int T, int D) {
+    using namespace forge;
+    if (B <= 0 || Hq <= 0 || Hkv <= 0 || T <= 0 || D <= 0 || Hq % Hkv != 0) return 0;
+    const long long rows = (long long)Hq / Hkv * T;
+    if (rows > (1 << 22)) return 0;
+    const RowSplit rs = split_rows((int)rows);
+    const size_t frag = (size_t)((D <= 64 ? 64 : 128) / 2 + 1) * 32 * sizeof(float);  // O, m and l of a warp's 16 rows
+    return counter_bytes((size_t)B * Hkv * rs.tiles) + (size_t)kKvMaxCtas * 2 * rs.RG * frag;
+}
+
+extern "C" int forge_attn_kv_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
+    return forge_attn_decode_workspace_init(workspace, workspace_bytes, stream);
+}
+
+extern "C" int forge_attn_decode_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, const int32_t* lens,
+                                    float scale, void* workspace, size_t workspace_bytes, void* stream) {
+    return forge::attn_kv(cache, q, out, dtype, Hq, 1, false, nullptr, nullptr, lens, nullptr, 1, scale, workspace, workspace_bytes, stream);
+}
+
+extern "C" int forge_attn_tree(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, const int64_t* q_strides,
+                               const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+    return forge::attn_kv(cache, q, out, dtype, Hq, T, true, q_strides, out_strides, lens, tree, tree_B, scale, workspace,
+                          workspace_bytes, stream);
+}
