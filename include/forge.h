@@ -276,8 +276,8 @@ int forge_linear_swiglu(const void* x, const void* w_gate, const void* w_up, voi
  * forge_kv_cache: k and v [B, Hkv, Smax, D].  8-bit formats keep a row x (one token and KV head) as D codes
  * and one fp32 scale in k_scale / v_scale [B, Hkv, Smax]; the row stands for scale * code:
  *     FORGE_KV_INT8   scale = max|x| / 127    code = rint(x * (127 / max|x|))        (symmetric; -128 is never written)
- *     FORGE_KV_E4M3   scale = max|x| / 448    code = e4m3(x * (448 / max|x|))        (to nearest even; NaN codes are never
- *                     written, and what reads a cache takes them for +-480)
+ *     FORGE_KV_E4M3   scale = max|x| / 448    code = e4m3(x * (448 / max|x|))        (to nearest even; e4m3's NaN is never
+ *                     written, and what a row that holds one stands for is not specified)
  * computed in fp32 from the unrounded row.  A row whose largest magnitude is below 2^-100 is kept as scale 0
  * and codes 0; one with a NaN or an infinity as scale NaN and codes 0, so that it stands for NaN.  D: a
  * multiple of 8 (16-bit formats) or 16 (8-bit formats), up to 128.  Pointers 16-byte aligned.  The struct is

@@ -8,7 +8,7 @@
 //
 // The work is bound by reading K and V once, up to about 64 rows; beyond, by the warp-level matrix instructions.  All CTAs
 // (one per SM) share the 128-key tiles of the whole call evenly: tiles are numbered through sequences, KV heads and row
-// groups, and CTA c of W takes tiles N c / W .. N (c + 1) / W.  What a cut leaves in two CTAs is merged by the one that finishes
+// groups, and each CTA takes a run of them.  What a cut leaves in two CTAs is merged by the one that finishes
 // last (arrival counters); a CTA has at most two such parts.  Within a CTA a producer warp keeps a ring of whole tiles
 // filled by TMA (the scales by 4-byte copies), and eight warps work on every tile: RG of them on different groups of 16 rows,
 // 8 / RG on different keys of it, merged when the CTA's part of the sequence ends.
@@ -39,6 +39,7 @@ struct KvAttnArgs {
     int T;                           // tokens; their rows are the last ones of the cache (0: one token that has none)
     int B, Hkv, G, Smax, D;
     int rows, row_tiles, tile_rows;  // G * T; groups of rows, and how many a group has
+    int least;                       // rows <= 8: blocks of keys that a CTA has at least
     int RG;                          // warps over the rows: 16 RG >= tile_rows, 1, 2, 4 or 8
     bool q_f16;
     float scale_log2;
@@ -111,8 +112,9 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
 __device__ __forceinline__ int kv_past(const KvAttnArgs& a, int b) { return min(max(__ldg(a.lens + b), 0), a.Smax); }
 // Rows that any token of the sequence may see.
 __device__ __forceinline__ int kv_rows(const KvAttnArgs& a, int past) { return min(past + a.T, a.Smax); }
-// Tiles of a (sequence, KV head, row group): one at least, so that a sequence without rows gets its zeros.
-__device__ __forceinline__ int kv_tiles(const KvAttnArgs& a, int past) { return max((kv_rows(a, past) + kTileKeys - 1) / kTileKeys, 1); }
+// Tiles of KEYS keys of a (sequence, KV head, row group): one at least, so that a sequence without rows gets its zeros.
+template <int KEYS>
+__device__ __forceinline__ int kv_tiles(const KvAttnArgs& a, int past) { return max((kv_rows(a, past) + KEYS - 1) / KEYS, 1); }
 
 // Where a CTA is in the call's tiles.  Every warp walks through the CTA's share by itself; all lanes hold the same.
 struct KvCursor {
@@ -121,45 +123,66 @@ struct KvCursor {
     int past, tiles;     // of sequence b
 };
 
-// N: tiles of the call; leaves the cursor on the CTA's first.
-__device__ __forceinline__ int kv_start(const KvAttnArgs& a, KvCursor& cur, int lane) {
-    const int per = a.Hkv * a.row_tiles;
-    int total = 0;
-    for (int b = lane; b < a.B; b += 32) total += kv_tiles(a, kv_past(a, b));
+// Whole numbers 0 .. n - 1 shared evenly by `by` (at most n) of them, in order: the first n % by get one more than the others.
+struct KvShares {
+    int by, each, more;
+    __device__ __forceinline__ KvShares(int n, int by_) : by(by_), each(n / by_), more(n - each * by_) {}
+    __device__ __forceinline__ int first(int i) const { return i * each + min(i, more); }
+    __device__ __forceinline__ int of(int u) const {  // who has u
+        const int low = more * (each + 1);
+        return u < low ? u / (each + 1) : more + (u - low) / max(each, 1);
+    }
+};
+
+// The call's tiles, which W CTAs share (at least `least` each), and the sequence in which tile u lies: `at(...)` leaves its b, base, past and
+// tiles in the cursor.  Lane l keeps what there is to know of sequence l, so that up to 32 sequences are read once.
+template <int KEYS>
+struct KvSchedule {
+    int N, W;
+    int past0, tiles0, incl0;
+    __device__ __forceinline__ KvSchedule(const KvAttnArgs& a, int least, int lane) {
+        past0 = lane < a.B ? kv_past(a, lane) : 0;
+        tiles0 = lane < a.B ? kv_tiles<KEYS>(a, past0) : 0;
+        incl0 = scan(tiles0, lane);
+        int total = tiles0;
+        for (int b = 32 + lane; b < a.B; b += 32) total += kv_tiles<KEYS>(a, kv_past(a, b));
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-    const int N = total * per;
-    const int W = min((int)gridDim.x, N);
-    cur.u = cur.end = 0;
-    cur.b = cur.base = 0;
-    cur.past = 0;
-    cur.tiles = 1;
-    if ((int)blockIdx.x >= W) return N;
-    cur.u = (int)((long long)N * blockIdx.x / W);
-    cur.end = (int)((long long)N * (blockIdx.x + 1) / W);
-    int before = 0;
-    for (int b0 = 0; b0 < a.B; b0 += 32) {
-        const int past = b0 + lane < a.B ? kv_past(a, b0 + lane) : 0;
-        const int tiles = b0 + lane < a.B ? kv_tiles(a, past) : 0;
-        int incl = tiles;
+        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        N = total * a.Hkv * a.row_tiles;
+        W = min((int)gridDim.x, (N + least - 1) / least);
+    }
+    static __device__ __forceinline__ int scan(int v, int lane) {
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += t;
+            const int t = __shfl_up_sync(0xffffffffu, v, o);
+            if (lane >= o) v += t;
         }
-        const unsigned hit = __ballot_sync(0xffffffffu, cur.u < (before + incl) * per);
-        if (hit) {
-            const int src = __ffs(hit) - 1;
-            cur.b = b0 + src;
-            cur.tiles = __shfl_sync(0xffffffffu, tiles, src);
-            cur.past = __shfl_sync(0xffffffffu, past, src);
-            cur.base = (before + __shfl_sync(0xffffffffu, incl, src) - cur.tiles) * per;
-            break;
-        }
-        before += __shfl_sync(0xffffffffu, incl, 31);
+        return v;
     }
-    return N;
-}
+    __device__ __forceinline__ int past_of(const KvAttnArgs& a, int b) const {  // the same b in all lanes
+        return b < 32 ? __shfl_sync(0xffffffffu, past0, b) : kv_past(a, b);
+    }
+    __device__ __forceinline__ void at(const KvAttnArgs& a, int u, KvCursor& cur, int lane) const {
+        const int per = a.Hkv * a.row_tiles;
+        int before = 0, past = past0, tiles = tiles0, incl = incl0;
+#pragma unroll 1
+        for (int b0 = 0;; b0 += 32) {
+            const unsigned hit = __ballot_sync(0xffffffffu, u < (before + incl) * per);
+            if (hit || b0 + 32 >= a.B) {
+                const int src = hit ? __ffs(hit) - 1 : 0;
+                cur.b = b0 + src;
+                cur.tiles = __shfl_sync(0xffffffffu, tiles, src);
+                cur.past = __shfl_sync(0xffffffffu, past, src);
+                cur.base = (before + __shfl_sync(0xffffffffu, incl, src) - cur.tiles) * per;
+                return;
+            }
+            before += __shfl_sync(0xffffffffu, incl, 31);
+            past = b0 + 32 + lane < a.B ? kv_past(a, b0 + 32 + lane) : 0;
+            tiles = b0 + 32 + lane < a.B ? kv_tiles<KEYS>(a, past) : 0;
+            incl = scan(tiles, lane);
+        }
+    }
+};
 
 // The CTA's part of one (sequence, KV head, row group).
 struct KvPart {
@@ -183,12 +206,13 @@ __device__ __forceinline__ KvPart kv_part(const KvAttnArgs& a, const KvCursor& c
     p.rows = kv_rows(a, cur.past);
     return p;
 }
+template <int KEYS>
 __device__ __forceinline__ void kv_advance(const KvAttnArgs& a, KvCursor& cur, int tiles) {
     cur.u += tiles;
     if (cur.u < cur.end && cur.u - cur.base >= cur.tiles * a.Hkv * a.row_tiles) {
         cur.base += cur.tiles * a.Hkv * a.row_tiles;
         cur.past = kv_past(a, ++cur.b);
-        cur.tiles = kv_tiles(a, cur.past);
+        cur.tiles = kv_tiles<KEYS>(a, cur.past);
     }
 }
 
@@ -271,9 +295,13 @@ attn_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
     pdl_launch_dependents();
     pdl_wait();
 
+    const KvSchedule<kTileKeys> sched(a, 1, lane);
+    const KvShares shares(sched.N, sched.W);
+    if ((int)blockIdx.x >= sched.W) return;
     KvCursor cur;
-    const int N = kv_start(a, cur, lane);
-    const int W = min((int)gridDim.x, N);
+    cur.u = shares.first(blockIdx.x);
+    cur.end = shares.first(blockIdx.x + 1);
+    sched.at(a, cur.u, cur, lane);
     bool failed = false;
 
     if (warp == kKvWarps) {
@@ -320,7 +348,7 @@ attn_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
                     copies_arrive(&full[st]);
                 }
             }
-            kv_advance(a, cur, p.tiles);
+            kv_advance<kTileKeys>(a, cur, p.tiles);
         }
         if (failed) {
             if (lane == 0) atomicExch(a.status, 1);
@@ -426,7 +454,7 @@ attn_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
                 const int e = (int)(__float_as_uint(big) >> 23) - 127;
                 const int up = big == 0.f || e == 128 ? 0 : min(max(14 - e, -110), 110);
                 const float f = __int_as_float((127 + up) << 23);
-                row_mul[r] = a.scale_log2 * __int_as_float((127 - up) << 23) * (kE4m3 ? kE4m3Unit : 1.f);
+                row_mul[r] = a.scale_log2 * __int_as_float((127 - up) << 23);
 #pragma unroll
                 for (int s = 0; s < KS; ++s) {
                     qf[s][r] = pack16<true>(x[4 * s] * f, x[4 * s + 1] * f);
@@ -635,8 +663,9 @@ attn_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
                         for (int hi = 0; hi < 2; ++hi) {
                             const uint32_t ab = __byte_perm(w[0][k], w[1][k], hi ? 0x7362 : 0x5140);
                             const uint32_t cd = __byte_perm(w[2][k], w[3][k], hi ? 0x7362 : 0x5140);
-                            mma_16816<true>(st.o[4 * k + 2 * hi], pf, codes_to_half2<kE4m3, false>(ab), codes_to_half2<kE4m3, false>(cd));
-                            mma_16816<true>(st.o[4 * k + 2 * hi + 1], pf, codes_to_half2<kE4m3, true>(ab), codes_to_half2<kE4m3, true>(cd));
+                            auto finite = [](uint32_t x) { return kE4m3 ? e4m3_finite(x) : x; };
+                            mma_16816<true>(st.o[4 * k + 2 * hi], pf, finite(codes_to_half2<kE4m3, false>(ab)), finite(codes_to_half2<kE4m3, false>(cd)));
+                            mma_16816<true>(st.o[4 * k + 2 * hi + 1], pf, finite(codes_to_half2<kE4m3, true>(ab)), finite(codes_to_half2<kE4m3, true>(cd)));
                         }
                 }
             }
@@ -651,7 +680,7 @@ attn_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
             st.l[r] += __shfl_xor_sync(0xffffffffu, st.l[r], 2);
         }
         if constexpr (kEight) {
-            const float f = unit * (kE4m3 ? kE4m3Unit : 1.f);
+            const float f = unit;
 #pragma unroll
             for (int t8 = 0; t8 < NT; ++t8)
 #pragma unroll
@@ -662,10 +691,9 @@ attn_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
         bool write = true;
         if (p.tiles < p.of) {
             // ---- other CTAs have parts of it: leave this one in the workspace, merge all of them if it is the last to arrive
-            auto cta_of = [&](int u) { return (int)((((long long)u + 1) * W - 1) / N); };
-            const int cta0 = cta_of(p.start), ctas = cta_of(p.start + p.of - 1) - cta0 + 1;
+            const int cta0 = shares.of(p.start), ctas = shares.of(p.start + p.of - 1) - cta0 + 1;
             auto slot = [&](int cta) {  // an item that covers a CTA's first tile has its first slot
-                const int which = p.start > (int)((long long)N * cta / W) ? 1 : 0;
+                const int which = p.start > shares.first(cta) ? 1 : 0;
                 return a.parts + ((size_t)(cta * 2 + which) * RG + rg) * S::kFrag + lane;
             };
             if (kg == 0) {
@@ -727,7 +755,7 @@ attn_kv_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant
                 }
             }
         }
-        kv_advance(a, cur, p.tiles);
+        kv_advance<kTileKeys>(a, cur, p.tiles);
     }
     if (failed) {
         if (lane == 0) atomicExch(a.status, 1);
@@ -754,12 +782,19 @@ int launch_attn_kv(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, c
 
 }  // namespace
 
+}  // namespace forge
+
+#include "attn_kv_narrow.cuh"
+
+namespace forge {
+
 // One per format, each in a file of its own (they compile side by side).
 template <int FMT>
 int run_attn_kv(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s);
 #define FORGE_ATTN_KV_FORMAT(fmt)                                                                         \
     template <>                                                                                           \
     int run_attn_kv<fmt>(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s) {    \
+        if (a.rows <= kNarrowRows) return cache.D <= 64 ? launch_attn_kv_narrow<64, fmt>(cache, a, ctas, s) : launch_attn_kv_narrow<128, fmt>(cache, a, ctas, s); \
         return cache.D <= 64 ? launch_attn_kv<64, fmt>(cache, a, ctas, s) : launch_attn_kv<128, fmt>(cache, a, ctas, s); \
     }
 

@@ -368,7 +368,7 @@ __global__ void __launch_bounds__(kReadThreads) read_rows_kernel(const ReadArgs 
         if (ok[u]) {
             const int64_t r = (int64_t)bh * a.Smax + src;
             raw[u] = *reinterpret_cast<const uint4*>(cache + (r * a.pieces + piece[u]) * 16);
-            if constexpr (FMT != kCache16) sc[u] = scales[r] * (FMT == kCacheE4m3 ? kE4m3Unit : 1.f);
+            if constexpr (FMT != kCache16) sc[u] = scales[r];
         }
     }
 #pragma unroll

@@ -44,11 +44,19 @@ inline int check_strides(const int64_t* in, int H, int S, int D, Strides* out) {
 #ifdef __CUDACC__
 // Codes to fp16, two at a time, exactly.  Word w holds four codes.
 //   int8: the byte with its top bit flipped is x + 128; put below 0x64 it is the fp16 number 1024 + x + 128.
-//   e4m3: sign, exponent and mantissa moved to where fp16 has them are the value times 2^-8 (kE4m3Unit undoes it); NaN codes
-//   come out as +-480 * 2^-8.
-constexpr float kE4m3Unit = 256.f;
+//   e4m3: a conversion of two codes in the lower half of a register.  NaN codes become NaN; e4m3_finite makes them 448, for operands of
+//   products in which they meet zeros that have to stay zeros.
 __device__ __forceinline__ uint32_t sub_1152(uint32_t h2) {
     const __half2 r = __hsub2(*reinterpret_cast<const __half2*>(&h2), __half2half2(__ushort_as_half((unsigned short)0x6480)));
+    return *reinterpret_cast<const uint32_t*>(&r);
+}
+__device__ __forceinline__ uint32_t e4m3_pair(uint32_t two) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)two));
+    return h;
+}
+__device__ __forceinline__ uint32_t e4m3_finite(uint32_t h2) {
+    const __half2 r = __hmin2(*reinterpret_cast<const __half2*>(&h2), __half2half2(__ushort_as_half((unsigned short)0x5f00)));
     return *reinterpret_cast<const uint32_t*>(&r);
 }
 // the codes in bytes 0, 1 (HI: 2, 3) of a word; int8 words have passed through flip_codes()
@@ -57,8 +65,7 @@ __device__ __forceinline__ uint32_t flip_codes(uint32_t w) { return E4M3 ? w : w
 template <bool E4M3, bool HI>
 __device__ __forceinline__ uint32_t codes_to_half2(uint32_t w) {
     if constexpr (E4M3) {
-        const uint32_t t = __byte_perm(w, 0u, HI ? 0x3424 : 0x1404);
-        return ((t >> 1) & 0x3f803f80u) | (t & 0x80008000u);
+        return e4m3_pair(HI ? w >> 16 : w);
     } else {
         return sub_1152(__byte_perm(w, 0x64646464u, HI ? 0x4342 : 0x4140));
     }

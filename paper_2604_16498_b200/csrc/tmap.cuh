@@ -28,7 +28,11 @@ bool encode_tmap_bf16_plain(CUtensorMap* map, const void* base, int rank, const 
 bool encode_tmap_u8_sw64(CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
                          const uint64_t* strides_bytes, const uint32_t* box);
 
-// The same for rows of box[0] = 128 bytes with 128-byte swizzle (16-byte piece c of row r at c ^ (r % 8)).
+// Encodes a tiled tensor map over fp32 elements without swizzle; same conventions (strides_bytes may be NULL for rank 1).
+bool encode_tmap_f32_plain(CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
+                           const uint64_t* strides_bytes, const uint32_t* box);
+
+// As encode_tmap_u8_sw64 for rows of box[0] = 128 bytes with 128-byte swizzle (16-byte piece c of row r at c ^ (r % 8)).
 bool encode_tmap_u8_sw128(CUtensorMap* map, const void* base, int rank, const uint64_t* dims,
                           const uint64_t* strides_bytes, const uint32_t* box);
 
