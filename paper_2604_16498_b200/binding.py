@@ -128,6 +128,7 @@ _host_calls = None
 _HOST_CALLS_ENTRIES = ("forge_attn_fused", "forge_attn_fused_f16", "forge_attn_fused_f32", "forge_attn_decode_splitkv",
                        "forge_attn_decode_splitkv_f16", "forge_linear_act", "forge_linear_act_f16", "forge_linear_act_w8a16",
                        "forge_linear_swiglu")
+_HOST_CALLS_KV_ENTRIES = ("forge_rotary_apply", "forge_kv_append", "forge_kv_read", "forge_attn_decode_kv", "forge_attn_tree")
 
 
 class ForgeError(RuntimeError):
@@ -166,6 +167,7 @@ def _bind_host_calls(lib) -> None:
     if getattr(host_calls, "built_for", None) != host_calls_stamp():
         return
     host_calls.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _HOST_CALLS_ENTRIES))
+    host_calls.bind_kv(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _HOST_CALLS_KV_ENTRIES))
     _host_calls = host_calls
 
 
@@ -506,6 +508,7 @@ class Rotary:
         self.inv_freq = inv_freq
         self.desc = RotaryDesc(inv_freq=_dev(inv_freq, torch.float32, "inv_freq"), dims=2 * inv_freq.numel(), layout=int(layout),
                                amplitude=float(amplitude))
+        self.address, self.device = ctypes.addressof(self.desc), inv_freq.device.index
 
 
 class KVCache:
@@ -530,6 +533,7 @@ class KVCache:
                                 B=self.B, Hkv=self.Hkv, Smax=self.Smax, D=self.D, format=self.format)
         if len({t.device for t in (k, v, k_scale, v_scale) if t is not None}) != 1:
             raise ValueError("the tensors of a cache must be on one device")
+        self.address, self.device = ctypes.addressof(self.desc), k.device.index
 
     @classmethod
     def empty(cls, B, Hkv, Smax, D, format=KV_BF16, device="cuda"):
@@ -542,6 +546,11 @@ class KVCache:
 def rotary_apply(x, rotary, positions=None, first=None, inverse=False, out=None):
     """forge_rotary_apply: x [B,H,S,D] view (bf16, fp16 or fp32) rotated at positions int32 [B,S], or first int32 [B] + s, or s;
     inverse: rotated back.  out may be x itself."""
+    if _host_calls is not None:
+        st = _host_calls.rotary(x, rotary.address, rotary.device, positions, first, 1 if inverse else 0, out)
+        if st >= 0:
+            _check("forge_rotary_apply", st)
+            return out
     B, H, S, D = x.shape
     if x.dtype not in _DTYPES:
         raise ValueError("x: bf16, fp16 or fp32 expected")
@@ -559,6 +568,12 @@ def kv_append(cache, k, v, lens, counts=None, positions=None, rows=None, rotary=
     """forge_kv_append: k, v [B,Hkv,S,D] views (bf16 or fp16) become rows lens[b] .. of the cache, k rotated first if `rotary` is
     given; q [B,Hq,S,D] is rotated into q_out in the same launch.  counts int32 [B]: how many tokens of each sequence; positions
     int32 [B,S]; rows int32 [B,n]: which tokens of k and v, and in which order.  Returns q_out (None without q)."""
+    if _host_calls is not None:
+        st = _host_calls.append(cache.address, cache.device, k, v, lens, counts, positions, rows, None if rotary is None else rotary.address,
+                                None if rotary is None else rotary.device, q, q_out)
+        if st >= 0:
+            _check("forge_kv_append", st)
+            return q_out
     B, H, S_src, D = k.shape
     if (B, H, D) != (cache.B, cache.Hkv, cache.D):
         raise ValueError("k, v [B,Hkv,S,D] of the cache's B, Hkv and D expected")
@@ -593,6 +608,11 @@ def kv_append(cache, k, v, lens, counts=None, positions=None, rows=None, rotary=
 def kv_read(cache, k_out, v_out, first=None, counts=None):
     """forge_kv_read: rows first[b] + i (first int32 [B] or None: 0) of the cache, for i < counts[b] (None: all), into
     k_out, v_out [B,Hkv,S,D] views (bf16 or fp16); other rows of these are left as they were.  Returns (k_out, v_out)."""
+    if _host_calls is not None:
+        st = _host_calls.read(cache.address, cache.device, k_out, v_out, first, counts)
+        if st >= 0:
+            _check("forge_kv_read", st)
+            return k_out, v_out
     if k_out.dim() != 4 or k_out.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError("k_out [B,Hkv,S,D] in bf16 or fp16 expected")
     shape = (cache.B, cache.Hkv, k_out.shape[2], cache.D)
@@ -625,6 +645,11 @@ def _kv_workspace(workspace, cache, Hq, T, device):
 def attn_decode_kv(q, cache, lens, scale=None, out=None, workspace=None):
     """forge_attn_decode_kv: q [B,Hq,D] (bf16 or fp16) over the first lens[b] rows of a KVCache.  A workspace passed in must have
     been cleared once (attn_kv_workspace_init); without one, a fresh cleared workspace is allocated."""
+    if _host_calls is not None:
+        st = _host_calls.decode_kv(cache.address, cache.device, q, lens, scale, out, workspace)
+        if st >= 0:
+            _check("forge_attn_decode_kv", st)
+            return out
     B, Hq, D = q.shape
     if (B, D) != (cache.B, cache.D):
         raise ValueError("q [B,Hq,D] of the cache's B and D expected")
@@ -646,6 +671,11 @@ def attn_tree(q, cache, lens, tree=None, scale=None, out=None, workspace=None):
     """forge_attn_tree: q [B,Hq,T,D] view (bf16 or fp16), T tokens whose own rows are rows lens[b] .. lens[b] + T - 1 of the cache; tree
     int64 [B or 1, T]: bit u of tree[b, t] says whether token t sees token u (None: those up to itself).  Workspace as in
     attn_decode_kv."""
+    if _host_calls is not None:
+        st = _host_calls.tree(cache.address, cache.device, q, lens, tree, scale, out, workspace)
+        if st >= 0:
+            _check("forge_attn_tree", st)
+            return out
     B, Hq, T, D = q.shape
     if (B, D) != (cache.B, cache.D):
         raise ValueError("q [B,Hq,T,D] of the cache's B and D expected")

@@ -24,8 +24,8 @@ size_t counter_bytes(size_t items) {
     return (n * sizeof(unsigned int) + 255) & ~(size_t)255;
 }
 
-// Floats of a warp's part: O of 16 rows, m and l (of up to 8 rows it is half of that).
-size_t frag_floats(int D) { return (size_t)((D <= 64 ? 64 : 128) / 2 + 1) * 32; }
+// Floats of what a CTA leaves of an item: O, m and l of the rows that its kernel works on.
+size_t part_floats(int rows, int D) { return (size_t)(rows <= kNarrowRows ? 8 : 128) * ((D <= 64 ? 64 : 128) + 4); }
 
 int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, bool own_rows, const int64_t* q_strides,
             const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale, void* workspace,
@@ -47,6 +47,7 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     const long long tiles = items * (((long long)cache->Smax + 15) / 16);  // of the smallest size
     if (tiles >= (1LL << 31)) return FORGE_ERR_UNSUPPORTED;  // counted in 32 bits
     a.q = q;
+    a.v = cache->v;
     a.out = out;
     a.lens = lens;
     a.tree = reinterpret_cast<const unsigned long long*>(tree);
@@ -57,7 +58,7 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     a.row_tiles = rs.tiles;
     a.tile_rows = rs.tile_rows;
     a.RG = rs.RG;
-    a.least = kNarrowWarps;
+    a.least = rs.tiles == 1 && G * T <= kNarrowRows ? kNarrowWarps : 1;
     a.q_f16 = dtype == FORGE_DTYPE_F16;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.counters = static_cast<unsigned int*>(workspace);
@@ -85,7 +86,7 @@ extern "C" size_t forge_attn_kv_workspace_bytes(int B, int Hq, int Hkv, int T, i
     const long long rows = (long long)Hq / Hkv * T;
     if (rows > (1 << 22)) return 0;
     const RowSplit rs = split_rows((int)rows);
-    return counter_bytes((size_t)B * Hkv * rs.tiles) + (size_t)kKvMaxCtas * 2 * rs.RG * frag_floats(D) * sizeof(float);
+    return counter_bytes((size_t)B * Hkv * rs.tiles) + (size_t)kKvMaxCtas * 2 * part_floats((int)rows, D) * sizeof(float);
 }
 
 extern "C" int forge_attn_kv_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {

@@ -27,10 +27,12 @@ namespace forge {
 constexpr int kKvMaxCtas = 160;         // what the workspace has room for
 constexpr int kKvMaxRows = 128;         // rows of a group of warps: more take further tiles of their own
 constexpr int kKvMaxTokens = 64;
+constexpr int kMidRows = 8;
 constexpr size_t kKvMinCounters = 65536;
 
 struct KvAttnArgs {
     const void* q;
+    const void* v;                   // the cache's
     void* out;
     Strides qs, os;
     const int32_t* lens;
@@ -785,6 +787,7 @@ int launch_attn_kv(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, c
 }  // namespace forge
 
 #include "attn_kv_narrow.cuh"
+#include "attn_kv_rows.cuh"
 
 namespace forge {
 
@@ -795,6 +798,7 @@ int run_attn_kv(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cuda
     template <>                                                                                           \
     int run_attn_kv<fmt>(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s) {    \
         if (a.rows <= kNarrowRows) return cache.D <= 64 ? launch_attn_kv_narrow<64, fmt>(cache, a, ctas, s) : launch_attn_kv_narrow<128, fmt>(cache, a, ctas, s); \
+        if (a.rows > kMidRows) return cache.D <= 64 ? launch_attn_kv_rows<64, fmt>(cache, a, ctas, s) : launch_attn_kv_rows<128, fmt>(cache, a, ctas, s); \
         return cache.D <= 64 ? launch_attn_kv<64, fmt>(cache, a, ctas, s) : launch_attn_kv<128, fmt>(cache, a, ctas, s); \
     }
 

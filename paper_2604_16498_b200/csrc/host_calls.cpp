@@ -188,6 +188,214 @@ PyObject* py_swiglu(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- the serving step around the KV cache.  Handles (forge_kv_cache, forge_rotary) come as addresses of the structs that binding.py keeps,
+// with the index of the device their tensors are on; views may have any strides that the C ABI takes.
+struct KvEntries {
+    decltype(&forge_rotary_apply) rotary;
+    decltype(&forge_kv_append) append;
+    decltype(&forge_kv_read) read;
+    decltype(&forge_attn_decode_kv) decode;
+    decltype(&forge_attn_tree) tree;
+} kv;
+bool kv_bound = false;
+bool kv_ready(Py_ssize_t n, Py_ssize_t want) { return kv_bound && ready(n, want); }
+
+// A [B,H,S,D] tensor of `type` with contiguous rows, plain but for its strides; these as {batch, head, token}, where a dimension of size
+// 1 gets one that the library takes.
+const at::Tensor* plain_view(PyObject* o, at::ScalarType type, int64_t* strides) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    static const uint64_t dense = c10::DispatchKeySet({c10::DispatchKey::CUDA, c10::DispatchKey::AutogradCUDA,
+                                                       c10::DispatchKey::ADInplaceOrView, c10::DispatchKey::AutocastCUDA}).raw_repr();
+    if (!t.defined() || (t.key_set().raw_repr() & ~dense) != 0 || !t.is_cuda() || t.scalar_type() != type || t.dim() != 4) return nullptr;
+    const auto n = t.sizes(), st = t.strides();
+    if (st[3] != 1) return nullptr;
+    for (int i = 0; i < 3; ++i) strides[i] = n[i] > 1 ? st[i] : 8;
+    return &t;
+}
+bool is_16_bit(PyObject* o, at::ScalarType* type) {
+    if (!THPVariable_CheckExact(o) || !THPVariable_Unpack(o).defined()) return false;
+    *type = THPVariable_Unpack(o).scalar_type();
+    return *type == at::kBFloat16 || *type == at::kHalf;
+}
+int dtype_of(at::ScalarType t) { return t == at::kBFloat16 ? FORGE_DTYPE_BF16 : t == at::kHalf ? FORGE_DTYPE_F16 : FORGE_DTYPE_F32; }
+template <typename T>
+bool handle(PyObject* address, PyObject* device, const T** h) {
+    int d;
+    if (!PyLong_CheckExact(address) || !as_int(device, &d)) return false;
+    *h = static_cast<const T*>(PyLong_AsVoidPtr(address));
+    return *h && d == c10::cuda::current_device();
+}
+bool here(std::initializer_list<const at::Tensor*> ts) {
+    const int d = c10::cuda::current_device();
+    for (const at::Tensor* t : ts)
+        if (t && t->get_device() != d) return false;
+    return true;
+}
+bool sized(const at::Tensor* t, int64_t n) { return !t || t->size(0) == n; }
+bool sized(const at::Tensor* t, int64_t n, int64_t m) { return !t || (t->size(0) == n && t->size(1) == m); }
+
+// rotary(x, rotary, device, positions, first, inverse, out)
+PyObject* py_rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        int inverse, B, H, S, D;
+        bool no_p, no_f;
+        int64_t xs[3], os[3];
+        const forge_rotary* r;
+        if (!kv_ready(n, 7) || !THPVariable_CheckExact(a[0]) || !THPVariable_Unpack(a[0]).defined() || !handle(a[1], a[2], &r) || !as_int(a[5], &inverse))
+            return not_plain();
+        const at::ScalarType ty = THPVariable_Unpack(a[0]).scalar_type();
+        if (ty != at::kBFloat16 && ty != at::kHalf && ty != at::kFloat) return not_plain();
+        const at::Tensor *x = plain_view(a[0], ty, xs), *out = plain_view(a[6], ty, os);
+        const at::Tensor *p = plain_or_none(a[3], at::kInt, 2, &no_p), *f = plain_or_none(a[4], at::kInt, 1, &no_f);
+        if (!x || !out || (!p && !no_p) || (!f && !no_f)) return not_plain();
+        const auto sz = x->sizes();
+        if (out->sizes() != sz || !small(sz[0], &B) || !small(sz[1], &H) || !small(sz[2], &S) || !small(sz[3], &D) || !sized(p, B, S) ||
+            !sized(f, B) || !here({x, out, p, f}))
+            return not_plain();
+        const void* px = address(x);
+        void *po = address(out), *s = stream();
+        const int32_t *pp = static_cast<const int32_t*>(address(p)), *pf = static_cast<const int32_t*>(address(f));
+        return run([&] { return kv.rotary(px, po, dtype_of(ty), B, H, S, D, xs, os, pp, pf, r, inverse, s); });
+    });
+}
+
+// append(cache, device, k, v, lens, counts, positions, rows, rotary or None, its device, q or None, q_out or None)
+PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_cache* cache;
+        at::ScalarType ty;
+        if (!kv_ready(n, 12) || !handle(a[0], a[1], &cache) || !is_16_bit(a[2], &ty)) return not_plain();
+        forge_kv_append_desc d = {};
+        int64_t ks[3], vs[3], qs[3], qos[3];
+        bool no_c, no_p, no_r;
+        const at::Tensor *k = plain_view(a[2], ty, ks), *v = plain_view(a[3], ty, vs), *lens = plain(a[4], at::kInt, 1);
+        const at::Tensor *c = plain_or_none(a[5], at::kInt, 1, &no_c), *p = plain_or_none(a[6], at::kInt, 2, &no_p);
+        const at::Tensor *r = plain_or_none(a[7], at::kInt, 2, &no_r), *q = nullptr, *qo = nullptr;
+        if (!k || !v || !lens || (!c && !no_c) || (!p && !no_p) || (!r && !no_r)) return not_plain();
+        if (a[8] != Py_None && !handle(a[8], a[9], &d.rotary)) return not_plain();
+        const auto sz = k->sizes();
+        if (sz[0] != cache->B || sz[1] != cache->Hkv || sz[3] != cache->D || v->sizes() != sz || !small(sz[2], &d.S_src)) return not_plain();
+        d.S = d.S_src;
+        if (r && (r->size(0) != sz[0] || !small(r->size(1), &d.S))) return not_plain();
+        if (a[10] != Py_None) {
+            q = plain_view(a[10], ty, qs);
+            qo = plain_view(a[11], ty, qos);
+            if (!q || !qo || qo->sizes() != q->sizes() || q->size(0) != sz[0] || q->size(2) != d.S || q->size(3) != sz[3] || !small(q->size(1), &d.Hq))
+                return not_plain();
+            d.q = address(q);
+            d.q_out = address(qo);
+            d.q_strides = qs;
+            d.q_out_strides = qos;
+        } else if (a[11] != Py_None) {
+            return not_plain();
+        }
+        if (!sized(lens, sz[0]) || !sized(c, sz[0]) || !sized(p, sz[0], sz[2]) || !here({k, v, q, qo, lens, c, p, r})) return not_plain();
+        d.k = address(k);
+        d.v = address(v);
+        d.k_strides = ks;
+        d.v_strides = vs;
+        d.lens = static_cast<const int32_t*>(address(lens));
+        d.counts = static_cast<const int32_t*>(address(c));
+        d.positions = static_cast<const int32_t*>(address(p));
+        d.rows = static_cast<const int32_t*>(address(r));
+        d.dtype = dtype_of(ty);
+        void* s = stream();
+        return run([&] { return kv.append(cache, &d, s); });
+    });
+}
+
+// read(cache, device, k_out, v_out, first, counts)
+PyObject* py_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_cache* cache;
+        at::ScalarType ty;
+        int S;
+        bool no_f, no_c;
+        int64_t ks[3], vs[3];
+        if (!kv_ready(n, 6) || !handle(a[0], a[1], &cache) || !is_16_bit(a[2], &ty)) return not_plain();
+        const at::Tensor *k = plain_view(a[2], ty, ks), *v = plain_view(a[3], ty, vs);
+        const at::Tensor *f = plain_or_none(a[4], at::kInt, 1, &no_f), *c = plain_or_none(a[5], at::kInt, 1, &no_c);
+        if (!k || !v || (!f && !no_f) || (!c && !no_c)) return not_plain();
+        const auto sz = k->sizes();
+        if (sz[0] != cache->B || sz[1] != cache->Hkv || sz[3] != cache->D || v->sizes() != sz || !small(sz[2], &S) || !sized(f, sz[0]) ||
+            !sized(c, sz[0]) || !here({k, v, f, c}))
+            return not_plain();
+        void *pk = address(k), *pv = address(v), *s = stream();
+        const int32_t *pf = static_cast<const int32_t*>(address(f)), *pc = static_cast<const int32_t*>(address(c));
+        return run([&] { return kv.read(cache, pk, pv, dtype_of(ty), S, ks, vs, pf, pc, s); });
+    });
+}
+
+// decode_kv(cache, device, q, lens, scale, out, workspace)
+PyObject* py_decode_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_cache* cache;
+        at::ScalarType ty;
+        int Hq;
+        float scale;
+        if (!kv_ready(n, 7) || !handle(a[0], a[1], &cache) || !is_16_bit(a[2], &ty) || !as_scale(a[4], cache->D, &scale)) return not_plain();
+        const at::Tensor *q = plain(a[2], ty, 3), *lens = plain(a[3], at::kInt, 1), *out = plain(a[5], ty, 3), *ws = plain(a[6], at::kByte, 1);
+        if (!q || !lens || !out || !ws) return not_plain();
+        const auto sz = q->sizes();
+        if (sz[0] != cache->B || sz[2] != cache->D || out->sizes() != sz || !small(sz[1], &Hq) || !sized(lens, sz[0]) || !here({q, lens, out, ws}))
+            return not_plain();
+        void *pq = address(q), *po = address(out), *pw = address(ws), *s = stream();
+        const int32_t* pl = static_cast<const int32_t*>(address(lens));
+        const size_t bytes = (size_t)ws->numel();
+        return run([&] { return kv.decode(cache, pq, po, dtype_of(ty), Hq, pl, scale, pw, bytes, s); });
+    });
+}
+
+// tree(cache, device, q, lens, tree or None, scale, out, workspace)
+PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_cache* cache;
+        at::ScalarType ty;
+        int Hq, T, tree_B = 1;
+        float scale;
+        bool no_t;
+        int64_t qs[3], os[3];
+        if (!kv_ready(n, 8) || !handle(a[0], a[1], &cache) || !is_16_bit(a[2], &ty) || !as_scale(a[5], cache->D, &scale)) return not_plain();
+        const at::Tensor *q = plain_view(a[2], ty, qs), *out = plain_view(a[6], ty, os), *lens = plain(a[3], at::kInt, 1);
+        const at::Tensor *t = plain_or_none(a[4], at::kLong, 2, &no_t), *ws = plain(a[7], at::kByte, 1);
+        if (!q || !out || !lens || (!t && !no_t) || !ws) return not_plain();
+        const auto sz = q->sizes();
+        if (sz[0] != cache->B || sz[3] != cache->D || out->sizes() != sz || !small(sz[1], &Hq) || !small(sz[2], &T) || !sized(lens, sz[0]) ||
+            !here({q, out, lens, t, ws}))
+            return not_plain();
+        if (t) {
+            if (t->size(1) != sz[2] || (t->size(0) != 1 && t->size(0) != sz[0])) return not_plain();
+            tree_B = (int)t->size(0);
+        }
+        void *pq = address(q), *po = address(out), *pw = address(ws), *s = stream();
+        const int32_t* pl = static_cast<const int32_t*>(address(lens));
+        const int64_t* pt = static_cast<const int64_t*>(address(t));
+        const size_t bytes = (size_t)ws->numel();
+        return run([&] { return kv.tree(cache, pq, po, dtype_of(ty), Hq, T, qs, os, pl, pt, tree_B, scale, pw, bytes, s); });
+    });
+}
+
+// bind_kv(addresses of the five entry points, in the order of KvEntries); after bind()
+PyObject* py_bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void* p[5];
+    if (n != 5) { PyErr_SetString(PyExc_TypeError, "five addresses expected"); return nullptr; }
+    for (int i = 0; i < 5; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "address expected");
+            return nullptr;
+        }
+    }
+    kv.rotary = reinterpret_cast<decltype(kv.rotary)>(p[0]);
+    kv.append = reinterpret_cast<decltype(kv.append)>(p[1]);
+    kv.read = reinterpret_cast<decltype(kv.read)>(p[2]);
+    kv.decode = reinterpret_cast<decltype(kv.decode)>(p[3]);
+    kv.tree = reinterpret_cast<decltype(kv.tree)>(p[4]);
+    kv_bound = true;
+    Py_RETURN_NONE;
+}
+
 // bind(addresses of the nine entry points, in the order of Entries)
 PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* p[9];
@@ -213,6 +421,8 @@ PyObject* py_bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
 #define FAST(f) reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr
 PyMethodDef methods[] = {{"attn", FAST(py_attn)},           {"decode", FAST(py_decode)}, {"linear", FAST(py_linear)},
                          {"linear_w8", FAST(py_linear_w8)}, {"swiglu", FAST(py_swiglu)}, {"bind", FAST(py_bind)},
+                         {"rotary", FAST(py_rotary)},       {"append", FAST(py_append)}, {"read", FAST(py_read)},
+                         {"decode_kv", FAST(py_decode_kv)}, {"tree", FAST(py_tree)},     {"bind_kv", FAST(py_bind_kv)},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

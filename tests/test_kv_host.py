@@ -168,9 +168,9 @@ def test_read_refusals(lib):
 
 def test_attention_refusals(lib):
     need = lib.forge_attn_kv_workspace_bytes(2, 8, 2, 5, 64)
-    assert need == 65536 * 4 + 160 * 2 * 2 * (33 * 32 * 4)  # 20 rows: two warps of 16
-    assert lib.forge_attn_kv_workspace_bytes(2, 8, 2, 1, 128) == 65536 * 4 + 160 * 2 * (65 * 32 * 4)
-    assert lib.forge_attn_kv_workspace_bytes(1000, 128, 128, 64, 64) == 128000 * 4 + 160 * 2 * 4 * (33 * 32 * 4)
+    assert need == 65536 * 4 + 160 * 2 * (128 * 68 * 4)
+    assert lib.forge_attn_kv_workspace_bytes(2, 8, 2, 1, 128) == 65536 * 4 + 160 * 2 * (8 * 132 * 4)
+    assert lib.forge_attn_kv_workspace_bytes(1000, 128, 128, 64, 64) == 128000 * 4 + 160 * 2 * (128 * 68 * 4)
     for args in ((0, 8, 2, 5, 64), (2, 8, 3, 5, 64), (2, 8, 2, 0, 64), (2, 8, 2, 5, 0), (2, 0, 2, 5, 64)):
         assert lib.forge_attn_kv_workspace_bytes(*args) == 0
 
@@ -215,8 +215,10 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
     # stand-ins for handles whose tensors are on a GPU
     c = binding.KVCache.__new__(binding.KVCache)
     c.B, c.Hkv, c.Smax, c.D, c.k, c.desc = 2, 3, 4, 64, x, cache(Hkv=3, Smax=4, format=0)
+    c.address, c.device = ctypes.addressof(c.desc), 0
     r = binding.Rotary.__new__(binding.Rotary)
     r.inv_freq, r.desc = torch.zeros(32), rotary()
+    r.address, r.device = ctypes.addressof(r.desc), 0
     for call in (lambda: binding.rotary_apply(x, r), lambda: binding.rotary_apply(x.to(torch.int8), r), lambda: binding.kv_append(c, x, x, lens),
                  lambda: binding.kv_append(c, x[:, :2], x, lens), lambda: binding.kv_append(c, x.float(), x.float(), lens),
                  lambda: binding.kv_append(c, x, x, lens, rows=lens), lambda: binding.kv_read(c, x, x), lambda: binding.kv_read(c, x[0], x),
