@@ -9,14 +9,12 @@ template <> int run_attn_kv<FORGE_KV_E4M3>(const forge_kv_cache&, const KvAttnAr
 
 namespace {
 
-// How the G T rows of a KV head go over warps: row groups of at most 128 rows, and RG warps of 16 rows for each.
-struct RowSplit { int tiles, tile_rows, RG; };
-RowSplit split_rows(int rows) {
+// How the G T rows of a KV head form tiles: of as many whole heads as 128 rows hold.
+struct RowSplit { int tiles, heads; };
+RowSplit split_rows(int G, int T) {
     RowSplit s;
-    s.tiles = (rows + kKvMaxRows - 1) / kKvMaxRows;
-    s.tile_rows = (rows + s.tiles - 1) / s.tiles;
-    s.RG = 1;
-    while (16 * s.RG < s.tile_rows) s.RG *= 2;
+    s.heads = 128 / T < G ? 128 / T : G;
+    s.tiles = (G + s.heads - 1) / s.heads;
     return s;
 }
 size_t counter_bytes(size_t items) {
@@ -25,7 +23,7 @@ size_t counter_bytes(size_t items) {
 }
 
 // Floats of what a CTA leaves of an item: O, m and l of the rows that its kernel works on.
-size_t part_floats(int rows, int D) { return (size_t)(rows <= kNarrowRows ? 8 : 128) * ((D <= 64 ? 64 : 128) + 4); }
+size_t part_floats(long long rows, int D) { return (size_t)(rows <= kNarrowRows ? 8 : 128) * ((D <= 64 ? 64 : 128) + 4); }
 
 int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, bool own_rows, const int64_t* q_strides,
             const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale, void* workspace,
@@ -42,7 +40,7 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     if ((st = check_strides(out_strides, Hq, T, cache->D, &a.os)) != FORGE_OK) return st;
     if (workspace_bytes < forge_attn_kv_workspace_bytes(cache->B, Hq, cache->Hkv, T, cache->D)) return FORGE_ERR_WORKSPACE;
     const int G = Hq / cache->Hkv;
-    const RowSplit rs = split_rows(G * T);
+    const RowSplit rs = split_rows(G, T);
     const long long items = (long long)cache->B * cache->Hkv * rs.tiles;
     const long long tiles = items * (((long long)cache->Smax + 15) / 16);  // of the smallest size
     if (tiles >= (1LL << 31)) return FORGE_ERR_UNSUPPORTED;  // counted in 32 bits
@@ -56,8 +54,8 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     a.B = cache->B; a.Hkv = cache->Hkv; a.G = G; a.Smax = cache->Smax; a.D = cache->D;
     a.rows = G * T;
     a.row_tiles = rs.tiles;
-    a.tile_rows = rs.tile_rows;
-    a.RG = rs.RG;
+    a.tile_heads = rs.heads;
+    a.tile_rows = rs.heads * T;
     a.least = rs.tiles == 1 && G * T <= kNarrowRows ? kNarrowWarps : 1;
     a.q_f16 = dtype == FORGE_DTYPE_F16;
     a.scale_log2 = scale * 1.4426950408889634f;
@@ -83,10 +81,10 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
 extern "C" size_t forge_attn_kv_workspace_bytes(int B, int Hq, int Hkv, int T, int D) {
     using namespace forge;
     if (B <= 0 || Hq <= 0 || Hkv <= 0 || T <= 0 || D <= 0 || Hq % Hkv != 0) return 0;
+    if (T > kKvMaxTokens) return 0;
     const long long rows = (long long)Hq / Hkv * T;
-    if (rows > (1 << 22)) return 0;
-    const RowSplit rs = split_rows((int)rows);
-    return counter_bytes((size_t)B * Hkv * rs.tiles) + (size_t)kKvMaxCtas * 2 * part_floats((int)rows, D) * sizeof(float);
+    const RowSplit rs = split_rows(Hq / Hkv, T);
+    return counter_bytes((size_t)B * Hkv * rs.tiles) + (size_t)kKvMaxCtas * 2 * part_floats(rows, D) * sizeof(float);
 }
 
 extern "C" int forge_attn_kv_workspace_init(void* workspace, size_t workspace_bytes, void* stream) {
