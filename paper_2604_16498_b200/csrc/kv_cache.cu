@@ -2,15 +2,14 @@
 //
 // All three are bound by moving bytes, and at a token per sequence by the launch.
 //
-// Rotation.  A warp works on the heads of one token (or on a share of them), LPR lanes to a row of 8 elements a lane, so the cosines and
-// sines of a lane's 8 elements are made once and serve every head: at 48 heads of 128 they are a sixth of the
-// instructions (per head they would take longer than the copies).  The angle in turns is position * F mod 2^64 with
+// Rotation.  A warp works on the heads of one token (or on a share of them), a lane on the same 16 elements of every head, which hold whole
+// pairs: so the cosines and sines are made once for all heads (per head they would take longer than the copies), and no
+// element leaves its lane.  The angle in turns is position * F mod 2^64 with
 // F = inv_freq / 2 pi in 64-bit fixed point: the product wraps around exactly where the circle does, so nothing is lost
-// at far positions.  y[j] = x[j] cos + partner[j] (-+ sin); the partner of a pair comes by shuffles where pairs lie whole
-// 8-element pieces apart, else through shared memory.
+// at far positions.
 //
 // Quantisation.  The row's largest magnitude is a maximum over its lanes (of the bit patterns, where NaN is the largest), then
-// each lane rounds its 8 elements and stores them as 8 bytes.  Rows are rounded once, from fp32.
+// each lane rounds its elements and stores them, 8 bytes at a time.  Rows are rounded once, from fp32.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -137,12 +136,15 @@ __device__ __forceinline__ uint2 encode8(const float (&y)[8], float mul) {
     return make_uint2(w[0], w[1]);
 }
 
-// LPR lanes of 8 elements to a row (8, 16, 32); FMT: what the k and v rows become (kNoCache: there are q rows only).
-template <typename T, int LPR, int FMT>
+// LPR lanes of two 8-element pieces to a row (4, 8, 16); FMT: what the k and v rows become (kNoCache: there are q rows only).
+// A lane's pieces are chosen so that pairs meet in it: half layout, pieces 8 i and half + 8 i (then the unrotated rest two by two); interleaved,
+// pieces 16 i and 16 i + 8.  GENERIC: half layout whose halves are not whole pieces: pairs meet in shared memory.
+template <typename T, int LPR, int FMT, bool GENERIC>
 __global__ void __launch_bounds__(kRotWarps * 32) rotate_append_kernel(const RotArgs a) {
-    constexpr int RPW = 32 / LPR;                        // rows at a time
-    constexpr int U = sizeof(T) == 4 ? 2 : 4;            // of those, loads in flight
-    __shared__ float swap_all[kRotWarps][RPW * LPR * 8]; // rows on the way to their partners
+    constexpr int RPW = 32 / LPR;                            // rows at a time
+    constexpr int U = sizeof(T) == 4 || GENERIC ? 1 : 2;     // of those, loads in flight
+    constexpr int kAngles = GENERIC ? 16 : 8;
+    __shared__ float swap_all[GENERIC ? kRotWarps : 1][GENERIC ? RPW * LPR * 16 : 1];  // rows on the way to their partners
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_launch_dependents();
     const int64_t unit = (int64_t)blockIdx.x * kRotWarps + warp;
@@ -161,107 +163,114 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotate_append_kernel(const Rot
     if (FMT != kNoCache) start = min(max(start, (int64_t)0), (int64_t)a.Smax);
     const int64_t dst = start + s;  // the row of the cache
     const int H = FMT == kNoCache ? a.Hq : a.Hq + 2 * a.Hkv;
-    const int sub = lane / LPR, d0 = (lane % LPR) * 8;
-
-    // cosines and sines of this lane's elements: y = x c + partner s
-    float cs[8], sn[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) { cs[j] = 1.f; sn[j] = 0.f; }
+    const int sub = lane / LPR, li = lane % LPR;
     const int dims = 2 * a.half;
-    const bool turns = d0 < dims;
-    const bool apart = a.interleaved || a.half % 8 == 0;  // no need of shared memory
-    if (turns) {
+    const bool together = !GENERIC && !a.interleaved && li < a.half / 8;  // the pieces are halves of the same pairs
+    const int d0 = together ? 8 * li : GENERIC || a.interleaved ? 16 * li : dims + 16 * (li - a.half / 8);
+    const int d1 = together ? a.half + 8 * li : d0 + 8;
+    const bool in0 = d0 < a.D, in1 = d1 < a.D;
+
+    // cosines and sines: of this lane's pairs, or (GENERIC) elements
+    float cs[kAngles], sn[kAngles];
+    if (dims > 0 && (together || ((GENERIC || a.interleaved) && d0 < dims))) {
         const int64_t pos = a.positions ? a.positions[(int64_t)b * a.S_src + src] : start + s;
-        if (a.interleaved) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (d0 + 2 * i < dims) {
-                    const float2 t = cos_sin(pos, a.inv_freq[d0 / 2 + i]);
-                    cs[2 * i] = cs[2 * i + 1] = t.x * a.amplitude;
-                    sn[2 * i + 1] = t.y * a.amplitude * a.sin_sign;
-                    sn[2 * i] = -sn[2 * i + 1];
-                }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (d0 + j < dims) {
-                    const bool upper = d0 + j >= a.half;
-                    const float2 t = cos_sin(pos, a.inv_freq[upper ? d0 + j - a.half : d0 + j]);
-                    cs[j] = t.x * a.amplitude;
-                    sn[j] = t.y * a.amplitude * (upper ? a.sin_sign : -a.sin_sign);
-                }
+        for (int i = 0; i < kAngles; ++i) {
+            int f;
+            if constexpr (GENERIC) f = d0 + i < a.half ? d0 + i : d0 + i - a.half;
+            else f = together ? d0 + i : d0 / 2 + i;
+            const float2 t = cos_sin(pos, a.inv_freq[min(f, a.half - 1)]);
+            cs[i] = t.x * a.amplitude;
+            sn[i] = t.y * a.amplitude * a.sin_sign;
         }
     }
-    const int partner = turns ? (d0 < a.half ? lane + a.half / 8 : lane - a.half / 8) : lane;  // half layout, whole pieces apart
 
     const int iters = (H + RPW - 1) / RPW;
     const int64_t cache_row = FMT == kNoCache ? 0 : ((int64_t)b * a.Hkv) * a.Smax + dst;  // of KV head 0
+    const T* const q_row = static_cast<const T*>(a.q) + b * a.qs.b + s * a.qs.s;
+    const T* const k_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.k) + b * a.kst.b + src * a.kst.s;
+    const T* const v_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.v) + b * a.vst.b + src * a.vst.s;
+    T* const out_row = static_cast<T*>(a.q_out) + b * a.qos.b + s * a.qos.s;
     for (int it0 = part; it0 < iters; it0 += a.parts * U) {
-        Vec8<T> raw[U];
+        Vec8<T> raw[U][2];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int h = (it0 + u * a.parts) * RPW + sub;
-            if (h >= H || d0 >= a.D) continue;
+            if (h >= H) continue;
             const T* p;
-            if (FMT == kNoCache || h < a.Hq) p = static_cast<const T*>(a.q) + b * a.qs.b + h * a.qs.h + s * a.qs.s;
-            else if (h < a.Hq + a.Hkv) p = static_cast<const T*>(a.k) + b * a.kst.b + (h - a.Hq) * a.kst.h + src * a.kst.s;
-            else p = static_cast<const T*>(a.v) + b * a.vst.b + (h - a.Hq - a.Hkv) * a.vst.h + src * a.vst.s;
-            raw[u].load(p + d0);
+            if (FMT == kNoCache || h < a.Hq) p = q_row + h * a.qs.h;
+            else if (h < a.Hq + a.Hkv) p = k_row + (h - a.Hq) * a.kst.h;
+            else p = v_row + (h - a.Hq - a.Hkv) * a.vst.h;
+            if (in0) raw[u][0].load(p + d0);
+            if (in1) raw[u][1].load(p + d1);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if ((it0 + u * a.parts) * RPW >= H) break;  // the whole warp
             const int h = (it0 + u * a.parts) * RPW + sub;
-            const bool here = h < H && d0 < a.D;
-            float x[8], y[8];
+            const bool here = h < H, is_v = FMT != kNoCache && h >= a.Hq + a.Hkv;
+            float x[2][8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[j] = 0.f;
-            if (here) raw[u].unpack(x);
-            const bool is_v = FMT != kNoCache && h >= a.Hq + a.Hkv;
-            if (dims > 0) {
-                float other[8];
-                if (a.interleaved) {
+            for (int j = 0; j < 8; ++j) x[0][j] = x[1][j] = 0.f;
+            if (here && in0) raw[u][0].unpack(x[0]);
+            if (here && in1) raw[u][1].unpack(x[1]);
+            if constexpr (GENERIC) {
+                float* row = swap_all[warp] + sub * LPR * 16;
+                __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) other[j] = x[j ^ 1];
-                } else if (apart) {
+                for (int j = 0; j < 16; ++j) row[d0 + j] = x[j >> 3][j & 7];
+                __syncwarp();
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) other[j] = __shfl_sync(0xffffffffu, x[j], partner);
-                } else {
-                    float* row = swap_all[warp] + sub * LPR * 8;
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) row[d0 + j] = x[j];
-                    __syncwarp();
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        other[j] = d0 + j < dims ? row[d0 + j < a.half ? d0 + j + a.half : d0 + j - a.half] : 0.f;
+                for (int j = 0; j < 16; ++j) {
+                    const int d = d0 + j;
+                    if (is_v || d >= dims) continue;
+                    const float other = row[d < a.half ? d + a.half : d - a.half];
+                    x[j >> 3][j & 7] = fmaf(other, d < a.half ? -sn[j] : sn[j], x[j >> 3][j & 7] * cs[j]);
                 }
+            } else if (is_v || dims == 0) {
+            } else if (together) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = is_v || d0 + j >= dims ? x[j] : fmaf(other[j], sn[j], x[j] * cs[j]);
-            } else {
+                for (int j = 0; j < 8; ++j) {
+                    const float lo = x[0][j], hi = x[1][j];
+                    x[0][j] = fmaf(hi, -sn[j], lo * cs[j]);
+                    x[1][j] = fmaf(lo, sn[j], hi * cs[j]);
+                }
+            } else if (a.interleaved) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) y[j] = x[j];
+                for (int i = 0; i < 8; ++i)
+                    if (d0 + 2 * i < dims) {
+                        float &lo = x[i >> 2][2 * (i & 3)], &hi = x[i >> 2][2 * (i & 3) + 1];
+                        const float was = lo;
+                        lo = fmaf(hi, -sn[i], was * cs[i]);
+                        hi = fmaf(was, sn[i], hi * cs[i]);
+                    }
             }
             if (FMT == kNoCache || h < a.Hq) {
-                if (here) Vec8<T>::store(static_cast<T*>(a.q_out) + b * a.qos.b + h * a.qos.h + s * a.qos.s + d0, y);
+                T* p = out_row + h * a.qos.h;
+                if (here && in0) Vec8<T>::store(p + d0, x[0]);
+                if (here && in1) Vec8<T>::store(p + d1, x[1]);
                 if constexpr (FMT == kNoCache || FMT == kCache16) continue;
             }
             if constexpr (FMT != kNoCache) {
-                const int kvh = is_v ? h - a.Hq - a.Hkv : h - a.Hq;
-                const int64_t row = cache_row + (int64_t)kvh * a.Smax;
+                const int64_t row = cache_row + (int64_t)(is_v ? h - a.Hq - a.Hkv : h - a.Hq) * a.Smax;
                 if constexpr (FMT == kCache16) {
-                    if (here && dst < a.Smax) Vec8<T>::store(static_cast<T*>(is_v ? a.vc : a.kc) + row * a.D + d0, y);
+                    T* p = static_cast<T*>(is_v ? a.vc : a.kc) + row * a.D;
+                    if (here && in0 && dst < a.Smax) Vec8<T>::store(p + d0, x[0]);
+                    if (here && in1 && dst < a.Smax) Vec8<T>::store(p + d1, x[1]);
                 } else {
+                    if (!__any_sync(0xffffffffu, h >= a.Hq)) continue;  // q rows only
                     uint32_t m = 0;  // the lanes of a row meet: all lanes take part, those of q rows too
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) m = max(m, __float_as_uint(y[j]) & 0x7fffffffu);
+                    for (int j = 0; j < 8; ++j) m = max(m, max(__float_as_uint(x[0][j]) & 0x7fffffffu, __float_as_uint(x[1][j]) & 0x7fffffffu));
 #pragma unroll
                     for (int o = LPR / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
                     float mul;
                     const float scale = row_scale<FMT>(m, &mul);
                     if (here && h >= a.Hq && dst < a.Smax) {
-                        *reinterpret_cast<uint2*>(static_cast<uint8_t*>(is_v ? a.vc : a.kc) + row * a.D + d0) = encode8<FMT>(y, mul);
-                        if (d0 == 0) (is_v ? a.vs : a.ks)[row] = scale;
+                        uint8_t* p = static_cast<uint8_t*>(is_v ? a.vc : a.kc) + row * a.D;
+                        if (in0) *reinterpret_cast<uint2*>(p + d0) = encode8<FMT>(x[0], mul);
+                        if (in1) *reinterpret_cast<uint2*>(p + d1) = encode8<FMT>(x[1], mul);
+                        if (li == 0) (is_v ? a.vs : a.ks)[row] = scale;
                     }
                 }
             }
@@ -281,17 +290,18 @@ int launch_rotate(RotArgs& a, cudaStream_t s) {
     a.parts = (int)(want < 1 ? 1 : want > iters ? iters : want);
     const long long ctas = (tokens * a.parts + kRotWarps - 1) / kRotWarps;
     if (ctas > 0x7fffffffLL) return FORGE_ERR_UNSUPPORTED;
-    FORGE_CUDA_TRY(launch_pdl(rotate_append_kernel<T, LPR, FMT>, dim3((unsigned)ctas), dim3(kRotWarps * 32), 0, s, a));
+    const auto kernel = !a.interleaved && a.half % 8 != 0 ? rotate_append_kernel<T, LPR, FMT, true> : rotate_append_kernel<T, LPR, FMT, false>;
+    FORGE_CUDA_TRY(launch_pdl(kernel, dim3((unsigned)ctas), dim3(kRotWarps * 32), 0, s, a));
     return finish_launch(1);
 }
 
 template <typename T>
 int launch_rotate_only(RotArgs& a, cudaStream_t s) {
-    return a.D <= 64 ? launch_rotate<T, 8, kNoCache>(a, s) : a.D <= 128 ? launch_rotate<T, 16, kNoCache>(a, s) : launch_rotate<T, 32, kNoCache>(a, s);
+    return a.D <= 64 ? launch_rotate<T, 4, kNoCache>(a, s) : a.D <= 128 ? launch_rotate<T, 8, kNoCache>(a, s) : launch_rotate<T, 16, kNoCache>(a, s);
 }
 template <typename T, int FMT>
 int launch_append(RotArgs& a, cudaStream_t s) {
-    return a.D <= 64 ? launch_rotate<T, 8, FMT>(a, s) : launch_rotate<T, 16, FMT>(a, s);
+    return a.D <= 64 ? launch_rotate<T, 4, FMT>(a, s) : launch_rotate<T, 8, FMT>(a, s);
 }
 template <typename T>
 int dispatch_append(int format, RotArgs& a, cudaStream_t s) {
