@@ -170,6 +170,29 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotate_append_kernel(const Rot
     const int d1 = together ? a.half + 8 * li : d0 + 8;
     const bool in0 = d0 < a.D, in1 = d1 < a.D;
 
+    const int iters = (H + RPW - 1) / RPW;
+    const int64_t cache_row = FMT == kNoCache ? 0 : ((int64_t)b * a.Hkv) * a.Smax + dst;  // of KV head 0
+    const T* const q_row = static_cast<const T*>(a.q) + b * a.qs.b + s * a.qs.s;
+    const T* const k_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.k) + b * a.kst.b + src * a.kst.s;
+    const T* const v_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.v) + b * a.vst.b + src * a.vst.s;
+    T* const out_row = static_cast<T*>(a.q_out) + b * a.qos.b + s * a.qos.s;
+    // the next rows are on their way while these are worked on; the first ones leave before the cosines are made
+    Vec8<T> raw[U][2], then[U][2];
+    auto load = [&](int it0, Vec8<T> (&to)[U][2]) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int h = (it0 + u * a.parts) * RPW + sub;
+            if (h >= H) continue;
+            const T* p;
+            if (FMT == kNoCache || h < a.Hq) p = q_row + h * a.qs.h;
+            else if (h < a.Hq + a.Hkv) p = k_row + (h - a.Hq) * a.kst.h;
+            else p = v_row + (h - a.Hq - a.Hkv) * a.vst.h;
+            if (in0) to[u][0].load(p + d0);
+            if (in1) to[u][1].load(p + d1);
+        }
+    };
+    load(part, then);
+
     // cosines and sines: of this lane's pairs, or (GENERIC) elements
     float cs[kAngles], sn[kAngles];
     if (dims > 0 && (together || ((GENERIC || a.interleaved) && d0 < dims))) {
@@ -185,25 +208,10 @@ __global__ void __launch_bounds__(kRotWarps * 32) rotate_append_kernel(const Rot
         }
     }
 
-    const int iters = (H + RPW - 1) / RPW;
-    const int64_t cache_row = FMT == kNoCache ? 0 : ((int64_t)b * a.Hkv) * a.Smax + dst;  // of KV head 0
-    const T* const q_row = static_cast<const T*>(a.q) + b * a.qs.b + s * a.qs.s;
-    const T* const k_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.k) + b * a.kst.b + src * a.kst.s;
-    const T* const v_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.v) + b * a.vst.b + src * a.vst.s;
-    T* const out_row = static_cast<T*>(a.q_out) + b * a.qos.b + s * a.qos.s;
     for (int it0 = part; it0 < iters; it0 += a.parts * U) {
-        Vec8<T> raw[U][2];
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int h = (it0 + u * a.parts) * RPW + sub;
-            if (h >= H) continue;
-            const T* p;
-            if (FMT == kNoCache || h < a.Hq) p = q_row + h * a.qs.h;
-            else if (h < a.Hq + a.Hkv) p = k_row + (h - a.Hq) * a.kst.h;
-            else p = v_row + (h - a.Hq - a.Hkv) * a.vst.h;
-            if (in0) raw[u][0].load(p + d0);
-            if (in1) raw[u][1].load(p + d1);
-        }
+        for (int u = 0; u < U; ++u) { raw[u][0] = then[u][0]; raw[u][1] = then[u][1]; }
+        if (it0 + a.parts * U < iters) load(it0 + a.parts * U, then);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if ((it0 + u * a.parts) * RPW >= H) break;  // the whole warp
