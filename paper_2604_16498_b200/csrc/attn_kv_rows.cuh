@@ -1,13 +1,13 @@
 // Attention over a KV cache for more than 8 query rows per (sequence, KV head): trees of drafted tokens, and single tokens of large head
 // groups.  Included by attn_kv.cuh.
 //
-// The rows (up to 128: several tokens of several heads that share K and V) are one tile of the tensor cores: per step of 128 keys (16-bit
-// rows) or 64 (8-bit)    S[128 x keys] = Q K^T  and  O[128 x DW] += P V   by tcgen05.mma, with S, P and O in tensor memory,
-// and thread = row does the softmax in between.  Even and odd steps belong to two groups of softmax threads with references, sums and O of
-// their own, so that one group's softmax runs beside the other's products; the two are merged when the CTA's part of an item
-// ends.  The call's steps are shared evenly by all CTAs, as in the other kernel, and what a CTA has of an item that others
-// have parts of too is merged by the one that finishes last, after its whole run: loads in the middle of it would wait behind the
-// copies in flight.
+// The rows (up to 128: several tokens of several heads that share K and V) are one tile of the tensor cores: per step of 128 keys (16-bit rows;
+// a product 128 x 64 would read Q from shared memory twice as often as the tensor cores need it) or 64 (8-bit)
+//     S[128 x keys] = Q K^T  and  O[128 x DW] += P V   by tcgen05.mma, with S (two steps' worth), P and O in tensor memory,
+// and thread = row does the softmax in between.  Each half of a step's keys belongs to a group of softmax threads with references, sums and an O
+// of its own; the two are merged when the CTA's part of an item ends.  The call's steps are shared evenly by all CTAs, as in the other kernel,
+// and what a CTA has of an item that others have parts of too is merged by the one that finishes last, after its whole run: loads in the
+// middle of it would wait behind the copies in flight.
 //   warps 0-7   softmax (two groups of 128 threads), O out      warp 8  TMA      warp 9  tcgen05.mma
 //   warps 10-13 8-bit rows only: codes of K and V to fp16, from the copies' ring into operands
 // 8-bit rows stay codes in the products (exact in fp16; int8 elements come in the order 0 2 1 3 of each four, in Q and O too); their scales
@@ -22,7 +22,7 @@ constexpr float kRowsTop = 14.f, kRowsLift = 6.f;  // p reaches 2^14, 2^8 above 
 template <int DW, int FMT>
 struct RowsShape {
     static constexpr bool kEight = FMT == FORGE_KV_INT8 || FMT == FORGE_KV_E4M3;
-    static constexpr int kStep = kEight ? 64 : 128;                  // keys
+    static constexpr int kStep = kEight ? 64 : 128, kHalf = kStep / 2;  // keys; of a group
     static constexpr int kConvWarps = kEight ? 4 : 0;
     static constexpr int kThreads = (10 + kConvWarps) * 32;
     static constexpr int kQChunk = 128 * 128;                        // 128 rows x 64 elements
@@ -32,7 +32,7 @@ struct RowsShape {
     static constexpr int kRawBytes = kStep * DW;                     // 8-bit: the codes of K, or V
     static constexpr int kScaleBox = 512;                            // scales from the 16-byte boundary at or before the first
     static constexpr int kScaleKeys = kStep + 4;
-    // 16-bit: rings of K and of V; K's runs further ahead, a step's scores being asked for two steps before its product with V.
+    // 16-bit: rings of K and of V; K's is longer, a step's scores being asked for two steps before its product with V.
     // 8-bit: a ring of codes, of K and V together, and operand buffers, K then V.
     static constexpr int kLoadBytes = 2 * kRawBytes + 2 * kScaleBox;
     static constexpr int kLoads = kEight ? (DW == 128 ? 4 : 8) : 0;
@@ -60,12 +60,13 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     constexpr int kLoads = S::kLoads ? S::kLoads : 1, kConvThreads = S::kConvWarps ? S::kConvWarps * 32 : 32;
     constexpr bool kEight = S::kEight, kE4m3 = FMT == FORGE_KV_E4M3;
     constexpr bool kF16 = FMT != FORGE_KV_BF16;
-    constexpr int kColS = 0, kColO = 2 * S::kStep, kTmemCols = 2 * (S::kStep + DW) <= 256 ? 256 : 512;  // S and O of group h at kColS + kStep h, kColO + DW h
+    constexpr int kColS = 0, kColO = 2 * S::kStep;  // S of step n at kStep (n % 2), O of group h at kColO + DW h
+    constexpr int kTmemCols = kColO + 2 * DW <= 256 ? 256 : 512;
     constexpr int kMaxOdd = 2 * kKvMaxTokens;
     extern __shared__ uint8_t smem_raw[];
     // codes (8-bit); operands of the scores and of the product with V (8-bit: complete together, k_full and k_empty serve for both)
     __shared__ uint64_t load_full[kLoads], load_empty[kLoads], k_full[S::kKBufs], k_empty[S::kKBufs], v_full[S::kVBufs], v_empty[S::kVBufs];
-    __shared__ uint64_t q_full, q_empty, q_ready, s_full[2], p_ready[2], pv_done[2];
+    __shared__ uint64_t q_full, q_empty, q_ready, s_full[2], p_ready[2][2], pv_done[2];  // p_ready: [step % 2][group]
     __shared__ uint32_t tmem_slot;
     // what the CTA has of the items at the ends of its run, if others have parts of them; the number of these CTAs if this one was last to arrive
     struct Cut { int item, start, tiles, b, kvh, rt; };
@@ -82,7 +83,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         for (int i = 0; i < S::kVBufs; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
         mbar_init(&q_full, 1);
         mbar_init(&q_empty, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i], 4); mbar_init(&pv_done[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i][0], 4); mbar_init(&p_ready[i][1], 4); mbar_init(&pv_done[i], 1); }
         mbar_init(&q_ready, 4);
         fence_mbar_init();
         prefetch_tmap(&tmap_q);
@@ -172,7 +173,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         constexpr uint32_t idesc_s = kF16 ? make_idesc_f16(128, S::kStep, false, false) : make_idesc_bf16(128, S::kStep, false, false);
         constexpr uint32_t idesc_o = kF16 ? make_idesc_f16(128, DW, false, true) : make_idesc_bf16(128, DW, false, true);
         if (elect_one()) {
-            int base = 0, parts = 0, steps[2] = {0, 0};
+            int base = 0, parts = 0;  // steps and parts before this part
             while (cur.u < cur.end && !failed) {
                 const KvPart p = kv_part(a, cur);
                 const int n = p.tiles;
@@ -184,26 +185,32 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     const uint64_t kd = make_smem_desc(smem_u32(smem + S::kKOff + buf * S::kKEach), 16, 1024);
 #pragma unroll
                     for (int k = 0; k < DW / 16; ++k)
-                        mma_ss(tmem + kColS + (g & 1) * S::kStep, qd + (((k / 4) * S::kQChunk + (k % 4) * 32) >> 4),
+                        mma_ss(tmem + kColS + (pos & 1) * S::kStep, qd + (((k / 4) * S::kQChunk + (k % 4) * 32) >> 4),
                                kd + (((k / 4) * S::kOpChunk + (k % 4) * 32) >> 4), idesc_s, k != 0);
-                    mma_commit(&s_full[g & 1]);
+                    mma_commit(&s_full[pos & 1]);
                     if (!kEight) mma_commit(&k_empty[buf]);
                     if (g == n - 1) mma_commit(&q_empty);
                     return true;
                 };
                 const bool have_q = kEight ? mbar_wait(&q_ready, parts & 1) : mbar_wait(&q_full, parts & 1);
-                if (!have_q || !issue_qk(0) || (n > 1 && !issue_qk(1))) { failed = true; break; }
+                failed = !have_q;
+                for (int g = 0; g < n && g < 2 && !failed; ++g) failed = !issue_qk(g);
+                if (failed) break;
                 for (int g = 0; g < n; ++g) {
-                    const int h = g & 1, pos = base + g, buf = pos % S::kVBufs;
+                    const int pos = base + g, buf = pos % S::kVBufs;
                     if (!kEight && !mbar_wait(&v_full[buf], (pos / S::kVBufs) & 1)) { failed = true; break; }
-                    if (!mbar_wait(&p_ready[h], steps[h] & 1)) { failed = true; break; }
-                    ++steps[h];
-                    tc_fence_after_sync();
                     const uint64_t vd = make_smem_desc(smem_u32(smem + S::kVOff + buf * S::kVEach), S::kOpChunk, 1024);
 #pragma unroll
-                    for (int k = 0; k < S::kStep / 16; ++k)
-                        mma_ts(tmem + kColO + h * DW, tmem + kColS + h * S::kStep + k * 8, vd + k * (2048 >> 4), idesc_o, g >= 2 || k != 0);
-                    mma_commit(&pv_done[h]);
+                    for (int h = 0; h < 2; ++h) {  // P of group h in the first columns of its half of S
+                        if (!mbar_wait(&p_ready[pos & 1][h], (pos / 2) & 1)) { failed = true; break; }
+                        tc_fence_after_sync();
+#pragma unroll
+                        for (int k = 0; k < S::kHalf / 16; ++k)
+                            mma_ts(tmem + kColO + h * DW, tmem + kColS + (pos & 1) * S::kStep + h * S::kHalf + k * 8,
+                                   vd + (h * (S::kHalf / 16) + k) * (2048 >> 4), idesc_o, g > 0 || k != 0);
+                        mma_commit(&pv_done[h]);
+                    }
+                    if (failed) break;
                     mma_commit(kEight ? &k_empty[buf] : &v_empty[buf]);
                     if (g + 2 < n && !issue_qk(g + 2)) { failed = true; break; }
                 }
@@ -281,8 +288,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             return a.parts + (size_t)(cta * 2 + (start > shares.first(cta) ? 1 : 0)) * S::kPart;
         };
         const bool out_f16 = kEight ? a.q_f16 : kF16;
-        constexpr int kHalf = DW / 2;
-        const int col0 = (warp >> 2) * kHalf;  // a group of threads writes a half of O's columns
+        constexpr int kCols = DW / 2;
+        const int col0 = (warp >> 2) * kCols;  // a group of threads writes a half of O's columns
         auto out_row = [&](int b, int kvh, int h, int tok) {
             return static_cast<uint16_t*>(a.out) + b * a.os.b + (int64_t)(kvh * a.G + h) * a.os.h + tok * a.os.s;
         };
@@ -356,16 +363,16 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             float unit = 1.17549435e-38f, unit_inv = 8.5070592e37f;  // 8-bit: power of two that P is divided by, at least V's largest scale so far
             const int n = p.tiles;
 #pragma unroll 1
-            for (int g = group; g < n; g += 2) {
+            for (int g = 0; g < n; ++g) {
                 const int pos = base + g, buf = pos % S::kVBufs;
-                const int key0 = (p.first + g) * S::kStep;
-                const uint32_t s_col = lanes + kColS + group * S::kStep, o_col = lanes + kColO + group * DW;
-                if (!failed && !warp_wait(&s_full[group], steps & 1)) failed = true;
+                const int key0 = (p.first + g) * S::kStep + group * S::kHalf;  // of this group's half
+                const uint32_t s_col = lanes + kColS + (pos & 1) * S::kStep + group * S::kHalf, o_col = lanes + kColO + group * DW;
+                if (!failed && !warp_wait(&s_full[pos & 1], (pos / 2) & 1)) failed = true;
                 if (failed) break;
                 tc_fence_after_sync();
-                const bool cut = key0 + S::kStep > p.past;
+                const bool cut = key0 + S::kHalf > p.past;
                 float alpha = 1.f;
-                const float* sc = reinterpret_cast<const float*>(smem + S::kScaleOff + buf * S::kScaleBytes);
+                const float* sc = reinterpret_cast<const float*>(smem + S::kScaleOff + buf * S::kScaleBytes) + group * S::kHalf;
                 // the scales, or the rows of V that are looked through below (complete by now: the scores waited for them)
                 if ((kEight || cut) && !warp_wait(kEight ? &k_full[buf] : &v_full[buf], (pos / S::kVBufs) & 1)) { failed = true; break; }
                 // 32 scores of this row; the keys that it sees, as bits (cut)
@@ -390,11 +397,12 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     if (have < 32) v &= have > 0 ? (1u << have) - 1u : 0u;
                     return v;
                 };
+                float kept[S::kHalf / 32][32];
                 if (!idle) {
                     float mx = -INFINITY;
-#pragma unroll 1
-                    for (int c = 0; c < S::kStep; c += 32) {
-                        float x[32];
+#pragma unroll
+                    for (int c = 0; c < S::kHalf; c += 32) {
+                        float (&x)[32] = kept[c / 32];
                         scores(c, x);
 #pragma unroll
                         for (int k = 0; k < 32; ++k) x[k] *= mul;
@@ -413,7 +421,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         l *= alpha;
                     }
                     if constexpr (kEight) {
-                        const float big = sc[2 * S::kStep];
+                        const float big = sc[2 * S::kStep - group * S::kHalf];
                         if (big > unit) {  // the same in all threads
                             const uint32_t up = min((__float_as_uint(big) + 0x007fffffu) & 0x7f800000u, 0x7e000000u);
                             unit_inv = __uint_as_float(0x7f000000u - up);
@@ -422,8 +430,10 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                     }
                 }
-                // (the group's last product is done: these scores were asked for after it, and they are here)
-                if (g >= 2 && __any_sync(0xffffffffu, alpha != 1.f)) {
+                if (g > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
+                    // O must hold the group's products so far
+                    if (!warp_wait(&pv_done[group], (steps - 1) & 1)) { failed = true; break; }
+                    tc_fence_after_sync();
 #pragma unroll 1
                     for (int c = 0; c < DW / 32; ++c) {
                         uint32_t r[32];
@@ -437,20 +447,16 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 ++steps;
                 if (!idle) {
                     const float ref = m == -INFINITY ? 0.f : m - kRowsLift;
-#pragma unroll 1
-                    for (int c = 0; c < S::kStep; c += 32) {
-                        float x[32], add = 0.f;
-                        scores(c, x);
-                        uint32_t v = 0xffffffffu;
-                        if (cut) v = seen(c);
+#pragma unroll
+                    for (int c = 0; c < S::kHalf; c += 32) {
+                        float (&x)[32] = kept[c / 32];
+                        float add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
-                            x[k] = fmaf(x[k], mul, -ref);
-                            if (cut) x[k] = v >> k & 1u ? x[k] : -INFINITY;
-                            x[k] = ex2(x[k]);
-                            add += x[k];
+                            x[k] = ex2(x[k] - ref);
+                            add[k & 3] += x[k];
                         }
-                        l += add;
+                        l += (add[0] + add[1]) + (add[2] + add[3]);
                         if constexpr (kEight) {
 #pragma unroll
                             for (int k = 0; k < 32; k += 4) {
@@ -458,6 +464,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                                 x[k] *= vs.x * unit_inv; x[k + 1] *= vs.y * unit_inv; x[k + 2] *= vs.z * unit_inv; x[k + 3] *= vs.w * unit_inv;
                             }
                             if (cut) {  // the scale of a row that is not seen may be anything
+                                const uint32_t v = seen(c);
 #pragma unroll
                                 for (int k = 0; k < 32; ++k) x[k] = v >> k & 1u ? x[k] : 0.f;
                             }
@@ -475,15 +482,14 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         constexpr uint32_t kExp = kF16 ? 0x7c00u : 0x7f80u;
                         uint8_t* v = smem + S::kVOff + buf * S::kVEach;
                         // two threads to a key, a half of its elements each
-#pragma unroll 1
-                        for (int key = row >> 1; key < S::kStep; key += 64) {
-                            if (key0 + key < p.past) continue;
+                        const int key = row >> 1, vrow = group * S::kHalf + key;
+                        if (key0 + key >= p.past) {
                             const bool out = key0 + key >= p.rows;
                             bool odd = false;
 #pragma unroll
                             for (int i = 0; i < DW / 16; ++i) {
                                 const int piece = (row & 1) * (DW / 16) + i;
-                                uint4* at16 = reinterpret_cast<uint4*>(v + (piece >> 3) * S::kOpChunk + sw128(key, piece & 7));
+                                uint4* at16 = reinterpret_cast<uint4*>(v + (piece >> 3) * S::kOpChunk + sw128(vrow, piece & 7));
                                 uint32_t x[4] = {at16->x, at16->y, at16->z, at16->w};
                                 bool put = out;
 #pragma unroll
@@ -505,9 +511,9 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&p_ready[group]);
+                if (lane == 0) mbar_arrive(&p_ready[pos & 1][group]);
             }
-            if (!failed && n > group && !warp_wait(&pv_done[group], (steps - 1) & 1)) failed = true;
+            if (!failed && !warp_wait(&pv_done[group], (steps - 1) & 1)) failed = true;
             tc_fence_after_sync();
             base += n;
             ++parts;
@@ -527,7 +533,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 const float e0 = ex2(s0.x - ref), e1 = ex2(s1.x - ref), L = fmaf(e0, s0.y, e1 * s1.y);
                 const float w0 = kEight ? e0 * s0.z : e0, w1 = kEight ? e1 * s1.z : e1;
 #pragma unroll 1
-                for (int c = 0; c < kHalf / 32; ++c) {
+                for (int c = 0; c < kCols / 32; ++c) {
                     const int d = col0 + c * 32;
                     uint32_t r[32];
                     float x[32];
@@ -535,12 +541,10 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     tmem_ld_wait();
 #pragma unroll
                     for (int k = 0; k < 32; ++k) x[k] = __uint_as_float(r[k]) * w0;
-                    if (n > 1) {
-                        tmem_ld_x32(lanes + kColO + DW + d, r);
-                        tmem_ld_wait();
+                    tmem_ld_x32(lanes + kColO + DW + d, r);
+                    tmem_ld_wait();
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] = fmaf(__uint_as_float(r[k]), w1, x[k]);
-                    }
+                    for (int k = 0; k < 32; ++k) x[k] = fmaf(__uint_as_float(r[k]), w1, x[k]);
                     if constexpr (kEight && !kE4m3) {
 #pragma unroll
                         for (int k = 1; k < 32; k += 4) {
@@ -609,9 +613,9 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll 4
             for (int i = 0; i < ctas; ++i) M = fmaxf(M, reinterpret_cast<const float2*>(slot(cta0 + i, cut.start) + 128 * DW)[row].x);
             const float ref = M == -INFINITY ? 0.f : M;
-            float x[kHalf / 32][32];
+            float x[kCols / 32][32];
 #pragma unroll
-            for (int c = 0; c < kHalf / 32; ++c)
+            for (int c = 0; c < kCols / 32; ++c)
 #pragma unroll
                 for (int k = 0; k < 32; ++k) x[c][k] = 0.f;
 #pragma unroll 1
@@ -621,7 +625,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 const float w = ex2(ml.x - ref);
                 L = fmaf(w, ml.y, L);
 #pragma unroll
-                for (int c = 0; c < kHalf / 32; ++c) {
+                for (int c = 0; c < kCols / 32; ++c) {
                     float4 y[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) y[k] = reinterpret_cast<const float4*>(from)[(col0 / 4 + c * 8 + k) * 128 + row];
@@ -637,7 +641,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             const int T = max(a.T, 1), h = at / T;
             uint16_t* orow = out_row(cut.b, cut.kvh, h, at - h * T);
 #pragma unroll
-            for (int c = 0; c < kHalf / 32; ++c) write_out(orow, col0 + c * 32, x[c], L == 0.f ? 0.f : 1.f / L);
+            for (int c = 0; c < kCols / 32; ++c) write_out(orow, col0 + c * 32, x[c], L == 0.f ? 0.f : 1.f / L);
         }
     }
 
