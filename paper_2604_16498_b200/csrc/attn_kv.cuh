@@ -37,7 +37,7 @@ struct KvAttnArgs {
     int T;                           // tokens; their rows are the last ones of the cache (0: one token that has none)
     int B, Hkv, G, Smax, D;
     int rows, row_tiles, tile_rows;  // G * T; groups of rows (of tile_heads whole heads), and how many a group has
-    int tile_heads;
+    int tile_heads, tile_stride;     // rows between the columns of a part in the workspace
     int least;                       // blocks of keys that a CTA has at least
     bool q_f16;
     float scale_log2;
@@ -72,6 +72,12 @@ __device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4],
     else
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+__device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(ptx::smem_u32(bar))
+                 : "memory");
 }
 
 __device__ __forceinline__ int kv_past(const KvAttnArgs& a, int b) { return min(max(__ldg(a.lens + b), 0), a.Smax); }

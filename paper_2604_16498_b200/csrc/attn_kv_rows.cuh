@@ -43,9 +43,11 @@ struct RowsShape {
     static constexpr int kLoadOff = kEight ? kKOff + kOps * 2 * kOpBytes : kVOff + kVBufs * kOpBytes;
     static constexpr int kScaleOff = kLoadOff + kLoads * kLoadBytes; // 8-bit: of each operand buffer, scales of K and V and the largest of V
     static constexpr int kScaleBytes = 2 * kStep * 4 + 16;
-    static constexpr int kSmem = 1024 + kScaleOff + kOps * kScaleBytes;
+    static constexpr int kOutOff = (kScaleOff + kOps * kScaleBytes + 127) / 128 * 128;  // of each softmax warp, 32 rows x 32 elements on their way out
+    static constexpr int kSmem = 1024 + kOutOff + 8 * 2048;
     static_assert(kSmem <= 232448 - 6144, "shared memory");
-    static constexpr int kPart = 128 * DW + 256;                     // floats of a CTA's part: [DW / 4][128 rows] of four, then m and l
+    static constexpr int kPart = 128 * DW + 256;                     // floats of a CTA's part: [DW / 4][rows] of four, then m and l; at most 128 rows
+    static constexpr int kRing = (kEight ? kScaleOff : kLoadOff) - kKOff;  // bytes of rings and operands: free at the end of a run
 };
 
 // Where element 8 i of row r of a [rows][64] chunk lies: 16-byte pieces swizzled over 128-byte lines.
@@ -66,6 +68,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     extern __shared__ uint8_t smem_raw[];
     // codes (8-bit); operands of the scores and of the product with V (8-bit: complete together, k_full and k_empty serve for both)
     __shared__ uint64_t load_full[kLoads], load_empty[kLoads], k_full[S::kKBufs], k_empty[S::kKBufs], v_full[S::kVBufs], v_empty[S::kVBufs];
+    constexpr int kMergeSlots = 4;
+    __shared__ uint64_t merge_full[kMergeSlots];
     __shared__ uint64_t q_full, q_empty, q_ready, s_full[2], p_ready[2][2], pv_done[2];  // p_ready: [step % 2][group]
     __shared__ uint32_t tmem_slot;
     // what the CTA has of the items at the ends of its run, if others have parts of them; the number of these CTAs if this one was last to arrive
@@ -82,6 +86,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         for (int i = 0; i < S::kKBufs; ++i) { mbar_init(&k_full[i], kEight ? S::kConvWarps : 1); mbar_init(&k_empty[i], 1); }
         for (int i = 0; i < S::kVBufs; ++i) { mbar_init(&v_full[i], 1); mbar_init(&v_empty[i], 1); }
         mbar_init(&q_full, 1);
+        for (int i = 0; i < kMergeSlots; ++i) mbar_init(&merge_full[i], 1);
         mbar_init(&q_empty, 1);
         for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i][0], 4); mbar_init(&p_ready[i][1], 4); mbar_init(&pv_done[i], 1); }
         mbar_init(&q_ready, 4);
@@ -293,25 +298,48 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         auto out_row = [&](int b, int kvh, int h, int tok) {
             return static_cast<uint16_t*>(a.out) + b * a.os.b + (int64_t)(kvh * a.G + h) * a.os.h + tok * a.os.s;
         };
-        auto write_out = [&](uint16_t* orow, int d, const float (&x)[32], float scale) {  // elements d .. d + 31
+        // Elements d .. d + 31 of this thread's row, scaled: through shared memory, so that a warp's store covers 8 rows' 64 bytes each (16 bytes of
+        // 32 rows each take four times as long).  All lanes of the warp take part.
+        uint8_t* out_stage = smem + S::kOutOff + warp * 2048;
+        auto write_out = [&](const uint16_t* orow, bool live, int d, const float (&x)[32], float scale) {
+            auto pair = [&](float y, float z) { return out_f16 ? pack16<true>(y * scale, z * scale) : pack16<false>(y * scale, z * scale); };
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *reinterpret_cast<uint4*>(out_stage + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)) =
+                    make_uint4(pair(x[i * 8], x[i * 8 + 1]), pair(x[i * 8 + 2], x[i * 8 + 3]), pair(x[i * 8 + 4], x[i * 8 + 5]), pair(x[i * 8 + 6], x[i * 8 + 7]));
+            __syncwarp();
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                auto pair = [&](float y, float z) { return out_f16 ? pack16<true>(y * scale, z * scale) : pack16<false>(y * scale, z * scale); };
-                if (d + i * 8 < a.D)
-                    *reinterpret_cast<uint4*>(orow + d + i * 8) = make_uint4(pair(x[i * 8], x[i * 8 + 1]), pair(x[i * 8 + 2], x[i * 8 + 3]),
-                                                                             pair(x[i * 8 + 4], x[i * 8 + 5]), pair(x[i * 8 + 6], x[i * 8 + 7]));
+                const int r = i * 8 + (lane >> 2), piece = lane & 3;
+                const unsigned long long to = __shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(orow), r);
+                const bool there = __shfl_sync(0xffffffffu, live, r);
+                if (there && d + piece * 8 < a.D)
+                    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(to) + d + piece * 8) =
+                        *reinterpret_cast<const uint4*>(out_stage + r * 64 + ((piece ^ (r >> 1 & 3)) << 4));
             }
         };
         auto rows_sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
         int base = 0, parts = 0, steps = 0;  // steps: of this group
+        unsigned long long next_sees = 0;
         while (cur.u < cur.end) {
             const KvPart p = kv_part(a, cur);
             const int at = p.rt * a.tile_rows + row;                  // row of the KV head
             const bool live = row < a.tile_rows && at < a.rows;
             const bool idle = (warp & 3) * 32 >= min(a.tile_rows, a.rows - p.rt * a.tile_rows);  // the whole warp has no row
             const int T = max(a.T, 1), h = at / T, tok = at - h * T;
-            unsigned long long sees = 0;
-            if (live && a.T > 0) sees = a.tree ? a.tree[(int64_t)p.b * a.tree_stride + tok] : (2ull << tok) - 1ull;
+            // the mask of this row's token, and that of the next item of the run: asked for now, behind the copies in flight it is long in coming
+            auto mask_of = [&](const KvPart& at_part) -> unsigned long long {
+                const int r = at_part.rt * a.tile_rows + row, t = r - r / T * T;
+                if (a.T == 0 || row >= a.tile_rows || r >= a.rows) return 0;
+                return a.tree ? a.tree[(int64_t)at_part.b * a.tree_stride + t] : (2ull << t) - 1ull;
+            };
+            const unsigned long long sees = parts == 0 ? mask_of(p) : next_sees;
+            {
+                KvCursor then = cur;
+                kv_advance<S::kStep>(a, then, p.tiles);
+                if (then.u < then.end) next_sees = mask_of(kv_part(a, then));
+            }
             float mul = a.scale_log2;
             if constexpr (kEight) {
                 // ---- group 0: the row of Q, in place, to fp16 in the codes' order, scaled by a power of two that puts its largest into
@@ -564,16 +592,15 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             if (!(fabsf(y) <= 3.4028235e38f)) x[k] += y;
                         }
                     }
-                    if (!live) continue;
                     if (whole) {
-                        write_out(orow, d, x, L == 0.f ? 0.f : 1.f / L);  // no key seen: zeros
-                    } else {
+                        write_out(orow, live, d, x, L == 0.f ? 0.f : 1.f / L);  // no key seen: zeros
+                    } else if (live) {
 #pragma unroll
                         for (int k = 0; k < 8; ++k)
-                            reinterpret_cast<float4*>(mine)[(d / 4 + k) * 128 + row] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+                            reinterpret_cast<float4*>(mine)[(d / 4 + k) * a.tile_stride + row] = make_float4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
                     }
                 }
-                if (!whole && live && group == 0) reinterpret_cast<float2*>(mine + 128 * DW)[row] = make_float2(M, L);
+                if (!whole && live && group == 0) reinterpret_cast<float2*>(mine + a.tile_stride * DW)[row] = make_float2(M, L);
             }
             tc_fence_before_sync();
             rows_sync();  // the parts are written; odd_keys and O have been read
@@ -601,47 +628,67 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             }
         }
         rows_sync();
+        uint32_t merge_phase = 0;  // a bit for each slot
 #pragma unroll 1
         for (int e = 0; e < 2; ++e) {
             const int ctas = cut_last[e];
-            if (ctas == 0 || failed) continue;
+            if (ctas == 0) continue;
             const Cut cut = cuts[e];
+            // The parts come by bulk copies into the rings, which are free by now, a few ahead of the one that is added.
+            const int cta0 = shares.of(cut.start), bytes = a.tile_stride * (DW + 2) * 4, slots = min(S::kRing / bytes, kMergeSlots);
             const int at = cut.rt * a.tile_rows + row;
-            if (row >= a.tile_rows || at >= a.rows) continue;
-            const int cta0 = shares.of(cut.start);
-            float M = -INFINITY, L = 0.f;
-#pragma unroll 4
-            for (int i = 0; i < ctas; ++i) M = fmaxf(M, reinterpret_cast<const float2*>(slot(cta0 + i, cut.start) + 128 * DW)[row].x);
-            const float ref = M == -INFINITY ? 0.f : M;
-            float x[kCols / 32][32];
+            const bool live = row < a.tile_rows && at < a.rows;
+            auto copy = [&](int i) {  // thread 0
+                uint64_t* full = &merge_full[i % slots];
+                mbar_expect_tx(full, bytes);
+                bulk_load(smem_u32(smem + S::kKOff + i % slots * bytes), slot(cta0 + i, cut.start), bytes, full);
+            };
+            if (threadIdx.x == 0) {
+                asm volatile("fence.proxy.async;" ::: "memory");  // what other SMs wrote with plain stores is read by the copy engine
+                for (int i = 0; i < min(slots, ctas); ++i) copy(i);
+            }
+            float M = -INFINITY, L = 0.f, x[kCols / 32][32];
 #pragma unroll
             for (int c = 0; c < kCols / 32; ++c)
 #pragma unroll
                 for (int k = 0; k < 32; ++k) x[c][k] = 0.f;
 #pragma unroll 1
             for (int i = 0; i < ctas; ++i) {
-                const float* from = slot(cta0 + i, cut.start);
-                const float2 ml = reinterpret_cast<const float2*>(from + 128 * DW)[row];
-                const float w = ex2(ml.x - ref);
-                L = fmaf(w, ml.y, L);
+                const int sl = i % slots;
+                if (!failed && !warp_wait(&merge_full[sl], merge_phase >> sl & 1u)) failed = true;
+                merge_phase ^= 1u << sl;
+                const uint8_t* from = smem + S::kKOff + sl * bytes;
+                if (live) {
+                    const float2 ml = reinterpret_cast<const float2*>(from + a.tile_stride * DW * 4)[row];
+                    if (ml.x > M) {
+                        const float again = ex2(M - ml.x);  // 0 for the first
+                        M = ml.x;
+                        L *= again;
 #pragma unroll
-                for (int c = 0; c < kCols / 32; ++c) {
-                    float4 y[8];
+                        for (int c = 0; c < kCols / 32; ++c)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) y[k] = reinterpret_cast<const float4*>(from)[(col0 / 4 + c * 8 + k) * 128 + row];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) {
-                        x[c][4 * k] = fmaf(w, y[k].x, x[c][4 * k]);
-                        x[c][4 * k + 1] = fmaf(w, y[k].y, x[c][4 * k + 1]);
-                        x[c][4 * k + 2] = fmaf(w, y[k].z, x[c][4 * k + 2]);
-                        x[c][4 * k + 3] = fmaf(w, y[k].w, x[c][4 * k + 3]);
+                            for (int k = 0; k < 32; ++k) x[c][k] *= again;
                     }
+                    const float w = ex2(ml.x - (M == -INFINITY ? 0.f : M));
+                    L = fmaf(w, ml.y, L);
+#pragma unroll
+                    for (int c = 0; c < kCols / 32; ++c)
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            const float4 y = reinterpret_cast<const float4*>(from)[(col0 / 4 + c * 8 + k) * a.tile_stride + row];
+                            x[c][4 * k] = fmaf(w, y.x, x[c][4 * k]);
+                            x[c][4 * k + 1] = fmaf(w, y.y, x[c][4 * k + 1]);
+                            x[c][4 * k + 2] = fmaf(w, y.z, x[c][4 * k + 2]);
+                            x[c][4 * k + 3] = fmaf(w, y.w, x[c][4 * k + 3]);
+                        }
                 }
+                rows_sync();  // read before the next copy lands
+                if (threadIdx.x == 0 && i + slots < ctas && !failed) copy(i + slots);
             }
             const int T = max(a.T, 1), h = at / T;
-            uint16_t* orow = out_row(cut.b, cut.kvh, h, at - h * T);
+            const uint16_t* orow = out_row(cut.b, cut.kvh, h, at - h * T);
 #pragma unroll
-            for (int c = 0; c < kCols / 32; ++c) write_out(orow, col0 + c * 32, x[c], L == 0.f ? 0.f : 1.f / L);
+            for (int c = 0; c < kCols / 32; ++c) write_out(orow, live && !failed, col0 + c * 32, x[c], L == 0.f ? 0.f : 1.f / L);
         }
     }
 
