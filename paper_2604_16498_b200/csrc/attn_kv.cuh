@@ -6,10 +6,9 @@
 // and what is computed over different keys is merged with the usual 2^(m - M) weights.  8-bit rows enter the products as codes
 // (exact in fp16); their scales multiply the score and the probability: q.k_j = ks_j (q.kc_j), p_j v_j = (p_j vs_j) vc_j.
 //
-// The work is bound by reading K and V once, and with many rows by the tensor cores.  All CTAs (one per SM) share the blocks of keys of the
-// whole call evenly: they are numbered through sequences, KV heads and row tiles, and each CTA takes a run of them.  What a cut leaves in
-// several CTAs is merged by the one that finishes last (arrival counters); a CTA has at most two such parts.  Up to 8 rows
-// run on attn_kv_narrow.cuh (warp-level products with the keys as the 16-row operand), more on attn_kv_rows.cuh (tcgen05, a tile of 128 rows).
+// The work is bound by reading K and V once, and with many rows by the tensor cores.  One CTA per SM; a long sequence is shared by several, and
+// what they have of it is merged by the one that finishes last (arrival counters).  Up to 8 rows run on attn_kv_narrow.cuh (warp-level
+// products with the keys as the 16-row operand), more on attn_kv_rows.cuh (tcgen05, a tile of 128 rows).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -83,16 +82,28 @@ __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, ui
 __device__ __forceinline__ int kv_past(const KvAttnArgs& a, int b) { return min(max(__ldg(a.lens + b), 0), a.Smax); }
 // Rows that any token of the sequence may see.
 __device__ __forceinline__ int kv_rows(const KvAttnArgs& a, int past) { return min(past + a.T, a.Smax); }
-// Tiles of KEYS keys of a (sequence, KV head, row group): one at least, so that a sequence without rows gets its zeros.
+// Tiles of KEYS keys of a (sequence, KV head): one at least, so that a sequence without rows gets its zeros.
 template <int KEYS>
 __device__ __forceinline__ int kv_tiles(const KvAttnArgs& a, int past) { return max((kv_rows(a, past) + KEYS - 1) / KEYS, 1); }
 
-// Where a CTA is in the call's tiles.  Every warp walks through the CTA's share by itself; all lanes hold the same.
+// A sequence of the call: its number, its first tile (of all its KV heads), its past and the tiles of one (KV head, row tile).
 struct KvCursor {
-    int u, end;          // tiles of the call: the next one, and the end of this CTA's share
-    int b, base;         // sequence, and its first tile
-    int past, tiles;     // of sequence b
+    int b, base, past, tiles;
 };
+
+__device__ __forceinline__ int kv_scan(int v, int lane) {  // inclusive sum over lanes
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+__device__ __forceinline__ int kv_sum(int v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
 
 // Whole numbers 0 .. n - 1 shared evenly by `by` (at most n) of them, in order: the first n % by get one more than the others.
 struct KvShares {
@@ -105,8 +116,8 @@ struct KvShares {
     }
 };
 
-// The call's tiles, which W CTAs share (at least `least` each), and the sequence in which tile u lies: `at(...)` leaves its b, base, past and
-// tiles in the cursor.  Lane l keeps what there is to know of sequence l, so that up to 32 sequences are read once.
+// The call's tiles of up to 8 rows, which W CTAs share (at least `least` each), and the sequence in which tile u lies.  Lane l keeps what there
+// is to know of sequence l, so that up to 32 sequences are read once.
 template <int KEYS>
 struct KvSchedule {
     int N, W;
@@ -114,27 +125,17 @@ struct KvSchedule {
     __device__ __forceinline__ KvSchedule(const KvAttnArgs& a, int least, int lane) {
         past0 = lane < a.B ? kv_past(a, lane) : 0;
         tiles0 = lane < a.B ? kv_tiles<KEYS>(a, past0) : 0;
-        incl0 = scan(tiles0, lane);
+        incl0 = kv_scan(tiles0, lane);
         int total = tiles0;
         for (int b = 32 + lane; b < a.B; b += 32) total += kv_tiles<KEYS>(a, kv_past(a, b));
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-        N = total * a.Hkv * a.row_tiles;
+        N = kv_sum(total) * a.Hkv;
         W = min((int)gridDim.x, (N + least - 1) / least);
-    }
-    static __device__ __forceinline__ int scan(int v, int lane) {
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, v, o);
-            if (lane >= o) v += t;
-        }
-        return v;
     }
     __device__ __forceinline__ int past_of(const KvAttnArgs& a, int b) const {  // the same b in all lanes
         return b < 32 ? __shfl_sync(0xffffffffu, past0, b) : kv_past(a, b);
     }
     __device__ __forceinline__ void at(const KvAttnArgs& a, int u, KvCursor& cur, int lane) const {
-        const int per = a.Hkv * a.row_tiles;
+        const int per = a.Hkv;
         int before = 0, past = past0, tiles = tiles0, incl = incl0;
 #pragma unroll 1
         for (int b0 = 0;; b0 += 32) {
@@ -150,42 +151,10 @@ struct KvSchedule {
             before += __shfl_sync(0xffffffffu, incl, 31);
             past = b0 + 32 + lane < a.B ? kv_past(a, b0 + 32 + lane) : 0;
             tiles = b0 + 32 + lane < a.B ? kv_tiles<KEYS>(a, past) : 0;
-            incl = scan(tiles, lane);
+            incl = kv_scan(tiles, lane);
         }
     }
 };
-
-// The CTA's part of one (sequence, KV head, row group).
-struct KvPart {
-    int b, kvh, rt, item;      // item: number of the (sequence, KV head, row group)
-    int first, tiles, of;      // tiles of it in this CTA, out of how many
-    int start;                 // the item's first tile in the call
-    int past, rows;
-};
-__device__ __forceinline__ KvPart kv_part(const KvAttnArgs& a, const KvCursor& cur) {
-    KvPart p;
-    const int in = cur.u - cur.base, item = in / cur.tiles;
-    p.b = cur.b;
-    p.kvh = item / a.row_tiles;
-    p.rt = item - p.kvh * a.row_tiles;
-    p.item = cur.b * a.Hkv * a.row_tiles + item;
-    p.first = in - item * cur.tiles;
-    p.of = cur.tiles;
-    p.tiles = min(cur.tiles - p.first, cur.end - cur.u);
-    p.start = cur.u - p.first;
-    p.past = cur.past;
-    p.rows = kv_rows(a, cur.past);
-    return p;
-}
-template <int KEYS>
-__device__ __forceinline__ void kv_advance(const KvAttnArgs& a, KvCursor& cur, int tiles) {
-    cur.u += tiles;
-    if (cur.u < cur.end && cur.u - cur.base >= cur.tiles * a.Hkv * a.row_tiles) {
-        cur.base += cur.tiles * a.Hkv * a.row_tiles;
-        cur.past = kv_past(a, ++cur.b);
-        cur.tiles = kv_tiles<KEYS>(a, cur.past);
-    }
-}
 
 }  // namespace
 }  // namespace forge

@@ -5,9 +5,11 @@
 // a product 128 x 64 would read Q from shared memory twice as often as the tensor cores need it) or 64 (8-bit)
 //     S[128 x keys] = Q K^T  and  O[128 x DW] += P V   by tcgen05.mma, with S (two steps' worth), P and O in tensor memory,
 // and thread = row does the softmax in between.  Each half of a step's keys belongs to a group of softmax threads with references, sums and an O
-// of its own; the two are merged when the CTA's part of an item ends.  The call's steps are shared evenly by all CTAs, as in the other kernel,
-// and what a CTA has of an item that others have parts of too is merged by the one that finishes last, after its whole run: loads in the
-// middle of it would wait behind the copies in flight.
+// of its own; the two are merged when a piece ends.  Every item (sequence, KV head, row tile) is cut into pieces of C steps, with one C for the
+// call, so that a CTA has one piece, if that can be had: changing the item costs as much as three steps, and a second merge
+// as much as four (with the steps shared out evenly, the runs of most CTAs going over the end of an item, 4 x 32/8 x 64 tokens took
+// 36 us).  The pieces of an item are merged by the CTA that finishes last, after all its pieces: loads between them would wait behind
+// the copies in flight.
 //   warps 0-7   softmax (two groups of 128 threads), O out      warp 8  TMA      warp 9  tcgen05.mma
 //   warps 10-13 8-bit rows only: codes of K and V to fp16, from the copies' ring into operands
 // 8-bit rows stay codes in the products (exact in fp16; int8 elements come in the order 0 2 1 3 of each four, in Q and O too); their scales
@@ -50,6 +52,85 @@ struct RowsShape {
     static constexpr int kRing = (kEight ? kScaleOff : kLoadOff) - kKOff;  // bytes of rings and operands: free at the end of a run
 };
 
+// The call's pieces: those of items with several come first, and number i of them has place i in the workspace.
+template <int STEP>
+struct RowsPieces {
+    int C, cut, all;               // steps of a piece; pieces of items with several, and of all
+    int past0, tiles0;             // of sequence `lane`
+    static __device__ __forceinline__ int pieces(int tiles, int C) { return (tiles + C - 1) / C; }
+    // The smallest C that gives each CTA its share of the steps; up to twice that if then no CTA has two pieces.
+    __device__ __forceinline__ RowsPieces(const KvAttnArgs& a, int ctas, int lane) {
+        const int per = a.Hkv * a.row_tiles;
+        past0 = lane < a.B ? kv_past(a, lane) : 0;
+        tiles0 = lane < a.B ? kv_tiles<STEP>(a, past0) : 0;
+        int total = tiles0;
+        for (int b = 32 + lane; b < a.B; b += 32) total += kv_tiles<STEP>(a, kv_past(a, b));
+        const int N = kv_sum(total) * per, low = max((N + ctas - 1) / ctas, a.least);
+        C = low;
+        count(a, lane);
+        for (int c = low; all > ctas && c < 2 * low;) {
+            c += max(c >> 4, 1);
+            C = c;
+            count(a, lane);
+        }
+        if (all > ctas && C > low) {
+            C = low;
+            count(a, lane);
+        }
+    }
+    __device__ __forceinline__ void count(const KvAttnArgs& a, int lane) {
+        const int per = a.Hkv * a.row_tiles;
+        int n = lane < a.B ? pieces(tiles0, C) : 0, m = n > 1 ? n : 0;
+        for (int b = 32 + lane; b < a.B; b += 32) {
+            const int x = pieces(kv_tiles<STEP>(a, kv_past(a, b)), C);
+            n += x;
+            m += x > 1 ? x : 0;
+        }
+        all = kv_sum(n) * per;
+        cut = kv_sum(m) * per;
+    }
+};
+// Piece number idx.
+struct RowsPiece {
+    int b, kvh, rt, item;          // item: number of the (sequence, KV head, row tile)
+    int first, tiles;              // its steps
+    int start, of;                 // the item's pieces: number of the first, and how many
+    int past, rows;
+};
+template <int STEP>
+__device__ __forceinline__ RowsPiece rows_piece(const KvAttnArgs& a, const RowsPieces<STEP>& ps, int idx, int lane) {
+    const int per = a.Hkv * a.row_tiles;
+    const bool is_cut = idx < ps.cut;
+    const int at = is_cut ? idx : idx - ps.cut;  // among those with several pieces, or among the others
+    RowsPiece p;
+    int before = 0, past = ps.past0, tiles = ps.tiles0;
+#pragma unroll 1
+    for (int b0 = 0;; b0 += 32) {
+        int n = b0 + lane < a.B ? RowsPieces<STEP>::pieces(tiles, ps.C) : 0;
+        if ((n > 1) != is_cut) n = 0;
+        const int incl = kv_scan(n, lane);
+        const unsigned hit = __ballot_sync(0xffffffffu, at < (before + incl) * per);
+        if (hit || b0 + 32 >= a.B) {
+            const int src = hit ? __ffs(hit) - 1 : 0;
+            p.b = b0 + src;
+            p.of = __shfl_sync(0xffffffffu, n, src);
+            p.past = __shfl_sync(0xffffffffu, past, src);
+            const int first = (before + __shfl_sync(0xffffffffu, incl, src) - p.of) * per, in = at - first, item = in / p.of;
+            p.kvh = item / a.row_tiles;
+            p.rt = item - p.kvh * a.row_tiles;
+            p.item = p.b * per + item;
+            p.start = first + item * p.of;  // (of items with several)
+            p.first = (in - item * p.of) * ps.C;
+            p.tiles = min(ps.C, __shfl_sync(0xffffffffu, tiles, src) - p.first);
+            p.rows = kv_rows(a, p.past);
+            return p;
+        }
+        before += __shfl_sync(0xffffffffu, incl, 31);
+        past = b0 + 32 + lane < a.B ? kv_past(a, b0 + 32 + lane) : 0;
+        tiles = b0 + 32 + lane < a.B ? kv_tiles<STEP>(a, past) : 0;
+    }
+}
+
 // Where element 8 i of row r of a [rows][64] chunk lies: 16-byte pieces swizzled over 128-byte lines.
 __device__ __forceinline__ uint32_t sw128(int r, int piece) { return r * 128 + ((piece ^ (r & 7)) << 4); }
 
@@ -72,8 +153,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     __shared__ uint64_t merge_full[kMergeSlots];
     __shared__ uint64_t q_full, q_empty, q_ready, s_full[2], p_ready[2][2], pv_done[2];  // p_ready: [step % 2][group]
     __shared__ uint32_t tmem_slot;
-    // what the CTA has of the items at the ends of its run, if others have parts of them; the number of these CTAs if this one was last to arrive
-    struct Cut { int item, start, tiles, b, kvh, rt; };
+    // items that the CTA had a piece of several of; whether it was the last to arrive
+    struct Cut { int item, start, of, b, kvh, rt; };
     __shared__ Cut cuts[2];
     __shared__ int cut_last[2];
     __shared__ int odd_keys[kMaxOdd], odd_count;  // halves of rows of V with elements that are not finite numbers, which some of the tokens see
@@ -95,7 +176,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         prefetch_tmap(&tmap_k);
         prefetch_tmap(&tmap_v);
         odd_count = 0;
-        cuts[0].tiles = cuts[1].tiles = 0;
+        cuts[0].of = cuts[1].of = 0;
     }
     if (warp == 9) {
         tmem_alloc(&tmem_slot, kTmemCols);
@@ -108,38 +189,30 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     pdl_launch_dependents();
     pdl_wait();
 
-    const KvSchedule<S::kStep> sched(a, a.least, lane);
-    const KvShares shares(sched.N, sched.W);
-    KvCursor cur;
-    cur.u = cur.end = 0;
-    if ((int)blockIdx.x < sched.W) {
-        cur.u = shares.first(blockIdx.x);
-        cur.end = shares.first(blockIdx.x + 1);
-        sched.at(a, cur.u, cur, lane);
-    }
+    const int ctas = gridDim.x;
+    const RowsPieces<S::kStep> pieces(a, ctas, lane);
     bool failed = false;
 
     if (warp == 8) {
         // ------------------------------------------------------------------ copies
-        if (elect_one()) {
-            // rows that only one row tile reads are marked first to go from L2
-            const uint64_t policy = a.row_tiles == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
-            int n = 0, parts = 0;
-            while (cur.u < cur.end && !failed) {
-                const KvPart p = kv_part(a, cur);
+        // rows that only one row tile reads are marked first to go from L2
+        const uint64_t policy = a.row_tiles == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
+        int n = 0, parts = 0;
+        for (int idx = blockIdx.x; idx < pieces.all; idx += ctas) {
+            const RowsPiece p = rows_piece(a, pieces, idx, lane);
+            if (elect_one()) {
                 const int bk = p.b * a.Hkv + p.kvh;
-                if (parts > 0 && !mbar_wait_relaxed(&q_empty, (parts - 1) & 1)) { failed = true; break; }
-                mbar_expect_tx(&q_full, a.tile_rows * (DW * 2));
+                if (parts > 0 && !failed && !mbar_wait_relaxed(&q_empty, (parts - 1) & 1)) failed = true;
+                if (!failed) mbar_expect_tx(&q_full, a.tile_rows * (DW * 2));
 #pragma unroll
-                for (int c = 0; c < DW / 64; ++c)
+                for (int c = 0; c < DW / 64 && !failed; ++c)
                     tma_load_4d(smem + c * S::kQChunk, &tmap_q, &q_full, c * 64, 0, p.kvh * a.G + p.rt * a.tile_heads, p.b);
-                ++parts;
-                for (int t = 0; t < p.tiles; ++t, ++n) {
+                for (int t = 0; t < p.tiles && !failed; ++t) {
                     const int j0 = (p.first + t) * S::kStep;
                     const bool none = j0 >= p.rows;  // a sequence without rows
                     if constexpr (kEight) {
-                        const int st = n % kLoads;
-                        if (n >= kLoads && !mbar_wait_relaxed(&load_empty[st], (n / kLoads - 1) & 1)) { failed = true; break; }
+                        const int pos = n + t, st = pos % kLoads;
+                        if (pos >= kLoads && !mbar_wait_relaxed(&load_empty[st], (pos / kLoads - 1) & 1)) { failed = true; break; }
                         if (none) { mbar_arrive(&load_full[st]); continue; }
                         const uint32_t dst = smem_u32(smem + S::kLoadOff + st * S::kLoadBytes);
                         const int x = (bk * a.Smax + j0) & ~3;
@@ -149,8 +222,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         tma_load_3d_addr_hint(dst + S::kRawBytes, &tmap_v, &load_full[st], 0, j0, bk, policy);
                         tma_load_1d(dst + 2 * S::kRawBytes + S::kScaleBox, &tmap_vs, &load_full[st], x);
                     } else {
-                        const int kb = n % S::kKBufs, vb = n % S::kVBufs;
-                        if (n >= S::kKBufs && !mbar_wait_relaxed(&k_empty[kb], (n / S::kKBufs - 1) & 1)) { failed = true; break; }
+                        const int pos = n + t, kb = pos % S::kKBufs, vb = pos % S::kVBufs;
+                        if (pos >= S::kKBufs && !mbar_wait_relaxed(&k_empty[kb], (pos / S::kKBufs - 1) & 1)) { failed = true; break; }
                         if (none) {
                             mbar_arrive(&k_full[kb]);
                         } else {
@@ -159,7 +232,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             for (int c = 0; c < DW / 64; ++c)
                                 tma_load_3d_addr_hint(smem_u32(smem + S::kKOff + kb * S::kKEach + c * S::kOpChunk), &tmap_k, &k_full[kb], c * 64, j0, bk, policy);
                         }
-                        if (n >= S::kVBufs && !mbar_wait_relaxed(&v_empty[vb], (n / S::kVBufs - 1) & 1)) { failed = true; break; }
+                        if (pos >= S::kVBufs && !mbar_wait_relaxed(&v_empty[vb], (pos / S::kVBufs - 1) & 1)) { failed = true; break; }
                         if (none) {
                             mbar_arrive(&v_full[vb]);
                         } else {
@@ -170,18 +243,20 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                     }
                 }
-                kv_advance<S::kStep>(a, cur, p.tiles);
             }
+            __syncwarp();
+            n += p.tiles;
+            ++parts;
         }
     } else if (warp == 9) {
         // ------------------------------------------------------------------ products
         constexpr uint32_t idesc_s = kF16 ? make_idesc_f16(128, S::kStep, false, false) : make_idesc_bf16(128, S::kStep, false, false);
         constexpr uint32_t idesc_o = kF16 ? make_idesc_f16(128, DW, false, true) : make_idesc_bf16(128, DW, false, true);
-        if (elect_one()) {
-            int base = 0, parts = 0;  // steps and parts before this part
-            while (cur.u < cur.end && !failed) {
-                const KvPart p = kv_part(a, cur);
-                const int n = p.tiles;
+        int base = 0, parts = 0;  // steps and pieces before this one
+        for (int idx = blockIdx.x; idx < pieces.all; idx += ctas) {
+            const RowsPiece p = rows_piece(a, pieces, idx, lane);
+            const int n = p.tiles;
+            if (elect_one() && !failed) {
                 const uint64_t qd = make_smem_desc(smem_u32(smem), 16, 1024);
                 auto issue_qk = [&](int g) -> bool {
                     const int pos = base + g, buf = pos % S::kKBufs;
@@ -200,8 +275,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 const bool have_q = kEight ? mbar_wait(&q_ready, parts & 1) : mbar_wait(&q_full, parts & 1);
                 failed = !have_q;
                 for (int g = 0; g < n && g < 2 && !failed; ++g) failed = !issue_qk(g);
-                if (failed) break;
-                for (int g = 0; g < n; ++g) {
+                for (int g = 0; g < n && !failed; ++g) {
                     const int pos = base + g, buf = pos % S::kVBufs;
                     if (!kEight && !mbar_wait(&v_full[buf], (pos / S::kVBufs) & 1)) { failed = true; break; }
                     const uint64_t vd = make_smem_desc(smem_u32(smem + S::kVOff + buf * S::kVEach), S::kOpChunk, 1024);
@@ -219,18 +293,18 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     mma_commit(kEight ? &k_empty[buf] : &v_empty[buf]);
                     if (g + 2 < n && !issue_qk(g + 2)) { failed = true; break; }
                 }
-                base += n;
-                ++parts;
-                kv_advance<S::kStep>(a, cur, n);
             }
+            __syncwarp();
+            base += n;
+            ++parts;
         }
     } else if (kEight && warp >= 10) {
         // ------------------------------------------------------------------ codes to fp16
         constexpr int kOps = S::kOps ? S::kOps : 1;
         const int t = threadIdx.x - 10 * 32;
         int n = 0;
-        while (cur.u < cur.end && !failed) {
-            const KvPart p = kv_part(a, cur);
+        for (int idx = blockIdx.x; idx < pieces.all && !failed; idx += ctas) {
+            const RowsPiece p = rows_piece(a, pieces, idx, lane);
             for (int i = 0; i < p.tiles; ++i, ++n) {
                 const int st = n % kLoads, buf = n % kOps, j0 = (p.first + i) * S::kStep;
                 if (!warp_wait(&load_full[st], (n / kLoads) & 1)) { failed = true; break; }
@@ -283,15 +357,12 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     mbar_arrive(&load_empty[st]);
                 }
             }
-            kv_advance<S::kStep>(a, cur, p.tiles);
         }
     } else if (warp < 8) {
         // ------------------------------------------------------------------ softmax, O
         const int group = warp >> 2, row = threadIdx.x & 127;
         const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-        auto slot = [&](int cta, int start) {  // an item that covers a CTA's first step has its first place
-            return a.parts + (size_t)(cta * 2 + (start > shares.first(cta) ? 1 : 0)) * S::kPart;
-        };
+        auto slot = [&](int piece) { return a.parts + (size_t)piece * S::kPart; };
         const bool out_f16 = kEight ? a.q_f16 : kF16;
         constexpr int kCols = DW / 2;
         const int col0 = (warp >> 2) * kCols;  // a group of threads writes a half of O's columns
@@ -322,24 +393,20 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         auto rows_sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
         int base = 0, parts = 0, steps = 0;  // steps: of this group
         unsigned long long next_sees = 0;
-        while (cur.u < cur.end) {
-            const KvPart p = kv_part(a, cur);
+        for (int idx = blockIdx.x; idx < pieces.all; idx += ctas) {
+            const RowsPiece p = rows_piece(a, pieces, idx, lane);
             const int at = p.rt * a.tile_rows + row;                  // row of the KV head
             const bool live = row < a.tile_rows && at < a.rows;
             const bool idle = (warp & 3) * 32 >= min(a.tile_rows, a.rows - p.rt * a.tile_rows);  // the whole warp has no row
             const int T = max(a.T, 1), h = at / T, tok = at - h * T;
-            // the mask of this row's token, and that of the next item of the run: asked for now, behind the copies in flight it is long in coming
-            auto mask_of = [&](const KvPart& at_part) -> unsigned long long {
-                const int r = at_part.rt * a.tile_rows + row, t = r - r / T * T;
+            // the mask of this row's token, and that of the next piece: asked for now, behind the copies in flight it is long in coming
+            auto mask_of = [&](const RowsPiece& of) -> unsigned long long {
+                const int r = of.rt * a.tile_rows + row, t = r - r / T * T;
                 if (a.T == 0 || row >= a.tile_rows || r >= a.rows) return 0;
-                return a.tree ? a.tree[(int64_t)at_part.b * a.tree_stride + t] : (2ull << t) - 1ull;
+                return a.tree ? a.tree[(int64_t)of.b * a.tree_stride + t] : (2ull << t) - 1ull;
             };
             const unsigned long long sees = parts == 0 ? mask_of(p) : next_sees;
-            {
-                KvCursor then = cur;
-                kv_advance<S::kStep>(a, then, p.tiles);
-                if (then.u < then.end) next_sees = mask_of(kv_part(a, then));
-            }
+            if (idx + ctas < pieces.all) next_sees = mask_of(rows_piece(a, pieces, idx + ctas, lane));
             float mul = a.scale_log2;
             if constexpr (kEight) {
                 // ---- group 0: the row of Q, in place, to fp16 in the codes' order, scaled by a power of two that puts its largest into
@@ -551,10 +618,10 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 
             // ---- the two groups' O together, normalised or not, a half of the columns for each group of threads;
             // int8: column 4 i + 1 holds element 4 i + 2 and the other way round
-            const bool whole = p.tiles == p.of;
+            const bool whole = p.of == 1;
             uint16_t* orow = out_row(p.b, p.kvh, h, tok);
             const int odds = kEight ? 0 : min(odd_count, kMaxOdd);
-            float* mine = slot(blockIdx.x, p.start);
+            float* mine = slot(idx);  // (of an item with several pieces)
             if (!idle && !failed) {
                 const float4 s0 = group_state[0][row], s1 = group_state[1][row];
                 const float M = fmaxf(s0.x, s1.x), ref = M == -INFINITY ? 0.f : M;
@@ -606,9 +673,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             rows_sync();  // the parts are written; odd_keys and O have been read
             if (threadIdx.x == 0) {
                 odd_count = 0;
-                if (!whole) cuts[p.start > shares.first(blockIdx.x) ? 1 : 0] = {p.item, p.start, p.of, p.b, p.kvh, p.rt};
+                if (!whole) cuts[idx / ctas] = {p.item, p.start, p.of, p.b, p.kvh, p.rt};  // at most two of them: they come first, and are no more than twice the CTAs
             }
-            kv_advance<S::kStep>(a, cur, n);
         }
 
         // ---- items that other CTAs have parts of: the CTA that arrives last merges all of them
@@ -617,13 +683,12 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             const int e = threadIdx.x / 32;
             const Cut cut = cuts[e];
             cut_last[e] = 0;
-            if (cut.tiles > 0) {
-                const int ctas = shares.of(cut.start + cut.tiles - 1) - shares.of(cut.start) + 1;
+            if (cut.of > 0) {
                 unsigned int before;
                 asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.counters + cut.item) : "memory");
-                if (before + 1 == (unsigned)ctas) {
+                if (before + 1 == (unsigned)cut.of) {
                     a.counters[cut.item] = 0;  // as the next call expects it
-                    cut_last[e] = ctas;
+                    cut_last[e] = 1;
                 }
             }
         }
@@ -631,21 +696,20 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         uint32_t merge_phase = 0;  // a bit for each slot
 #pragma unroll 1
         for (int e = 0; e < 2; ++e) {
-            const int ctas = cut_last[e];
-            if (ctas == 0) continue;
+            if (!cut_last[e]) continue;
             const Cut cut = cuts[e];
             // The parts come by bulk copies into the rings, which are free by now, a few ahead of the one that is added.
-            const int cta0 = shares.of(cut.start), bytes = a.tile_stride * (DW + 2) * 4, slots = min(S::kRing / bytes, kMergeSlots);
+            const int bytes = a.tile_stride * (DW + 2) * 4, slots = min(S::kRing / bytes, kMergeSlots);
             const int at = cut.rt * a.tile_rows + row;
             const bool live = row < a.tile_rows && at < a.rows;
             auto copy = [&](int i) {  // thread 0
                 uint64_t* full = &merge_full[i % slots];
                 mbar_expect_tx(full, bytes);
-                bulk_load(smem_u32(smem + S::kKOff + i % slots * bytes), slot(cta0 + i, cut.start), bytes, full);
+                bulk_load(smem_u32(smem + S::kKOff + i % slots * bytes), slot(cut.start + i), bytes, full);
             };
             if (threadIdx.x == 0) {
                 asm volatile("fence.proxy.async;" ::: "memory");  // what other SMs wrote with plain stores is read by the copy engine
-                for (int i = 0; i < min(slots, ctas); ++i) copy(i);
+                for (int i = 0; i < min(slots, cut.of); ++i) copy(i);
             }
             float M = -INFINITY, L = 0.f, x[kCols / 32][32];
 #pragma unroll
@@ -653,7 +717,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                 for (int k = 0; k < 32; ++k) x[c][k] = 0.f;
 #pragma unroll 1
-            for (int i = 0; i < ctas; ++i) {
+            for (int i = 0; i < cut.of; ++i) {
                 const int sl = i % slots;
                 if (!failed && !warp_wait(&merge_full[sl], merge_phase >> sl & 1u)) failed = true;
                 merge_phase ^= 1u << sl;
@@ -683,7 +747,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                 }
                 rows_sync();  // read before the next copy lands
-                if (threadIdx.x == 0 && i + slots < ctas && !failed) copy(i + slots);
+                if (threadIdx.x == 0 && i + slots < cut.of && !failed) copy(i + slots);
             }
             const int T = max(a.T, 1), h = at / T;
             const uint16_t* orow = out_row(cut.b, cut.kvh, h, at - h * T);
@@ -693,7 +757,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     }
 
     if (failed) {
-        if (lane == 0) atomicExch(a.status, 1);
+        atomicExch(a.status, 1);
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // let copies and products in flight end before their memory goes away
     }
     tc_fence_before_sync();
