@@ -599,7 +599,7 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     }
 
     // Registers warp, warp + 8, ... of a fragment of O^T in this lane, summed over several fragments; a few at a time, whose loads leave
-    // together.  of(i): the i-th, or nullptr.
+    // together.  of(i): the i-th.
     constexpr int kMine = KS * 4 / kNarrowWarps;
     float sum[kMine], M[2], L[2];
     auto sum_over = [&](int n_of, auto of) {
@@ -614,12 +614,12 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
             float x[kAtOnce][kMine];
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) {
-                const float* f = i0 + i < n_of ? of(i0 + i) : nullptr;
+                const float* f = of(min(i0 + i, n_of - 1));
                 m[i] = make_float2(-INFINITY, -INFINITY);
                 l[i] = make_float2(0.f, 0.f);
 #pragma unroll
                 for (int k = 0; k < kMine; ++k) x[i][k] = 0.f;
-                if (f) {
+                if (i0 + i < n_of) {
                     m[i] = *reinterpret_cast<const float2*>(f + kMl + 2 * c);
                     l[i] = *reinterpret_cast<const float2*>(f + kMl + 8 + 2 * c);
 #pragma unroll
@@ -659,30 +659,54 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     };
     __syncthreads();
 
-    // ---- once per CTA: what several of its warps have of an item is merged
-#pragma unroll 1
-    for (int w = 0; w < kNarrowWarps; ++w) {
-        const Left left = tails[w];
-        if (left.blocks == 0) continue;
-        const int end = left.start + left.blocks, to = min(end, u1), w1 = runs.of(to - 1 - u0);
+    // ---- once per CTA: what several of its warps have of an item is merged by those whose runs end in it, each some of the fragment's
+    // registers, all items of the CTA at a time
+    if (tails[warp].blocks > 0) {
+        const Left left = tails[warp];
+        const int end = left.start + left.blocks, to = min(end, u1), w0 = runs.of(max(left.start, u0) - u0), w1 = runs.of(to - 1 - u0);
         const bool head = u0 + runs.first(w1 + 1) > to;  // the last of the warps has other items after it
-        sum_over(w1 - w + 1, [&](int i) -> const float* {
-            if (w + i == w1 && head) return heads + w1 * S::kFrag;
-            return tails[w + i].blocks == 0 ? nullptr : reinterpret_cast<const float*>(base_ptr + (w + i) * S::kRingBytes);
-        });
-        if (left.start >= u0 && end <= u1) {
-            write_sum(left.b, left.kvh);
-        } else {
-            float* f = part_of(blockIdx.x, left.start);
+        const int n_of = w1 - w0 + 1, helpers = n_of - head;
+        const float* f[kNarrowWarps];
+        float2 wt[kNarrowWarps];
+        M[0] = M[1] = -INFINITY;
+        L[0] = L[1] = 0.f;
 #pragma unroll
-            for (int k = 0; k < kMine; ++k) f[(warp + k * kNarrowWarps) * 32 + lane] = sum[k];
-            if (warp == 0) {
-                st.m[0] = M[0]; st.m[1] = M[1]; st.l[0] = L[0]; st.l[1] = L[1];
-                put_ml(f);
-                if (lane == 0) cuts[left.start > u0 ? 1 : 0] = left;
-            }
+        for (int i = 0; i < kNarrowWarps; ++i) {
+            const int w = w0 + min(i, n_of - 1);
+            f[i] = w == w1 && head ? heads + w * S::kFrag : reinterpret_cast<const float*>(base_ptr + w * S::kRingBytes);
+            wt[i] = i < n_of ? *reinterpret_cast<const float2*>(f[i] + kMl + 2 * c) : make_float2(-INFINITY, -INFINITY);
+            M[0] = fmaxf(M[0], wt[i].x);
+            M[1] = fmaxf(M[1], wt[i].y);
         }
-        w = head ? w1 - 1 : w1;
+        const float ref0 = M[0] == -INFINITY ? 0.f : M[0], ref1 = M[1] == -INFINITY ? 0.f : M[1];
+#pragma unroll
+        for (int i = 0; i < kNarrowWarps; ++i) {
+            // (beyond the last: weight 0 for the last one's values, which count already)
+            wt[i] = make_float2(ex2(wt[i].x - ref0), ex2(wt[i].y - ref1));
+            const float2 l = *reinterpret_cast<const float2*>(f[i] + kMl + 8 + 2 * c);
+            L[0] = fmaf(wt[i].x, l.x, L[0]);
+            L[1] = fmaf(wt[i].y, l.y, L[1]);
+        }
+        const bool whole = left.start >= u0 && end <= u1;
+        float* part = part_of(blockIdx.x, left.start);
+        const float inv0 = L[0] == 0.f ? 0.f : 1.f / L[0], inv1 = L[1] == 0.f ? 0.f : 1.f / L[1];  // no key seen: zeros
+        int t;
+        uint16_t* out0 = static_cast<uint16_t*>(a.out) + row_at(left.b, left.kvh, 2 * c, a.os, &t);
+        uint16_t* out1 = static_cast<uint16_t*>(a.out) + row_at(left.b, left.kvh, 2 * c + 1, a.os, &t);
+#pragma unroll 1
+        for (int r = warp - w0; r < KS * 4; r += helpers) {
+            const bool odd = r & 1;
+            float y = 0.f;
+#pragma unroll
+            for (int i = 0; i < kNarrowWarps; ++i) y = fmaf(odd ? wt[i].y : wt[i].x, f[i][r * 32 + lane], y);
+            if (!whole) part[r * 32 + lane] = y;
+            else if (2 * c + odd < a.rows && dim_of(r) < a.D && !failed) (odd ? out1 : out0)[dim_of(r)] = narrow(y * (odd ? inv1 : inv0));
+        }
+        if (!whole && warp == w0) {
+            st.m[0] = M[0]; st.m[1] = M[1]; st.l[0] = L[0]; st.l[1] = L[1];
+            put_ml(part);
+            if (lane == 0) cuts[left.start > u0 ? 1 : 0] = left;
+        }
     }
     __syncthreads();
 
