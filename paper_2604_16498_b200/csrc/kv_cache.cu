@@ -140,7 +140,7 @@ __device__ __forceinline__ uint2 encode8(const float (&y)[8], float mul) {
 // A lane's pieces are chosen so that pairs meet in it: half layout, pieces 8 i and half + 8 i (then the unrotated rest two by two); interleaved,
 // pieces 16 i and 16 i + 8.  GENERIC: half layout whose halves are not whole pieces: pairs meet in shared memory.
 template <typename T, int LPR, int FMT, bool GENERIC>
-__global__ void __launch_bounds__(kRotWarps * 32) rotate_append_kernel(const RotArgs a) {
+__global__ void __launch_bounds__(kRotWarps * 32, FMT == kNoCache ? 1 : 5) rotate_append_kernel(const RotArgs a) {
     constexpr int RPW = 32 / LPR;                            // rows at a time
     constexpr int U = sizeof(T) == 4 || GENERIC ? 1 : 2;     // of those, loads in flight
     constexpr int kAngles = GENERIC ? 16 : 8;
