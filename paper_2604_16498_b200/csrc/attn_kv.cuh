@@ -105,6 +105,10 @@ __device__ __forceinline__ int kv_sum(int v) {
     return v;
 }
 
+__device__ __forceinline__ int kv_max(int v) {  // over all lanes
+    return __reduce_max_sync(0xffffffffu, v);
+}
+
 // Whole numbers 0 .. n - 1 shared evenly by `by` (at most n) of them, in order: the first n % by get one more than the others.
 struct KvShares {
     int by, each, more;
@@ -116,20 +120,44 @@ struct KvShares {
     }
 };
 
-// The call's tiles of up to 8 rows, which W CTAs share (at least `least` each), and the sequence in which tile u lies.  Lane l keeps what there
+// The call's tiles of up to 8 rows, which W CTAs share (at least `least` each; or one item each, if the longest then has at most `merge` tiles
+// more than an even share, which is what joining parts of several CTAs takes), and the sequence in which tile u lies.  Lane l keeps what there
 // is to know of sequence l, so that up to 32 sequences are read once.
 template <int KEYS>
 struct KvSchedule {
     int N, W;
+    bool whole;                    // CTA i has item i, all of it
     int past0, tiles0, incl0;
-    __device__ __forceinline__ KvSchedule(const KvAttnArgs& a, int least, int lane) {
+    __device__ __forceinline__ KvSchedule(const KvAttnArgs& a, int least, int merge, int lane) {
         past0 = lane < a.B ? kv_past(a, lane) : 0;
         tiles0 = lane < a.B ? kv_tiles<KEYS>(a, past0) : 0;
         incl0 = kv_scan(tiles0, lane);
-        int total = tiles0;
-        for (int b = 32 + lane; b < a.B; b += 32) total += kv_tiles<KEYS>(a, kv_past(a, b));
+        int total = tiles0, most = tiles0;
+        for (int b = 32 + lane; b < a.B; b += 32) {
+            const int tiles = kv_tiles<KEYS>(a, kv_past(a, b));
+            total += tiles;
+            most = max(most, tiles);
+        }
         N = kv_sum(total) * a.Hkv;
         W = min((int)gridDim.x, (N + least - 1) / least);
+        const int items = a.B * a.Hkv;
+        whole = items <= (int)gridDim.x && kv_max(most) <= N / W + merge;
+        if (whole) W = items;
+    }
+    // The first tile of item i, and (whole) where the CTA's share ends.
+    __device__ __forceinline__ int item_at(const KvAttnArgs& a, int i, int lane, int* end) const {
+        const int b = i / a.Hkv, kvh = i - b * a.Hkv;
+        int before = 0, tiles = tiles0, incl = incl0;
+#pragma unroll 1
+        for (int b0 = 32; b0 <= b; b0 += 32) {
+            before += __shfl_sync(0xffffffffu, incl, 31);
+            tiles = b0 + lane < a.B ? kv_tiles<KEYS>(a, kv_past(a, b0 + lane)) : 0;
+            incl = kv_scan(tiles, lane);
+        }
+        const int n = __shfl_sync(0xffffffffu, tiles, b & 31);
+        const int first = (before + __shfl_sync(0xffffffffu, incl, b & 31) - n) * a.Hkv + kvh * n;
+        *end = first + n;
+        return first;
     }
     __device__ __forceinline__ int past_of(const KvAttnArgs& a, int b) const {  // the same b in all lanes
         return b < 32 ? __shfl_sync(0xffffffffu, past0, b) : kv_past(a, b);

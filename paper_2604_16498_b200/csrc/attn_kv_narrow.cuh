@@ -17,6 +17,9 @@ namespace {
 constexpr int kNarrowRows = 8;
 constexpr int kNarrowWarps = 8;
 constexpr int kNarrowThreads = kNarrowWarps * 32;
+// Blocks that joining the parts of several CTAs is worth.  int8 rows of 128, 32/8 heads: 16 x 1000 rows take 15.8 us in even shares and 11.8
+// as whole items (5 blocks more than the share), 8 x 1000 rows 12.7 and 11.7 (19 more), 2 x 1000 rows 8.4 and 11.5 (25 more).
+constexpr int kNarrowMerge = 20;
 // The scales of a block of 32 keys, copied from the 16-byte boundary at or before the first: up to 3 others come first.
 constexpr int kScaleKeys = 36, kScaleBox = 256;
 
@@ -153,10 +156,11 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     pdl_launch_dependents();
     pdl_wait();
 
-    const KvSchedule<KEYS> sched(a, a.least, lane);
+    const KvSchedule<KEYS> sched(a, a.least, kNarrowMerge, lane);
     if ((int)blockIdx.x >= sched.W) return;
     const KvShares shares(sched.N, sched.W);
-    const int u0 = shares.first(blockIdx.x), u1 = shares.first(blockIdx.x + 1);
+    int u0 = shares.first(blockIdx.x), u1 = shares.first(blockIdx.x + 1);
+    if (sched.whole) u0 = sched.item_at(a, blockIdx.x, lane, &u1);
     const KvShares runs(u1 - u0, kNarrowWarps);
     NarrowWalk cur;
     cur.u = u0 + runs.first(warp);
@@ -255,10 +259,30 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         return a.parts + (size_t)(cta * 2 + (item_start > shares.first(cta) ? 1 : 0)) * S::kFrag;
     };
     const bool out_f16 = kEight ? a.q_f16 : kF16;
-    auto dim_of = [&](int r) {  // of register r (its rows: 2c + (r & 1))
-        return kEight ? g * (DW / 8) + 2 * (r >> 2) + ((r >> 1) & 1) : 16 * (r >> 2) + 8 * ((r >> 1) & 1) + g;
+    auto pack = [&](float y, float z) { return out_f16 ? pack16<true>(y, z) : pack16<false>(y, z); };
+    // Registers 4 s .. 4 s + 3 of O^T (rows 2c, 2c + 1 of one dim, then of another), normalised, to the output.
+    auto write4 = [&](uint16_t* out0, uint16_t* out1, int s, const float (&y)[4], float inv0, float inv1) {
+        const uint32_t y0 = pack(y[0] * inv0, y[2] * inv0), y1 = pack(y[1] * inv1, y[3] * inv1);
+        const bool has0 = 2 * c < a.rows && !failed, has1 = 2 * c + 1 < a.rows && !failed;
+        if constexpr (kEight) {  // dims side by side
+            const int d = g * (DW / 8) + 2 * s;
+            if (has0 && d < a.D) *reinterpret_cast<uint32_t*>(out0 + d) = y0;
+            if (has1 && d < a.D) *reinterpret_cast<uint32_t*>(out1 + d) = y1;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int d = 16 * s + 8 * i + g;
+                if (has0 && d < a.D) out0[d] = (uint16_t)(y0 >> (16 * i));
+                if (has1 && d < a.D) out1[d] = (uint16_t)(y1 >> (16 * i));
+            }
+        }
     };
-    auto narrow = [&](float y) { return (uint16_t)((out_f16 ? pack16<true>(y, 0.f) : pack16<false>(y, 0.f)) & 0xffffu); };
+    auto rows_of_item = [&](int b, int kvh, uint16_t** out0, uint16_t** out1) {
+        int t;
+        *out0 = static_cast<uint16_t*>(a.out) + row_at(b, kvh, 2 * c, a.os, &t);
+        *out1 = static_cast<uint16_t*>(a.out) + row_at(b, kvh, 2 * c + 1, a.os, &t);
+    };
+    auto inverse = [](float l) { return l == 0.f ? 0.f : 1.f / l; };  // no key seen: zeros
     while (cur.u < cur.end) {
         struct { int b, kvh, past, rows; } p = {cur.b, cur.kvh, cur.past, kv_rows(a, cur.past)};
         const int item_start = cur.u - cur.tile, item_end = item_start + cur.tiles;
@@ -576,18 +600,11 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         }
         const Left left = {item_start, cur.tiles, p.b, p.kvh};
         if (blocks == cur.tiles) {  // all of it
+            uint16_t *out0, *out1;
+            rows_of_item(p.b, p.kvh, &out0, &out1);
+            const float inv0 = inverse(st.l[0]), inv1 = inverse(st.l[1]);
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                if (2 * c + r >= a.rows || failed) continue;
-                const float inv = st.l[r] == 0.f ? 0.f : 1.f / st.l[r];  // no key seen: zeros
-                int t;
-                uint16_t* out = static_cast<uint16_t*>(a.out) + row_at(p.b, p.kvh, 2 * c + r, a.os, &t);
-#pragma unroll
-                for (int s = 0; s < KS; ++s)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-                        if (dim_of(4 * s + 2 * i) < a.D) out[dim_of(4 * s + 2 * i)] = narrow(st.o[s][2 * i + r] * inv);
-            }
+            for (int s = 0; s < KS; ++s) write4(out0, out1, s, st.o[s], inv0, inv1);
         } else if (item_end < cur.end) {  // its end: warp 0 has all that the CTA has of it, the others' joins what the warps before have
             put(warp == 0 ? part_of(blockIdx.x, item_start) : heads + warp * S::kFrag);
             if (lane == 0 && warp == 0) cuts[0] = left;
@@ -598,7 +615,7 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         cur.step<KEYS>(a, sched, blocks);
     }
 
-    // Registers warp, warp + 8, ... of a fragment of O^T in this lane, summed over several fragments; a few at a time, whose loads leave
+    // kMine registers of a fragment of O^T from kMine warp on in this lane, summed over several fragments; a few at a time, whose loads leave
     // together.  of(i): the i-th.
     constexpr int kMine = KS * 4 / kNarrowWarps;
     float sum[kMine], M[2], L[2];
@@ -623,7 +640,7 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                     m[i] = *reinterpret_cast<const float2*>(f + kMl + 2 * c);
                     l[i] = *reinterpret_cast<const float2*>(f + kMl + 8 + 2 * c);
 #pragma unroll
-                    for (int k = 0; k < kMine; ++k) x[i][k] = f[(warp + k * kNarrowWarps) * 32 + lane];
+                    for (int k = 0; k < kMine; ++k) x[i][k] = f[(warp * kMine + k) * 32 + lane];
                 }
             }
             float old[2] = {M[0], M[1]};
@@ -634,27 +651,29 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
             L[0] *= a0;
             L[1] *= a1;
 #pragma unroll
-            for (int k = 0; k < kMine; ++k) sum[k] *= warp & 1 ? a1 : a0;  // (8 is even: this warp's registers are all of one row)
+            for (int k = 0; k < kMine; ++k) sum[k] *= k & 1 ? a1 : a0;
 #pragma unroll
             for (int i = 0; i < kAtOnce; ++i) {
                 const float w0 = ex2(m[i].x - ref0), w1 = ex2(m[i].y - ref1);
                 L[0] = fmaf(w0, l[i].x, L[0]);
                 L[1] = fmaf(w1, l[i].y, L[1]);
 #pragma unroll
-                for (int k = 0; k < kMine; ++k) sum[k] = fmaf(warp & 1 ? w1 : w0, x[i][k], sum[k]);
+                for (int k = 0; k < kMine; ++k) sum[k] = fmaf(k & 1 ? w1 : w0, x[i][k], sum[k]);
             }
         }
     };
     auto write_sum = [&](int b, int kvh) {  // normalised, to the output
-        const int row = 2 * c + (warp & 1);
-        if (row >= a.rows || failed) return;
-        const float l = warp & 1 ? L[1] : L[0], inv = l == 0.f ? 0.f : 1.f / l;
-        int t;
-        uint16_t* out = static_cast<uint16_t*>(a.out) + row_at(b, kvh, row, a.os, &t);
-#pragma unroll
-        for (int k = 0; k < kMine; ++k) {
-            const int r = warp + k * kNarrowWarps;
-            if (dim_of(r) < a.D) out[dim_of(r)] = narrow(sum[k] * inv);
+        uint16_t *out0, *out1;
+        rows_of_item(b, kvh, &out0, &out1);
+        const float inv0 = inverse(L[0]), inv1 = inverse(L[1]);
+        if constexpr (kMine == 4) {
+            write4(out0, out1, warp, sum, inv0, inv1);
+        } else {  // one dim of both rows
+            static_assert(kMine == 2);
+            const int s = warp >> 1, i = warp & 1, d = kEight ? g * (DW / 8) + 2 * s + i : 16 * s + 8 * i + g;
+            if (d >= a.D || failed) return;
+            if (2 * c < a.rows) out0[d] = (uint16_t)pack(sum[0] * inv0, 0.f);
+            if (2 * c + 1 < a.rows) out1[d] = (uint16_t)pack(sum[1] * inv1, 0.f);
         }
     };
     __syncthreads();
@@ -666,41 +685,59 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         const int end = left.start + left.blocks, to = min(end, u1), w0 = runs.of(max(left.start, u0) - u0), w1 = runs.of(to - 1 - u0);
         const bool head = u0 + runs.first(w1 + 1) > to;  // the last of the warps has other items after it
         const int n_of = w1 - w0 + 1, helpers = n_of - head;
-        const float* f[kNarrowWarps];
-        float2 wt[kNarrowWarps];
-        M[0] = M[1] = -INFINITY;
-        L[0] = L[1] = 0.f;
-#pragma unroll
-        for (int i = 0; i < kNarrowWarps; ++i) {
-            const int w = w0 + min(i, n_of - 1);
-            f[i] = w == w1 && head ? heads + w * S::kFrag : reinterpret_cast<const float*>(base_ptr + w * S::kRingBytes);
-            wt[i] = i < n_of ? *reinterpret_cast<const float2*>(f[i] + kMl + 2 * c) : make_float2(-INFINITY, -INFINITY);
-            M[0] = fmaxf(M[0], wt[i].x);
-            M[1] = fmaxf(M[1], wt[i].y);
+        constexpr int kNext = S::kRingBytes / 4;  // floats from a warp's ring to the next one's
+        const float* const first = reinterpret_cast<const float*>(base_ptr + w0 * S::kRingBytes);
+        const float* const last = head ? heads + w1 * S::kFrag : first + (n_of - 1) * kNext;
+        // lane (g, c): the weights of rows 2c, 2c + 1 of warp w0 + g; from there to all lanes with this c
+        const float* const ml = (g < n_of - 1 ? first + g * kNext : last) + kMl + 2 * c;
+        float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);
+        if (g < n_of) {
+            m = *reinterpret_cast<const float2*>(ml);
+            l = *reinterpret_cast<const float2*>(ml + 8);
         }
-        const float ref0 = M[0] == -INFINITY ? 0.f : M[0], ref1 = M[1] == -INFINITY ? 0.f : M[1];
+        M[0] = m.x;
+        M[1] = m.y;
 #pragma unroll
-        for (int i = 0; i < kNarrowWarps; ++i) {
-            // (beyond the last: weight 0 for the last one's values, which count already)
-            wt[i] = make_float2(ex2(wt[i].x - ref0), ex2(wt[i].y - ref1));
-            const float2 l = *reinterpret_cast<const float2*>(f[i] + kMl + 8 + 2 * c);
-            L[0] = fmaf(wt[i].x, l.x, L[0]);
-            L[1] = fmaf(wt[i].y, l.y, L[1]);
+        for (int o = 4; o < 32; o <<= 1)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) M[r] = fmaxf(M[r], __shfl_xor_sync(0xffffffffu, M[r], o));
+        const float w0_ = ex2(m.x - (M[0] == -INFINITY ? 0.f : M[0])), w1_ = ex2(m.y - (M[1] == -INFINITY ? 0.f : M[1]));
+        L[0] = w0_ * l.x;
+        L[1] = w1_ * l.y;
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1)
+#pragma unroll
+            for (int r = 0; r < 2; ++r) L[r] += __shfl_xor_sync(0xffffffffu, L[r], o);
+        float wt[kNarrowWarps][2];
+#pragma unroll
+        for (int i = 0; i < kNarrowWarps; ++i) {  // the last one's come last
+            const int from = (i < kNarrowWarps - 1 ? i : n_of - 1) * 4 + c;
+            wt[i][0] = __shfl_sync(0xffffffffu, w0_, from);
+            wt[i][1] = __shfl_sync(0xffffffffu, w1_, from);
         }
         const bool whole = left.start >= u0 && end <= u1;
         float* part = part_of(blockIdx.x, left.start);
-        const float inv0 = L[0] == 0.f ? 0.f : 1.f / L[0], inv1 = L[1] == 0.f ? 0.f : 1.f / L[1];  // no key seen: zeros
-        int t;
-        uint16_t* out0 = static_cast<uint16_t*>(a.out) + row_at(left.b, left.kvh, 2 * c, a.os, &t);
-        uint16_t* out1 = static_cast<uint16_t*>(a.out) + row_at(left.b, left.kvh, 2 * c + 1, a.os, &t);
+        const float inv0 = inverse(L[0]), inv1 = inverse(L[1]);
+        uint16_t *out0, *out1;
+        rows_of_item(left.b, left.kvh, &out0, &out1);
 #pragma unroll 1
-        for (int r = warp - w0; r < KS * 4; r += helpers) {
-            const bool odd = r & 1;
-            float y = 0.f;
+        for (int s = warp - w0; s < KS; s += helpers) {
+            const int at = s * 128 + lane;
+            float y[4];
 #pragma unroll
-            for (int i = 0; i < kNarrowWarps; ++i) y = fmaf(odd ? wt[i].y : wt[i].x, f[i][r * 32 + lane], y);
-            if (!whole) part[r * 32 + lane] = y;
-            else if (2 * c + odd < a.rows && dim_of(r) < a.D && !failed) (odd ? out1 : out0)[dim_of(r)] = narrow(y * (odd ? inv1 : inv0));
+            for (int k = 0; k < 4; ++k) y[k] = wt[kNarrowWarps - 1][k & 1] * last[at + 32 * k];
+#pragma unroll
+            for (int i = 0; i < kNarrowWarps - 1; ++i)
+                if (i < n_of - 1) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) y[k] = fmaf(wt[i][k & 1], first[i * kNext + at + 32 * k], y[k]);
+                }
+            if (whole) {
+                write4(out0, out1, s, y, inv0, inv1);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) part[at + 32 * k] = y[k];
+            }
         }
         if (!whole && warp == w0) {
             st.m[0] = M[0]; st.m[1] = M[1]; st.l[0] = L[0]; st.l[1] = L[1];

@@ -19,6 +19,10 @@
 namespace forge {
 namespace {
 
+// Steps that joining the pieces of an item is worth.  8 x 32/8 heads x 16 tokens over int8 rows: 400 rows of the past take 16.3 us cut and 15.7
+// whole (4 steps more), 600 take 17.6 and 19.0 (7 more); 1 x 32/8 x 5 tokens over 16-bit rows: 600 take 11.7 and 11.3 (4 more), 800 take
+// 13.7 and 14.8 (6 more).
+constexpr int kRowsMerge = 4;
 constexpr float kRowsTop = 14.f, kRowsLift = 6.f;  // p reaches 2^14, 2^8 above what the reference stands for
 
 template <int DW, int FMT>
@@ -58,15 +62,21 @@ struct RowsPieces {
     int C, cut, all;               // steps of a piece; pieces of items with several, and of all
     int past0, tiles0;             // of sequence `lane`
     static __device__ __forceinline__ int pieces(int tiles, int C) { return (tiles + C - 1) / C; }
-    // The smallest C that gives each CTA its share of the steps; up to twice that if then no CTA has two pieces.
+    // The smallest C that gives each CTA its share of the steps; up to twice that if then no CTA has two pieces, and a few steps more if then
+    // nothing is cut.
     __device__ __forceinline__ RowsPieces(const KvAttnArgs& a, int ctas, int lane) {
         const int per = a.Hkv * a.row_tiles;
         past0 = lane < a.B ? kv_past(a, lane) : 0;
         tiles0 = lane < a.B ? kv_tiles<STEP>(a, past0) : 0;
-        int total = tiles0;
-        for (int b = 32 + lane; b < a.B; b += 32) total += kv_tiles<STEP>(a, kv_past(a, b));
+        int total = tiles0, most = tiles0;
+        for (int b = 32 + lane; b < a.B; b += 32) {
+            const int tiles = kv_tiles<STEP>(a, kv_past(a, b));
+            total += tiles;
+            most = max(most, tiles);
+        }
+        most = kv_max(most);
         const int N = kv_sum(total) * per, low = max((N + ctas - 1) / ctas, a.least);
-        C = low;
+        C = a.B * per <= ctas && most <= low + kRowsMerge ? most : low;
         count(a, lane);
         for (int c = low; all > ctas && c < 2 * low;) {
             c += max(c >> 4, 1);
