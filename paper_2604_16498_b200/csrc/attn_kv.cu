@@ -57,7 +57,6 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     a.tile_heads = rs.heads;
     a.tile_rows = rs.heads * T;
     a.tile_stride = (a.tile_rows + 31) / 32 * 32;
-    a.least = rs.tiles == 1 && G * T <= kNarrowRows ? kNarrowWarps : 1;
     a.q_f16 = dtype == FORGE_DTYPE_F16;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.counters = static_cast<unsigned int*>(workspace);

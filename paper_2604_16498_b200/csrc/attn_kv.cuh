@@ -37,7 +37,6 @@ struct KvAttnArgs {
     int B, Hkv, G, Smax, D;
     int rows, row_tiles, tile_rows;  // G * T; groups of rows (of tile_heads whole heads), and how many a group has
     int tile_heads, tile_stride;     // rows between the columns of a part in the workspace
-    int least;                       // blocks of keys that a CTA has at least
     bool q_f16;
     float scale_log2;
     unsigned int* counters;
@@ -99,15 +98,8 @@ __device__ __forceinline__ int kv_scan(int v, int lane) {  // inclusive sum over
     }
     return v;
 }
-__device__ __forceinline__ int kv_sum(int v) {
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    return v;
-}
-
-__device__ __forceinline__ int kv_max(int v) {  // over all lanes
-    return __reduce_max_sync(0xffffffffu, v);
-}
+__device__ __forceinline__ int kv_sum(int v) { return __reduce_add_sync(0xffffffffu, v); }  // over all lanes
+__device__ __forceinline__ int kv_max(int v) { return __reduce_max_sync(0xffffffffu, v); }
 
 // Whole numbers 0 .. n - 1 shared evenly by `by` (at most n) of them, in order: the first n % by get one more than the others.
 struct KvShares {
@@ -120,15 +112,15 @@ struct KvShares {
     }
 };
 
-// The call's tiles of up to 8 rows, which W CTAs share (at least `least` each; or one item each, if the longest then has at most `merge` tiles
+// The call's tiles of up to 8 rows, which W CTAs share (at least LEAST each; or one item each, if the longest then has at most MERGE tiles
 // more than an even share, which is what joining parts of several CTAs takes), and the sequence in which tile u lies.  Lane l keeps what there
 // is to know of sequence l, so that up to 32 sequences are read once.
-template <int KEYS>
+template <int KEYS, int LEAST, int MERGE>
 struct KvSchedule {
     int N, W;
     bool whole;                    // CTA i has item i, all of it
     int past0, tiles0, incl0;
-    __device__ __forceinline__ KvSchedule(const KvAttnArgs& a, int least, int merge, int lane) {
+    __device__ __forceinline__ KvSchedule(const KvAttnArgs& a, int lane) {
         past0 = lane < a.B ? kv_past(a, lane) : 0;
         tiles0 = lane < a.B ? kv_tiles<KEYS>(a, past0) : 0;
         incl0 = kv_scan(tiles0, lane);
@@ -139,9 +131,9 @@ struct KvSchedule {
             most = max(most, tiles);
         }
         N = kv_sum(total) * a.Hkv;
-        W = min((int)gridDim.x, (N + least - 1) / least);
+        W = min((int)gridDim.x, (N + LEAST - 1) / LEAST);
         const int items = a.B * a.Hkv;
-        whole = items <= (int)gridDim.x && kv_max(most) <= N / W + merge;
+        whole = items <= (int)gridDim.x && kv_max(most) <= N / W + MERGE;
         if (whole) W = items;
     }
     // The first tile of item i, and (whole) where the CTA's share ends.

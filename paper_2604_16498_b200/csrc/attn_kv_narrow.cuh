@@ -91,12 +91,14 @@ struct NarrowState {
     }
 };
 
+template <int KEYS>
+using NarrowSchedule = KvSchedule<KEYS, kNarrowWarps, kNarrowMerge>;
 // A warp's run of blocks.
 struct NarrowWalk {
     int u, end;                          // blocks of the call
     int b, kvh, tile, tiles, past;       // the next one is block `tile` of `tiles` of (b, kvh)
     template <int KEYS>
-    __device__ __forceinline__ void step(const KvAttnArgs& a, const KvSchedule<KEYS>& sched, int n) {
+    __device__ __forceinline__ void step(const KvAttnArgs& a, const NarrowSchedule<KEYS>& sched, int n) {
         u += n;
         tile += n;
         if (tile == tiles && u < end) {
@@ -156,7 +158,7 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     pdl_launch_dependents();
     pdl_wait();
 
-    const KvSchedule<KEYS> sched(a, a.least, kNarrowMerge, lane);
+    const NarrowSchedule<KEYS> sched(a, lane);
     if ((int)blockIdx.x >= sched.W) return;
     const KvShares shares(sched.N, sched.W);
     int u0 = shares.first(blockIdx.x), u1 = shares.first(blockIdx.x + 1);

@@ -75,7 +75,7 @@ struct RowsPieces {
             most = max(most, tiles);
         }
         most = kv_max(most);
-        const int N = kv_sum(total) * per, low = max((N + ctas - 1) / ctas, a.least);
+        const int N = kv_sum(total) * per, low = (N + ctas - 1) / ctas;
         C = a.B * per <= ctas && most <= low + kRowsMerge ? most : low;
         count(a, lane);
         for (int c = low; all > ctas && c < 2 * low;) {
