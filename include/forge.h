@@ -353,6 +353,7 @@ int forge_rotary_apply(const void* x, void* y, int dtype, int B, int H, int S, i
  *   k, v [B, Hkv, S, D], q, q_out [B, Hq, S, D]: views, all of `dtype`: FORGE_DTYPE_BF16 or FORGE_DTYPE_F16; a 16-bit cache
  *   has the same type.  q needs `rotary`.
  *   positions: int32 [B, S_src], the positions of the tokens of k (and q); NULL: that of a row is its place lens[b] + i.
+ *   None of them may overlap the cache.
  *   rows: int32 [B, S] or NULL: row lens[b] + i is taken from token rows[b S + i] of k and v, which have S_src tokens then
  *   (without rows S_src is not read and counts as S).  A value outside 0 .. S_src - 1 leaves its row as it is.  This is what follows a tree of drafted
  *   tokens: the accepted path is appended once more, to its final rows.  Not together with q.

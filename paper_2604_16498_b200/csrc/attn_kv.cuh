@@ -131,9 +131,12 @@ struct KvSchedule {
             most = max(most, tiles);
         }
         N = kv_sum(total) * a.Hkv;
-        W = min((int)gridDim.x, (N + LEAST - 1) / LEAST);
+        most = kv_max(most);
+        // Adding one part to a merge takes as long as a tile: n + most / n is smallest at sqrt(most).
+        const int least = max(LEAST, (int)__fsqrt_rn((float)most));
+        W = min((int)gridDim.x, (N + least - 1) / least);
         const int items = a.B * a.Hkv;
-        whole = items <= (int)gridDim.x && kv_max(most) <= N / W + MERGE;
+        whole = items <= (int)gridDim.x && most <= N / W + MERGE;
         if (whole) W = items;
     }
     // The first tile of item i, and (whole) where the CTA's share ends.

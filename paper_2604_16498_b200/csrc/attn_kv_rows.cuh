@@ -14,6 +14,10 @@
 //   warps 10-13 8-bit rows only: codes of K and V to fp16, from the copies' ring into operands
 // 8-bit rows stay codes in the products (exact in fp16; int8 elements come in the order 0 2 1 3 of each four, in Q and O too); their scales
 // multiply the scores and the probabilities.  Q comes by TMA, an item ahead: plain loads would wait behind the copies in flight.
+//
+// What bounds it: the chain of a step (scores, softmax of a row per thread, P into tensor memory, product with V; 2350 cycles for 128 keys where the
+// tensor cores need 1024), and some 8 us around the steps: start, first copies, the output and the merge of pieces.  4 x 32/8 heads x 64 tokens behind
+// 1024 .. 4096 16-bit rows take 29.1 us, 8 x 28/4 x 16 behind 600 .. 2400 int8 rows 23.4, 1 x 32/8 x 5 behind some 600 13.5.
 #pragma once
 
 namespace forge {
@@ -62,7 +66,7 @@ struct RowsPieces {
     int C, cut, all;               // steps of a piece; pieces of items with several, and of all
     int past0, tiles0;             // of sequence `lane`
     static __device__ __forceinline__ int pieces(int tiles, int C) { return (tiles + C - 1) / C; }
-    // The smallest C that gives each CTA its share of the steps; up to twice that if then no CTA has two pieces, and a few steps more if then
+    // The smallest C that gives each CTA its share of the steps and no item too many pieces; up to twice that if then no CTA has two pieces, and a few steps more if then
     // nothing is cut.
     __device__ __forceinline__ RowsPieces(const KvAttnArgs& a, int ctas, int lane) {
         const int per = a.Hkv * a.row_tiles;
@@ -75,7 +79,8 @@ struct RowsPieces {
             most = max(most, tiles);
         }
         most = kv_max(most);
-        const int N = kv_sum(total) * per, low = (N + ctas - 1) / ctas;
+        // Adding one part to a merge takes as long as half a step: C + most / C / 2 is smallest at sqrt(most / 2).
+        const int N = kv_sum(total) * per, low = max((N + ctas - 1) / ctas, (int)ceilf(__fsqrt_rn(0.5f * most)));
         C = a.B * per <= ctas && most <= low + kRowsMerge ? most : low;
         count(a, lane);
         for (int c = low; all > ctas && c < 2 * low;) {
