@@ -19,6 +19,8 @@
 namespace forge {
 namespace {
 
+// What the instructions have room for.  With few rows this kernel is the faster one: 16 sequences of 32/8 heads of 128, 8 rows (4 heads x 2 tokens), 4000
+// cached rows: int8 29.3 us, on the other kernel 77.8; bf16 47.3 and 48.3, 1000 rows 11.2 and 16.2.
 constexpr int kNarrowRows = 8;
 constexpr int kNarrowWarps = 8;
 constexpr int kNarrowThreads = kNarrowWarps * 32;

@@ -296,6 +296,8 @@ int launch_rotate(RotArgs& a, cudaStream_t s) {
     const int iters = (H + 32 / LPR - 1) / (32 / LPR);
     const long long tokens = (long long)a.B * a.S;
     // A token's heads are shared out while that leaves SMs short of warps (16 of them each): the cosines are made once per share.
+    // 16 tokens of 40 heads: 3.8 us in one share, 2.1 in ten; append of 16 tokens of 32/8 heads 7.3 and 2.7.  4 x 2048 tokens: 41.6 in one, 44.0 in
+    // two, 49.2 in three.
     const long long want = (16LL * sms + tokens - 1) / tokens;
     a.parts = (int)(want < 1 ? 1 : want > iters ? iters : want);
     const long long ctas = (tokens * a.parts + kRotWarps - 1) / kRotWarps;
