@@ -8,7 +8,9 @@
  *     variant;
  *   - fused Linear + bias + GELU: matmul, element-wise bias add and activation in
  *     one dispatch, the linear output never materialised (Section 4.3 "Pass 5:
- *     Operator Fusion", Listing 6 and Eq. 11).
+ *     Operator Fusion", Listing 6 and Eq. 11);
+ *   - what stands around the decode step when a model is served: rotary positions, KV caches
+ *     of 16-bit or 8-bit rows, attention of single tokens and of drafted trees over them.
  *
  * Conventions shared by every entry point
  *   - Unless a parameter says HOST, pointers are DEVICE pointers owned by the
@@ -382,6 +384,7 @@ int forge_kv_read(const forge_kv_cache* cache, void* k_out, void* v_out, int dty
  *     out[b,h,:] = sum_j softmax_j(scale * q[b,h,:].k[b,h/G,j,:]) v[b,h/G,j,:]   over rows j < lens[b]
  * q, out: [B, Hq, D] of `dtype` FORGE_DTYPE_BF16 or _F16 (that of a 16-bit cache); lens clamped to 0 .. Smax; a sequence
  * without rows gives zeros; rows at and beyond lens[b] may hold anything.  Any finite scale.  Hq / Hkv: any whole number.
+ * out may not overlap q or the cache.
  *
  * forge_attn_tree: T tokens per sequence (1 .. 64) whose own rows are in the cache behind the lens[b] rows of their common
  * past, at lens[b] .. lens[b] + T - 1 (as forge_kv_append leaves them, with the same lens).  Token t sees all rows before

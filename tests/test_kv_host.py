@@ -227,3 +227,14 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
                  lambda: binding.attn_tree(x.float(), c, lens), lambda: binding.attn_kv_workspace_init(lens)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_tensors_of_another_device_are_refused(monkeypatch):
+    """The library launches on the current device, whatever device the tensors are on."""
+    class On:
+        def __init__(self, index):
+            self.device = torch.device("cuda", index)
+    monkeypatch.setattr(binding, "_current_device", lambda: 1)
+    binding._on_current(On(1), None, On(1))
+    with pytest.raises(ValueError, match="cuda:0"):
+        binding._on_current(On(1), None, On(0))

@@ -295,3 +295,20 @@ def test_two_streams_with_a_workspace_each():
     binding.check_status()
     for o, w in zip(outs, want):
         assert torch.equal(o, w)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=IDS)
+@pytest.mark.parametrize("B,Hq,Hkv,D", [(5, 12, 4, 128), (40, 6, 3, 64), (37, 12, 1, 128), (49, 3, 3, 80)])
+def test_sequences_of_nearly_the_same_length(dtype, form, B, Hq, Hkv, D):
+    """No more (sequence, KV head) pairs than CTAs, and of lengths that are not worth sharing, with some without rows."""
+    lens = [0 if b % 13 == 5 else 260 - (7 * b) % 60 for b in range(B)]
+    check_decode(31, dtype, form, Hq, Hkv, D, lens, 270)
+    check_tree(32, dtype, form, Hq, Hkv, D, 5, lens, 270)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=IDS)
+@pytest.mark.parametrize("Hq,D,T", [(8, 128, 1), (4, 64, 2), (24, 64, 1), (16, 128, 3)])
+def test_one_kv_head_over_a_long_cache(dtype, form, Hq, D, T):
+    """One item shared by many CTAs: as many parts as a merge is worth, of any length."""
+    for lens in ([19999 - T], [4097], [1, 12000]):
+        check_tree(33, dtype, form, Hq, 1, D, T, lens, 20000)
