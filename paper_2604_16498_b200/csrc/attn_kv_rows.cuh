@@ -17,7 +17,7 @@
 //
 // What bounds it: the chain of a step (scores, softmax of a row per thread, P into tensor memory, product with V; 2350 cycles for 128 keys where the
 // tensor cores need 1024), and some 8 us around the steps: start, first copies, the output and the merge of pieces.  4 x 32/8 heads x 64 tokens behind
-// 1024 .. 4096 16-bit rows take 29.1 us, 8 x 28/4 x 16 behind 600 .. 2400 int8 rows 23.4, 1 x 32/8 x 5 behind some 600 13.5.
+// 1024 .. 4096 16-bit rows take 28.6 us, 8 x 28/4 x 16 behind 600 .. 2400 int8 rows 23.6, 1 x 32/8 x 5 behind some 600 12.4.
 #pragma once
 
 namespace forge {
@@ -80,7 +80,8 @@ struct RowsPieces {
         }
         most = kv_max(most);
         // Adding one part to a merge takes as long as half a step: C + most / C / 2 is smallest at sqrt(most / 2).  16/1 heads of 128 over int8 rows of
-        // one sequence, with as many pieces as CTAs and with this: 1000 rows 17.8 and 14.8 us, 4000 42.1 and 20.3, 32,000 77.4 and 42.7.
+        // one sequence, with as many pieces as CTAs and with this: 1000 rows 17.8 and 14.8 us, 4000 42.1 and 20.3, 32,000 77.4 and 42.7 (13.8 and 18.6 for the
+        // first two since a part takes a third less).
         const int N = kv_sum(total) * per, low = max((N + ctas - 1) / ctas, (int)__fsqrt_rn(0.5f * most));
         C = a.B * per <= ctas && most <= low + kRowsMerge ? most : low;
         count(a, lane);
@@ -718,38 +719,32 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             const int bytes = a.tile_stride * (DW + 2) * 4, slots = min(S::kRing / bytes, kMergeSlots);
             const int at = cut.rt * a.tile_rows + row;
             const bool live = row < a.tile_rows && at < a.rows;
-            auto copy = [&](int i) {  // thread 0
-                uint64_t* full = &merge_full[i % slots];
-                mbar_expect_tx(full, bytes);
-                bulk_load(smem_u32(smem + S::kKOff + i % slots * bytes), slot(cut.start + i), bytes, full);
+            auto copy = [&](int i, int sl) {  // thread 0
+                mbar_expect_tx(&merge_full[sl], bytes);
+                bulk_load(smem_u32(smem + S::kKOff + sl * bytes), slot(cut.start + i), bytes, &merge_full[sl]);
             };
             if (threadIdx.x == 0) {
                 asm volatile("fence.proxy.async;" ::: "memory");  // what other SMs wrote with plain stores is read by the copy engine
-                for (int i = 0; i < min(slots, cut.of); ++i) copy(i);
+                for (int i = 0; i < min(slots, cut.of); ++i) copy(i, i);
             }
             float M = -INFINITY, L = 0.f, x[kCols / 32][32];
+            if (live) {  // the row's reference first, while the copies fly: then a part is one product and sum for each element
+#pragma unroll 4
+                for (int i = 0; i < cut.of; ++i) M = fmaxf(M, slot(cut.start + i)[a.tile_stride * DW + 2 * row]);
+            }
+            const float ref = M == -INFINITY ? 0.f : M;
 #pragma unroll
             for (int c = 0; c < kCols / 32; ++c)
 #pragma unroll
                 for (int k = 0; k < 32; ++k) x[c][k] = 0.f;
 #pragma unroll 1
-            for (int i = 0; i < cut.of; ++i) {
-                const int sl = i % slots;
+            for (int i = 0, sl = 0; i < cut.of; ++i, sl = sl + 1 == slots ? 0 : sl + 1) {
                 if (!failed && !warp_wait(&merge_full[sl], merge_phase >> sl & 1u)) failed = true;
                 merge_phase ^= 1u << sl;
                 const uint8_t* from = smem + S::kKOff + sl * bytes;
                 if (live) {
                     const float2 ml = reinterpret_cast<const float2*>(from + a.tile_stride * DW * 4)[row];
-                    if (ml.x > M) {
-                        const float again = ex2(M - ml.x);  // 0 for the first
-                        M = ml.x;
-                        L *= again;
-#pragma unroll
-                        for (int c = 0; c < kCols / 32; ++c)
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) x[c][k] *= again;
-                    }
-                    const float w = ex2(ml.x - (M == -INFINITY ? 0.f : M));
+                    const float w = ex2(ml.x - ref);
                     L = fmaf(w, ml.y, L);
 #pragma unroll
                     for (int c = 0; c < kCols / 32; ++c)
@@ -763,7 +758,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                 }
                 rows_sync();  // read before the next copy lands
-                if (threadIdx.x == 0 && i + slots < cut.of && !failed) copy(i + slots);
+                if (threadIdx.x == 0 && i + slots < cut.of && !failed) copy(i + slots, sl);
             }
             const int T = max(a.T, 1), h = at / T;
             const uint16_t* orow = out_row(cut.b, cut.kvh, h, at - h * T);
