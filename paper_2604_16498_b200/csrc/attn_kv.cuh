@@ -101,6 +101,11 @@ __device__ __forceinline__ int kv_scan(int v, int lane) {  // inclusive sum over
 __device__ __forceinline__ int kv_sum(int v) { return __reduce_add_sync(0xffffffffu, v); }  // over all lanes
 __device__ __forceinline__ int kv_max(int v) { return __reduce_max_sync(0xffffffffu, v); }
 
+// n / d for quotients up to a few thousand: the float quotient is off by one at most.
+__device__ __forceinline__ int kv_small_quotient(int n, int d) {
+    const int q = (int)__fdividef((float)n, (float)d), rest = n - q * d;
+    return q + (rest >= d ? 1 : rest < 0 ? -1 : 0);
+}
 // Whole numbers 0 .. n - 1 shared evenly by `by` (at most n) of them, in order: the first n % by get one more than the others.
 struct KvShares {
     int by, each, more;
@@ -108,7 +113,7 @@ struct KvShares {
     __device__ __forceinline__ int first(int i) const { return i * each + min(i, more); }
     __device__ __forceinline__ int of(int u) const {  // who has u
         const int low = more * (each + 1);
-        return u < low ? u / (each + 1) : more + (u - low) / max(each, 1);
+        return u < low ? kv_small_quotient(u, each + 1) : more + kv_small_quotient(u - low, max(each, 1));
     }
 };
 

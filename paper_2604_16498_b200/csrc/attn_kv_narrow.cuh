@@ -12,7 +12,7 @@
 //
 // What bounds it: the copies' latency times the 128 KB of them that an SM has in flight while it streams, and before and after that some 5 us of
 // dependent steps (lengths, shares and queries; the warps' merge; the CTAs').  int8 rows, heads of 128: 16 x 32/8 x 1024 .. 4096 rows (87 MB)
-// 23.3 us, 1 x 32/8 x 32,768 e4m3 rows (69 MB) 22.5; 12/12 heads of 64, 40 x up to 1000 rows (34 MB) 18.7.  Twelve warps with smaller rings took
+// 23.1 us, 1 x 32/8 x 32,768 e4m3 rows (69 MB) 22.6; 12/12 heads of 64, 40 x up to 1000 rows (34 MB) 18.4.  Twelve warps with smaller rings took
 // 31.9 us for the first of these when eight took 27.3; a warp that only copies would leave the others 168 registers of the 242 they use.
 #pragma once
 
