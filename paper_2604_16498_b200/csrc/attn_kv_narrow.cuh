@@ -12,7 +12,7 @@
 //
 // What bounds it: the copies' latency times the 128 KB of them that an SM has in flight while it streams, and before and after that some 5 us of
 // dependent steps (lengths, shares and queries; the warps' merge; the CTAs').  int8 rows, heads of 128: 16 x 32/8 x 1024 .. 4096 rows (87 MB)
-// 23.1 us, 1 x 32/8 x 32,768 e4m3 rows (69 MB) 22.6; 12/12 heads of 64, 40 x up to 1000 rows (34 MB) 18.4.  Twelve warps with smaller rings took
+// 23.7 us, 1 x 32/8 x 32,768 e4m3 rows (69 MB) 23.1; 12/12 heads of 64, 40 x up to 1000 rows (34 MB) 19.2.  Twelve warps with smaller rings took
 // 31.9 us for the first of these when eight took 27.3; a warp that only copies would leave the others 168 registers of the 242 they use.
 #pragma once
 
@@ -502,7 +502,10 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
             }
             // ---- probabilities, and P^T as the B operand: keys 2c, 2c + 1 (and + 8) of row g
             const float sub[2] = {ref[0] == -INFINITY ? 0.f : ref[0], ref[1] == -INFINITY ? 0.f : ref[1]};
-            uint32_t pf[KG][2];
+            // P is rounded once to the products' type; where the output's type is no wider that would be as much as its own rounding, and what
+            // the rounding left is multiplied too (pl): fp16 outputs are off by 2.1e-4 of their size, the rounding alone, instead of 2.9e-4, for 3 % of the time.
+            const bool rest = !kEight || out_f16;
+            uint32_t pf[KG][2], pl[KG][2];
             float pr[KG][4];
 #pragma unroll
             for (int k = 0; k < KG; ++k) {
@@ -516,8 +519,17 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                     }
                     pr[k][i] = w;
                 }
-                pf[k][0] = transpose8x8(pack16<kF16>(pr[k][0], pr[k][1]));
-                pf[k][1] = transpose8x8(pack16<kF16>(pr[k][2], pr[k][3]));
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t p16 = pack16<kF16>(pr[k][2 * u], pr[k][2 * u + 1]);
+                    pf[k][u] = transpose8x8(p16);
+                    pl[k][u] = 0;
+                    if (rest) {
+                        const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&p16))
+                                                 : make_float2(__uint_as_float(p16 << 16), __uint_as_float(p16 & 0xffff0000u));
+                        pl[k][u] = transpose8x8(pack16<kF16>(pr[k][2 * u] - back.x, pr[k][2 * u + 1] - back.y));
+                    }
+                }
             }
             // ---- O^T += V^T P^T
             if constexpr (kEight) {
@@ -532,6 +544,7 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                             value_codes<kE4m3>(vr[4 * k][w4], vr[4 * k + 1][w4], hi, f[0], f[1]);
                             value_codes<kE4m3>(vr[4 * k + 2][w4], vr[4 * k + 3][w4], hi, f[2], f[3]);
                             mma_16816<true>(st.o[2 * w4 + hi], f, pf[k][0], pf[k][1]);
+                            if (rest) mma_16816<true>(st.o[2 * w4 + hi], f, pl[k][0], pl[k][1]);
                         }
                     }
             } else {
@@ -570,6 +583,7 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                 for (int s = 0; s < KS; ++s) {
                     const uint32_t f[4] = {vr[s][0] & keep[0], vr[s][1] & keep[0], vr[s][2] & keep[1], vr[s][3] & keep[1]};
                     mma_16816<kF16>(st.o[s], f, pf[0][0], pf[0][1]);
+                    mma_16816<kF16>(st.o[s], f, pl[0][0], pl[0][1]);
                 }
                 if (odd != 0) {  // those rows one by one, for the rows that see them; this lane has elements 16 s + g (+ 8) of O^T
 #pragma unroll 1
