@@ -174,7 +174,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     struct Cut { int item, start, of, b, kvh, rt; };
     __shared__ Cut cuts[2];
     __shared__ int cut_last[2];
-    __shared__ int odd_keys[kMaxOdd], odd_count;  // halves of rows of V with elements that are not finite numbers, which some of the tokens see
+    // halves of rows of V with elements that are not finite numbers, which some of the tokens see; pieces count in turns (see where they are cleared)
+    __shared__ int odd_keys[kMaxOdd], odd_count[2];
     __shared__ float q_mul[128];                  // 8-bit: what a row's scores are multiplied by
     __shared__ float4 group_state[2][128];        // m, l and the unit of O
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -192,7 +193,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         prefetch_tmap(&tmap_q);
         prefetch_tmap(&tmap_k);
         prefetch_tmap(&tmap_v);
-        odd_count = 0;
+        odd_count[0] = odd_count[1] = 0;
         cuts[0].of = cuts[1].of = 0;
     }
     if (warp == 9) {
@@ -613,7 +614,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                                 if (put) *at16 = make_uint4(x[0], x[1], x[2], x[3]);
                             }
                             if (odd && !out) {
-                                const int i = atomicAdd(&odd_count, 1);
+                                const int i = atomicAdd(&odd_count[parts & 1], 1);
                                 if (i < kMaxOdd) odd_keys[i] = (key0 + key) * 2 + (row & 1);
                             }
                         }
@@ -628,7 +629,6 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             if (!failed && !warp_wait(&pv_done[group], (steps - 1) & 1)) failed = true;
             tc_fence_after_sync();
             base += n;
-            ++parts;
             group_state[group][row] = make_float4(m, l, unit, 0.f);
             rows_sync();  // both groups' products are done, their states and odd_keys complete
             tc_fence_after_sync();
@@ -637,7 +637,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             // int8: column 4 i + 1 holds element 4 i + 2 and the other way round
             const bool whole = p.of == 1;
             uint16_t* orow = out_row(p.b, p.kvh, h, tok);
-            const int odds = kEight ? 0 : min(odd_count, kMaxOdd);
+            const int odds = kEight ? 0 : min(odd_count[parts & 1], kMaxOdd);
             float* mine = slot(idx);  // (of an item with several pieces)
             if (!idle && !failed) {
                 const float4 s0 = group_state[0][row], s1 = group_state[1][row];
@@ -686,12 +686,14 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 }
                 if (!whole && live && group == 0) reinterpret_cast<float2*>(mine + a.tile_stride * DW)[row] = make_float2(M, L);
             }
+            // The next piece's counter, cleared on this side of the barrier, behind which other warps count into it at once: it was last read
+            // before the previous piece's.  This piece's is being read.
+            if (threadIdx.x == 0) odd_count[(parts + 1) & 1] = 0;
+            ++parts;
             tc_fence_before_sync();
             rows_sync();  // the parts are written; odd_keys and O have been read
-            if (threadIdx.x == 0) {
-                odd_count = 0;
-                if (!whole) cuts[idx / ctas] = {p.item, p.start, p.of, p.b, p.kvh, p.rt};  // at most two of them: they come first, and are no more than twice the CTAs
-            }
+            if (threadIdx.x == 0 && !whole)
+                cuts[idx / ctas] = {p.item, p.start, p.of, p.b, p.kvh, p.rt};  // at most two of them: they come first, and are no more than twice the CTAs
         }
 
         // ---- items that other CTAs have parts of: the CTA that arrives last merges all of them
