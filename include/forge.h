@@ -393,6 +393,9 @@ int forge_kv_read(const forge_kv_cache* cache, void* k_out, void* v_out, int dty
  * beyond Smax are not there.  q, out: [B, Hq, T, D] views.  A row of the cache that a token does not see has no part in
  * its output, whatever the row holds.
  *
+ * Rows may be of any sizes.  8-bit formats: what a row adds to a token's output (its weight times its scale) is lost where it is more than 2^30
+ * smaller than the largest such part of that token; FORGE_KV_F16: a weight is, where it is more than 2^30 smaller than the token's largest.
+ *
  * workspace: at least forge_attn_kv_workspace_bytes(B, Hq, Hkv, T, D) bytes, 16-byte aligned; T = 1 for the single token.  Its
  * arrival counters (the first max(256 KiB, 4 B Hkv ceil(G / min(G, floor(128 / T)))) bytes, G = Hq / Hkv) must be ZERO when a call
  * starts and are zero when it has completed: clear a new workspace once with forge_attn_kv_workspace_init; every shape with

@@ -101,6 +101,31 @@ __device__ __forceinline__ int kv_scan(int v, int lane) {  // inclusive sum over
 __device__ __forceinline__ int kv_sum(int v) { return __reduce_add_sync(0xffffffffu, v); }  // over all lanes
 __device__ __forceinline__ int kv_max(int v) { return __reduce_max_sync(0xffffffffu, v); }
 
+// 8-bit rows of V: the products' operand is p vs (vs the row's scale) in fp16, and what a query row has of it may be anything: scales differ by
+// up to 2^230, and a row of any size may have next to no weight.  So each query row has a unit of its own, a power of two by which its
+// p vs are divided and in which its O is kept.  It follows the largest p vs that the row has met, seen rows alone: raised where one would pass 2^14 in
+// fp16 (so that the largest comes to 2^5 .. 2^6: what is more than 2^30 smaller than the largest is lost, and no more), and lowered with p when the
+// reference m is raised.  Units are 2^kUnitLow to 2^122: the smallest scale that a cache has is 2^-109, and p at least 2^-9 for the largest.
+// unit_inv holds 1 / unit.  p is at most 1 there, so that p vs stays finite.
+constexpr int kUnitLow = -125, kUnitHigh = 122;
+constexpr float kUnitTop = 16384.f;
+__device__ __forceinline__ float kv_pow2(int n) { return __int_as_float(max(n + 127, 0) << 23); }  // n <= 127; 0 below 2^-126
+__device__ __forceinline__ int kv_log2(float pow2) { return (__float_as_int(pow2) >> 23) - 127; }
+__device__ __forceinline__ float kv_unit(float unit_inv) { return kv_pow2(-kv_log2(unit_inv)); }
+// Both return what O is multiplied by.  p becomes 2^by times what it was (by: a whole number, at most 0): so does the unit, as far down as it goes.
+__device__ __forceinline__ float kv_lower_unit(float& unit_inv, float by) {
+    const int unit = -kv_log2(unit_inv) + (int)fmaxf(by, -300.f), now = max(unit, kUnitLow);
+    unit_inv = kv_pow2(-now);
+    return kv_pow2(unit - now);
+}
+// `most`: the largest |p vs| of the row that is about to enter O.
+__device__ __forceinline__ float kv_raise_unit(float& unit_inv, float most) {
+    if (!(most * unit_inv > kUnitTop)) return 1.f;
+    const int unit = -kv_log2(unit_inv), now = min(kv_log2(most) + 1 - 6, kUnitHigh);
+    unit_inv = kv_pow2(-now);
+    return kv_pow2(unit - now);
+}
+
 // n / d for quotients up to a few thousand: the float quotient is off by one at most.
 __device__ __forceinline__ int kv_small_quotient(int n, int d) {
     const int q = (int)__fdividef((float)n, (float)d), rest = n - q * d;

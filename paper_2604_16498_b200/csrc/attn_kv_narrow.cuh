@@ -130,8 +130,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     constexpr int KEYS = S::kKeys;
     constexpr int KG = KEYS / 16;                // groups of 16 keys in a block
     constexpr int KS = DW / 16;                  // 16-wide steps over the head: of the scores' contraction, and of O^T's rows
-    // p reaches 2^14, 2^8 above what the reference stands for
-    constexpr float kTop = 14.f, kLift = 6.f;
+    // 16-bit rows: p reaches 2^14, 2^8 above what the reference m stands for.  8-bit rows: m is a whole number, p is 2^(x - m - 8), at most 1.
+    constexpr float kTop = kEight ? 0.f : 14.f, kLift = kEight ? -8.f : 6.f;
     extern __shared__ __align__(128) uint8_t smem_raw[];
     __shared__ uint64_t full_all[kNarrowWarps][S::kStages];
     // What a warp leaves of an item that it did not have all of: where it lies, how many blocks and which rows of the cache; 0 blocks: nothing.
@@ -366,8 +366,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
 
         st.clear();
         float ref[2] = {-INFINITY, -INFINITY};  // reference - kLift; -infinity: none yet
-        float unit = 1.17549435e-38f, unit_inv = 0.f;  // 8-bit: power of two that P is divided by, at least the largest scale of V so far
-        if constexpr (kEight) unit_inv = 8.5070592e37f;  // 1 / unit
+        // 8-bit rows: O^T of each row is kept in units of a power of two, with which p vs goes into the products' fp16 (see kv_unit)
+        float unit_inv[2] = {kv_pow2(-kUnitLow), kv_pow2(-kUnitLow)};
         for (int blk = 0; blk < blocks; ++blk, ++n) {
             const int stage = n % S::kStages;
             if (!failed && !ptx::warp_wait(&full[stage], (n / S::kStages) & 1)) failed = true;
@@ -460,40 +460,29 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                     }
             }
             // ---- references: raised where a score passes them by 2^8 (the first of a row always does)
-            float mx[2] = {-INFINITY, -INFINITY}, big = 0.f;
+            float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
             for (int k = 0; k < KG; ++k)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) mx[i & 1] = fmaxf(mx[i & 1], x[k][i]);
-            bool lift = mx[0] > ref[0] + kTop || mx[1] > ref[1] + kTop;
-            if constexpr (kEight) {
-#pragma unroll
-                for (int k = 0; k < KG; ++k) big = fmaxf(big, fmaxf(vs[k][0], vs[k][1]));
-                lift |= big > unit;
-            }
+            const bool lift = mx[0] > ref[0] + kTop || mx[1] > ref[1] + kTop;
             if (__any_sync(0xffffffffu, lift)) {
                 float alpha[2];
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
 #pragma unroll
                     for (int o = 4; o < 32; o <<= 1) mx[r] = fmaxf(mx[r], __shfl_xor_sync(0xffffffffu, mx[r], o));
-                    const float m_new = fmaxf(st.m[r], mx[r]);
+                    const float m_new = fmaxf(st.m[r], kEight ? ceilf(mx[r]) : mx[r]);
                     alpha[r] = m_new == -INFINITY ? 1.f : ex2(st.m[r] - m_new);
+                    if constexpr (kEight) {
+                        const float by = st.m[r] == -INFINITY ? 0.f : st.m[r] - m_new;
+                        st.l[r] *= alpha[r];
+                        alpha[r] = kv_lower_unit(unit_inv[r], by);
+                    } else {
+                        st.l[r] *= alpha[r];
+                    }
                     st.m[r] = m_new;
                     ref[r] = m_new - kLift;  // -infinity stays
-                    st.l[r] *= alpha[r];
-                }
-                if constexpr (kEight) {
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-                    if (big > unit) {
-                        const uint32_t up = min((__float_as_uint(big) + 0x007fffffu) & 0x7f800000u, 0x7e000000u);  // at most 2^125
-                        const float now = __uint_as_float(up), now_inv = __uint_as_float(0x7f000000u - up);
-                        alpha[0] *= unit * now_inv;
-                        alpha[1] *= unit * now_inv;
-                        unit = now;
-                        unit_inv = now_inv;
-                    }
                 }
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
@@ -514,11 +503,38 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                     float w = ex2(x[k][i] - sub[i & 1]);
                     st.l[i & 1] += w;
                     if constexpr (kEight) {
-                        w *= vs[k][i >> 1] * unit_inv;
+                        w *= vs[k][i >> 1];
                         if (cut && !(there >> (4 * k + i) & 1u)) w = 0.f;
                     }
                     pr[k][i] = w;
                 }
+            }
+            if constexpr (kEight) {
+                float most[2] = {0.f, 0.f};
+#pragma unroll
+                for (int k = 0; k < KG; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) most[i & 1] = fmaxf(most[i & 1], fabsf(pr[k][i]));
+                if (__any_sync(0xffffffffu, most[0] * unit_inv[0] > kUnitTop || most[1] * unit_inv[1] > kUnitTop)) {
+                    float alpha[2];
+#pragma unroll
+                    for (int r = 0; r < 2; ++r) {
+#pragma unroll
+                        for (int o = 4; o < 32; o <<= 1) most[r] = fmaxf(most[r], __shfl_xor_sync(0xffffffffu, most[r], o));
+                        alpha[r] = kv_raise_unit(unit_inv[r], most[r]);
+                    }
+#pragma unroll
+                    for (int s = 0; s < KS; ++s)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) st.o[s][i] *= alpha[i & 1];
+                }
+#pragma unroll
+                for (int k = 0; k < KG; ++k)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) pr[k][i] *= unit_inv[i & 1];
+            }
+#pragma unroll
+            for (int k = 0; k < KG; ++k) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const uint32_t p16 = pack16<kF16>(pr[k][2 * u], pr[k][2 * u + 1]);
@@ -615,11 +631,11 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) st.l[r] += __shfl_xor_sync(0xffffffffu, st.l[r], o);
         if constexpr (kEight) {
-            const float f = unit ;
+            const float unit[2] = {kv_unit(unit_inv[0]), kv_unit(unit_inv[1])};
 #pragma unroll
             for (int s = 0; s < KS; ++s)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) st.o[s][i] *= f;
+                for (int i = 0; i < 4; ++i) st.o[s][i] *= unit[i & 1];
         }
         const Left left = {item_start, cur.tiles, p.b, p.kvh};
         if (blocks == cur.tiles) {  // all of it

@@ -27,7 +27,8 @@ namespace {
 // whole (4 steps more), 600 take 17.6 and 19.0 (7 more); 1 x 32/8 x 5 tokens over 16-bit rows: 600 take 11.7 and 11.3 (4 more), 800 take
 // 13.7 and 14.8 (6 more).
 constexpr int kRowsMerge = 4;
-constexpr float kRowsTop = 14.f, kRowsLift = 6.f;  // p reaches 2^14, 2^8 above what the reference stands for
+// p reaches 2^8 above what the reference m stands for.  16-bit rows: that is 2^14.  8-bit rows: 1, and m is a whole number.
+constexpr float kRowsAbove = 8.f;
 
 template <int DW, int FMT>
 struct RowsShape {
@@ -51,8 +52,8 @@ struct RowsShape {
     static constexpr int kKOff = kQBytes, kKEach = kEight ? 2 * kOpBytes : kOpBytes;
     static constexpr int kVOff = kEight ? kKOff + kOpBytes : kKOff + kKBufs * kOpBytes, kVEach = kKEach;
     static constexpr int kLoadOff = kEight ? kKOff + kOps * 2 * kOpBytes : kVOff + kVBufs * kOpBytes;
-    static constexpr int kScaleOff = kLoadOff + kLoads * kLoadBytes; // 8-bit: of each operand buffer, scales of K and V and the largest of V
-    static constexpr int kScaleBytes = 2 * kStep * 4 + 16;
+    static constexpr int kScaleOff = kLoadOff + kLoads * kLoadBytes; // 8-bit: of each operand buffer, scales of K and V
+    static constexpr int kScaleBytes = 2 * kStep * 4;
     static constexpr int kOutOff = (kScaleOff + kOps * kScaleBytes + 127) / 128 * 128;  // of each softmax warp, 32 rows x 32 elements on their way out
     static constexpr int kSmem = 1024 + kOutOff + 8 * 2048;
     static_assert(kSmem <= 232448 - 6144, "shared memory");
@@ -160,6 +161,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     constexpr int kLoads = S::kLoads ? S::kLoads : 1, kConvThreads = S::kConvWarps ? S::kConvWarps * 32 : 32;
     constexpr bool kEight = S::kEight, kE4m3 = FMT == FORGE_KV_E4M3;
     constexpr bool kF16 = FMT != FORGE_KV_BF16;
+    constexpr float kLift = kEight ? -8.f : 6.f;
     constexpr int kColS = 0, kColO = 2 * S::kStep;  // S of step n at kStep (n % 2), O of group h at kColO + DW h
     constexpr int kTmemCols = kColO + 2 * DW <= 256 ? 256 : 512;
     constexpr int kMaxOdd = 2 * kKvMaxTokens;
@@ -353,7 +355,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         *reinterpret_cast<uint4*>(dst + sw128(row, (piece & 3) * 2)) = make_uint4(o[0], o[1], o[2], o[3]);
                         *reinterpret_cast<uint4*>(dst + sw128(row, (piece & 3) * 2 + 1)) = make_uint4(o[4], o[5], o[6], o[7]);
                     }
-                // scales (warp 10: of K, warp 11: of V): those of rows that are not there count as zero; the largest of V's
+                // scales (warp 10: of K, warp 11: of V): those of rows that are not there count as zero
                 if (warp < 12) {
                     float* sc = reinterpret_cast<float*>(smem + S::kScaleOff + buf * S::kScaleBytes) + (warp - 10) * S::kStep;
                     const float* from = reinterpret_cast<const float*>(smem + S::kLoadOff + st * S::kLoadBytes + 2 * S::kRawBytes + (warp - 10) * S::kScaleBox) +
@@ -361,12 +363,6 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     const float x0 = j0 + lane < p.rows ? from[lane] : 0.f, x1 = j0 + 32 + lane < p.rows ? from[32 + lane] : 0.f;
                     sc[lane] = x0;
                     sc[32 + lane] = x1;
-                    if (warp == 11) {
-                        float big = fmaxf(x0, x1);
-#pragma unroll
-                        for (int o = 16; o > 0; o >>= 1) big = fmaxf(big, __shfl_xor_sync(0xffffffffu, big, o));
-                        if (lane == 0) sc[S::kStep] = big;
-                    }
                 }
                 fence_proxy_async_smem();
                 __syncwarp();
@@ -473,7 +469,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             }
 
             float m = -INFINITY, l = 0.f;
-            float unit = 1.17549435e-38f, unit_inv = 8.5070592e37f;  // 8-bit: power of two that P is divided by, at least V's largest scale so far
+            float unit_inv = kv_pow2(-kUnitLow);  // 8-bit: of this row (see kUnitLow)
             const int n = p.tiles;
 #pragma unroll 1
             for (int g = 0; g < n; ++g) {
@@ -528,19 +524,41 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         for (int k = 0; k < 32; k += 2) mx = max3(mx, x[k], x[k + 1]);
                     }
                     // the reference is raised only where a score passes it by 2^8 (the first of a row always does)
-                    if (mx > m + (kRowsTop - kRowsLift)) {
-                        alpha = m == -INFINITY ? 1.f : ex2(m - mx);
+                    if (mx > m + kRowsAbove) {
+                        if constexpr (kEight) mx = ceilf(mx);
+                        const float by = m == -INFINITY ? 0.f : m - mx;
                         m = mx;
+                        alpha = ex2(by);
                         l *= alpha;
+                        if constexpr (kEight) alpha = kv_lower_unit(unit_inv, by);
                     }
-                    if constexpr (kEight) {
-                        const float big = sc[2 * S::kStep - group * S::kHalf];
-                        if (big > unit) {  // the same in all threads
-                            const uint32_t up = min((__float_as_uint(big) + 0x007fffffu) & 0x7f800000u, 0x7e000000u);
-                            unit_inv = __uint_as_float(0x7f000000u - up);
-                            alpha *= unit * unit_inv;
-                            unit = __uint_as_float(up);
+                    if constexpr (kEight) {  // p, then p vs
+                        const float ref = m == -INFINITY ? 0.f : m - kLift;
+                        float most = 0.f;
+#pragma unroll
+                        for (int c = 0; c < S::kHalf; c += 32) {
+                            float (&x)[32] = kept[c / 32];
+                            float add[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                            for (int k = 0; k < 32; ++k) {
+                                x[k] = ex2(x[k] - ref);
+                                add[k & 3] += x[k];
+                            }
+                            l += (add[0] + add[1]) + (add[2] + add[3]);
+#pragma unroll
+                            for (int k = 0; k < 32; k += 4) {
+                                const float4 vs = *reinterpret_cast<const float4*>(sc + S::kStep + c + k);
+                                x[k] *= vs.x; x[k + 1] *= vs.y; x[k + 2] *= vs.z; x[k + 3] *= vs.w;
+                            }
+                            if (cut) {  // the scale of a row that is not seen may be anything
+                                const uint32_t v = seen(c);
+#pragma unroll
+                                for (int k = 0; k < 32; ++k) x[k] = v >> k & 1u ? x[k] : 0.f;
+                            }
+#pragma unroll
+                            for (int k = 0; k < 32; k += 2) most = max3(most, fabsf(x[k]), fabsf(x[k + 1]));
                         }
+                        alpha *= kv_raise_unit(unit_inv, most);
                     }
                 }
                 if (g > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
@@ -559,28 +577,21 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 }
                 ++steps;
                 if (!idle) {
-                    const float ref = m == -INFINITY ? 0.f : m - kRowsLift;
+                    const float ref = m == -INFINITY ? 0.f : m - kLift;
 #pragma unroll
                     for (int c = 0; c < S::kHalf; c += 32) {
                         float (&x)[32] = kept[c / 32];
-                        float add[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) {
-                            x[k] = ex2(x[k] - ref);
-                            add[k & 3] += x[k];
-                        }
-                        l += (add[0] + add[1]) + (add[2] + add[3]);
                         if constexpr (kEight) {
 #pragma unroll
-                            for (int k = 0; k < 32; k += 4) {
-                                const float4 vs = *reinterpret_cast<const float4*>(sc + S::kStep + c + k);
-                                x[k] *= vs.x * unit_inv; x[k + 1] *= vs.y * unit_inv; x[k + 2] *= vs.z * unit_inv; x[k + 3] *= vs.w * unit_inv;
-                            }
-                            if (cut) {  // the scale of a row that is not seen may be anything
-                                const uint32_t v = seen(c);
+                            for (int k = 0; k < 32; ++k) x[k] *= unit_inv;
+                        } else {
+                            float add[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                                for (int k = 0; k < 32; ++k) x[k] = v >> k & 1u ? x[k] : 0.f;
+                            for (int k = 0; k < 32; ++k) {
+                                x[k] = ex2(x[k] - ref);
+                                add[k & 3] += x[k];
                             }
+                            l += (add[0] + add[1]) + (add[2] + add[3]);
                         }
                         uint32_t packed[16];
 #pragma unroll
@@ -629,7 +640,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             if (!failed && !warp_wait(&pv_done[group], (steps - 1) & 1)) failed = true;
             tc_fence_after_sync();
             base += n;
-            group_state[group][row] = make_float4(m, l, unit, 0.f);
+            group_state[group][row] = make_float4(m, l, kv_unit(unit_inv), 0.f);
             rows_sync();  // both groups' products are done, their states and odd_keys complete
             tc_fence_after_sync();
 

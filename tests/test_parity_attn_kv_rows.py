@@ -45,3 +45,145 @@ def test_not_a_number_in_every_item_of_a_long_run(dtype, form, B, Hq, Hkv, T):
         after = run_tree(q, cache, n, bits)
         assert torch.equal(after.isnan().all(-1), hit[:, None].expand(B, Hq, T))
         assert torch.equal(torch.where(hit[:, None, :, None], before, after), before)
+
+
+# ------------------------------------------------------------------------------------------------------- as close as it is said to be
+def definition(q, cache, past, sees=None, scale=None):
+    """q [B,Hq,T,D], the rows as in kv_reference.attention -> (out in 64 bits, bound), both from the rows that a token sees alone.
+    Weights (softmax, times the row's scale with 8-bit rows) are rounded to the operands' type, twice (what the first leaves is multiplied
+    too) where the output is no narrower than them: 2^-8 or 2^-11, or their squares; in fp16 to 2^-24 at least, where the token's largest
+    has come to 2^5 or more: 2^-30 of it.  The output is rounded once.  Scores and sums as in kv_reference.attention."""
+    B, Hq, T, D = q.shape
+    k, v = ref.decode_values(cache.k, cache.k_scale), ref.decode_values(cache.v, cache.v_scale)
+    Smax, Hkv = k.shape[2], k.shape[1]
+    G, eight = Hq // Hkv, cache.k_scale is not None
+    scale = D ** -0.5 if scale is None else scale
+    past = past.clamp(0, Smax)
+    smallest = 2.0 ** -25 if q.dtype == HF else 2.0 ** -134  # half of the type's smallest number
+    operand = torch.float16 if eight else q.dtype
+    u = ref.HALF[operand] if eight and q.dtype == BF else ref.HALF[operand] ** 2
+    top = cache.v_scale.double().abs() * ref.TOP[cache.v.dtype] if eight else v.abs().amax(-1)  # of a row's elements
+    out, bound = torch.zeros(q.shape, dtype=torch.float64, device="cuda"), torch.zeros(q.shape, dtype=torch.float64, device="cuda")
+    for b in range(B):
+        for t in range(T):
+            rows = torch.arange(Smax, device="cuda") < past[b]
+            if sees is not None:
+                at = int(past[b])
+                n = min(T, Smax - at)
+                rows[at:at + n] = sees[b, t, :n]
+            if not bool(rows.any()):
+                continue
+            kb, vb, tb = k[b][:, rows], v[b][:, rows], top[b][:, rows]
+            x = q[b, :, t].double().view(Hkv, G, D)
+            s = torch.einsum("hgd,hjd->hgj", x, kb) * scale
+            mag = (torch.einsum("hgd,hjd->hgj", x.abs(), kb.abs()) * abs(scale)).amax(-1)
+            w = torch.softmax(s, -1)
+            o = torch.einsum("hgj,hjd->hgd", w, vb)
+            wv = torch.einsum("hgj,hjd->hgd", w, vb.abs())
+            if operand == BF:
+                lost = 0.0
+            elif eight:  # of the largest weight times its row
+                lost = w.shape[-1] * 2.0 ** -30 * (w * tb[:, None]).amax(-1)
+            else:        # of the largest weight, times any row
+                lost = w.shape[-1] * 2.0 ** -30 * w.amax(-1) * tb.amax(-1)[:, None]
+            e = (u + 2 * mag * (D + 8) * 2.0 ** -22 + 2.0 ** -17)[..., None] * wv + ref.HALF[q.dtype] * o.abs() * 1.01 + smallest
+            out[b, :, t], bound[b, :, t] = o.view(Hq, D), (e + (lost if operand == BF else lost[..., None])).view(Hq, D)
+    return out, bound
+
+
+def run_decode(q, cache, lens, **kw):
+    out = binding.attn_decode_kv(q, cache, lens, **kw)
+    binding.check_status()
+    return out
+
+
+def assert_close(q, cache, lens, sees=None, scale=None, what=""):
+    """The call for these tokens (a single one, with no rows of its own: decode)."""
+    want, bound = definition(q, cache, lens, sees, scale)
+    if sees is None:
+        got = run_decode(q[:, :, 0].contiguous(), cache, lens, scale=scale)[:, :, None]
+    else:
+        got = run_tree(q, cache, lens, ref.tree_bits(sees), scale=scale)
+    ref.assert_within(got, want, bound, what)
+
+
+def rows_cache(k, v, form):
+    """A cache of the rows k, v (fp32, finite)."""
+    (k, ks), (v, vs) = (ref.quantise(x, form) if form in ref.TOP else (x.to(form), None) for x in (k, v))
+    return binding.KVCache(k, v, ks, vs)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=IDS)
+@pytest.mark.parametrize("Hq,T", [(2, 6), (8, 40)])
+@pytest.mark.parametrize("size", [2.0 ** 20, 2.0 ** 100, float("inf")])
+def test_the_size_of_a_row_that_is_not_seen_changes_nothing(dtype, form, Hq, T, size):
+    g = ref.seeded(62)
+    if dtype == HF and form == HF:
+        size = min(size, 60000.0)
+    for past in (0, 40, 125):
+        cache = ref.make_cache(g, 2, 2, 300, 128, form, binding)
+        q, n = ref.normal(g, (2, Hq, T, 128), dtype), lens_of([past, past])
+        sees = torch.eye(T, dtype=torch.bool, device="cuda")
+        sees[:, 0] = True
+        bits = ref.tree_bits(sees)[None]
+        before = run_tree(q, cache, n, bits)
+        at = past + 3  # token 3 alone sees it
+        if cache.v_scale is None:
+            cache.k[:, :, at], cache.v[:, :, at] = 0, size
+        else:
+            cache.v_scale[:, :, at] = size
+        after = run_tree(q, cache, n, bits)
+        after[:, :, 3] = before[:, :, 3]
+        assert torch.equal(before, after)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS[2:], ids=IDS[2:])
+@pytest.mark.parametrize("Hq,T", [(2, 1), (2, 3), (16, 5)])
+@pytest.mark.parametrize("power", [16, 30, 45, 60, 100])
+@pytest.mark.parametrize("at", [0, 70, 299])
+def test_a_huge_row_with_next_to_no_weight(dtype, form, Hq, T, power, at):
+    """A row of V 2^power times the others' size, whose weight makes less of it than of any of them: first, in the middle, last."""
+    g = ref.seeded(63)
+    B, Hkv, D, past = 2, 2, 64, 300
+    k, v = (torch.randn((B, Hkv, 310, D), generator=g, device="cuda") for _ in range(2))
+    q = ref.normal(g, (B, Hq, T, D), dtype)
+    k[..., 0], q[..., 0] = 0, 8
+    k[:, :, at] = 0
+    k[:, :, at, 0] = -(power + 20.0)  # a score of -(power + 20) below zero: a weight of 2^(-1.44 (power + 20))
+    v[:, :, at] *= 2.0 ** power
+    cache = rows_cache(k, v, form)
+    sees = None if T == 1 else torch.ones((B, T, T), dtype=torch.bool, device="cuda").tril()
+    assert_close(q, cache, lens_of([past, past - at // 100]), sees, 0.125)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS[2:], ids=IDS[2:])
+@pytest.mark.parametrize("Hq,T", [(2, 1), (2, 3), (16, 5)])
+def test_sizes_and_scores_far_apart(dtype, form, Hq, T):
+    """Rows of V between 2^-30 and 2^30 and scores of -60 to 60, apart from one another and the larger the smaller: what has the
+    most of the output changes over the rows, upwards and downwards."""
+    g = ref.seeded(64)
+    B, Hkv, D, past = 6, 2, 64, 700
+    k, v = (torch.randn((B, Hkv, 710, D), generator=g, device="cuda") for _ in range(2))
+    x = torch.linspace(-60, 60, 710, device="cuda")
+    x = torch.stack([x, -x, x.abs(), -x.abs(), 60 * torch.sin(x), x[torch.randperm(710, generator=g, device="cuda")]])[:, None, :]
+    q = ref.normal(g, (B, Hq, T, D), dtype, 0.1)
+    q[..., 0] = 8
+    k[..., 0] = x
+    v *= torch.exp2(-0.5 * x + 4 * torch.randn((B, Hkv, 710), generator=g, device="cuda"))[..., None]
+    cache = rows_cache(k, v, form)
+    sees = None if T == 1 else torch.ones((B, T, T), dtype=torch.bool, device="cuda").tril()
+    assert_close(q, cache, lens_of([past - 50 * b for b in range(B)]), sees, 0.125)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS[2:], ids=IDS[2:])
+@pytest.mark.parametrize("Hq,T", [(2, 1), (16, 5)])
+def test_rows_of_the_smallest_and_largest_sizes(dtype, form, Hq, T):
+    """The ends of what kv_append keeps of bf16 rows, one sequence each; outputs of fp16 tokens stay within their range."""
+    g = ref.seeded(65)
+    sizes = [2.0 ** -99, 2.0 ** -60, 2.0 ** 100] if dtype == BF else [2.0 ** -20, 1.0, 2.0 ** 10]
+    k, v = (torch.randn((len(sizes), 2, 200, 64), generator=g, device="cuda") for _ in range(2))
+    v *= torch.tensor(sizes, device="cuda")[:, None, None, None]
+    cache = rows_cache(k, v, form)
+    q = ref.normal(g, (len(sizes), Hq, T, 64), dtype)
+    sees = None if T == 1 else torch.ones((len(sizes), T, T), dtype=torch.bool, device="cuda").tril()
+    assert_close(q, cache, lens_of([190] * len(sizes)), sees)
