@@ -187,3 +187,18 @@ def test_rows_of_the_smallest_and_largest_sizes(dtype, form, Hq, T):
     q = ref.normal(g, (len(sizes), Hq, T, 64), dtype)
     sees = None if T == 1 else torch.ones((len(sizes), T, T), dtype=torch.bool, device="cuda").tril()
     assert_close(q, cache, lens_of([190] * len(sizes)), sees)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=IDS)
+@pytest.mark.parametrize("Hq,T", [(2, 1), (2, 3), (8, 6), (32, 1), (24, 17)])
+def test_weights_keep_their_bits(dtype, form, Hq, T):
+    """Few rows, of which half cancel the other half: what the rounding of the weights leaves shows in the output."""
+    g = ref.seeded(66)
+    B, Hkv, D = 24, 2, 64
+    v = torch.randn((B, Hkv, 40, D), generator=g, device="cuda")
+    v[:, :, 1::2] = -v[:, :, 0::2]
+    k = torch.randn((B, Hkv, 40, D), generator=g, device="cuda")
+    cache = rows_cache(k, v, form)
+    q = ref.normal(g, (B, Hq, T, D), dtype)
+    sees = None if T == 1 and Hq == 2 else torch.ones((B, T, T), dtype=torch.bool, device="cuda").tril()
+    assert_close(q, cache, lens_of([2 + 2 * (b % 9) for b in range(B)]), sees, 0.02)
