@@ -202,3 +202,21 @@ def test_weights_keep_their_bits(dtype, form, Hq, T):
     q = ref.normal(g, (B, Hq, T, D), dtype)
     sees = None if T == 1 and Hq == 2 else torch.ones((B, T, T), dtype=torch.bool, device="cuda").tril()
     assert_close(q, cache, lens_of([2 + 2 * (b % 9) for b in range(B)]), sees, 0.02)
+
+
+@pytest.mark.parametrize("dtype,form", FORMS, ids=IDS)
+@pytest.mark.parametrize("Hq,T", [(2, 1), (8, 6)])
+def test_scores_of_queries_of_one_sign(dtype, form, Hq, T):
+    """Keys with one large element, where the query has none, and otherwise small ones of either sign: the score is no larger than
+    its few small terms, however large the sum of the query's elements is."""
+    g = ref.seeded(67)
+    B, Hkv, D = 48, 2, 128
+    k = torch.randint(-1, 2, (B, Hkv, 30, D), generator=g, device="cuda").float()
+    k[..., 0] = 127
+    v = torch.randn((B, Hkv, 30, D), generator=g, device="cuda")
+    v[:, :, 1::2] = -v[:, :, 0::2]
+    cache = rows_cache(k, v, form)
+    q = (1 + 0.3 * torch.rand((B, Hq, T, D), generator=g, device="cuda")).to(dtype)
+    q[..., 0] = 0
+    sees = None if T == 1 else torch.ones((B, T, T), dtype=torch.bool, device="cuda").tril()
+    assert_close(q, cache, lens_of([2 + 2 * (b % 8) for b in range(B)]), sees, 0.25)
