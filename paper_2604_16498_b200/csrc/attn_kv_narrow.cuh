@@ -321,8 +321,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 const float top = a.q_f16 ? __half2float(__ushort_as_half((unsigned short)big)) : __uint_as_float(big << 16);
-                const int e = (int)(__float_as_uint(top) >> 23) - 127;  // the largest goes to [2^14, 2^15); rows of zeros or with infinities stay
-                const int up = top == 0.f || e == 128 ? 0 : min(max(14 - e, -110), 110);
+                const int e = (int)(__float_as_uint(top) >> 23) - 127;  // the largest goes to [2^14, 2^15) (bf16's goes up to 2^127; one below 2^-96 stays smaller); rows of zeros or with infinities stay
+                const int up = top == 0.f || e == 128 ? 0 : min(max(14 - e, -113), 110);
                 const float f = __int_as_float((127 + up) << 23);
                 q_mul = a.scale_log2 * __int_as_float((127 - up) << 23);
 #pragma unroll

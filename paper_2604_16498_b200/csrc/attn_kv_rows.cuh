@@ -448,7 +448,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     big = max(big & 0xffffu, big >> 16);
                     const float top = a.q_f16 ? __half2float(__ushort_as_half((unsigned short)big)) : __uint_as_float(big << 16);
                     const int e = (int)(__float_as_uint(top) >> 23) - 127;
-                    const int up = top == 0.f || e == 128 ? 0 : min(max(14 - e, -110), 110);
+                    const int up = top == 0.f || e == 128 ? 0 : min(max(14 - e, -113), 110);
                     const float f = __int_as_float((127 + up) << 23);
                     q_mul[row] = a.scale_log2 * __int_as_float((127 - up) << 23);
 #pragma unroll 4

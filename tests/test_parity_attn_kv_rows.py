@@ -220,3 +220,16 @@ def test_scores_of_queries_of_one_sign(dtype, form, Hq, T):
     q[..., 0] = 0
     sees = None if T == 1 else torch.ones((B, T, T), dtype=torch.bool, device="cuda").tril()
     assert_close(q, cache, lens_of([2 + 2 * (b % 8) for b in range(B)]), sees, 0.25)
+
+
+@pytest.mark.parametrize("form", [I8, E4])
+@pytest.mark.parametrize("Hq,T", [(4, 1), (32, 4)])
+@pytest.mark.parametrize("power", [126, 120, -96, -110, -124])
+def test_queries_at_the_ends_of_bf16(form, Hq, T, power):
+    """Only their products with the scale are ordinary numbers."""
+    g = ref.seeded(68)
+    k, v = (torch.randn((2, 2, 150, 64), generator=g, device="cuda") for _ in range(2))
+    cache = rows_cache(k / 16 if power > 0 else k, v, form)
+    q = ((torch.rand((2, Hq, T, 64), generator=g, device="cuda") * 3.9 - 1.95) * 2.0 ** power).to(BF)
+    sees = None if T == 1 else torch.ones((2, T, T), dtype=torch.bool, device="cuda").tril()
+    assert_close(q, cache, lens_of([140, 77]), sees, (2.0 if power > 0 else 0.125) * 2.0 ** -power)
