@@ -433,8 +433,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     x[k][i] = even[i] + odd[i];
-                    if constexpr (kEight) x[k][i] *= ks[k][i >> 1];
-                    x[k][i] *= row_mul[i & 1];
+                    // the factors first: each may be as far from 1 as the other makes up for
+                    x[k][i] *= kEight ? ks[k][i >> 1] * row_mul[i & 1] : row_mul[i & 1];
                 }
             }
             const bool cut = j0 + KEYS > p.past;  // keys beyond the past: not everyone sees them

@@ -495,7 +495,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 const float* sc = reinterpret_cast<const float*>(smem + S::kScaleOff + buf * S::kScaleBytes) + group * S::kHalf;
                 // the scales, or the rows of V that are looked through below (complete by now: the scores waited for them)
                 if ((kEight || cut) && !warp_wait(kEight ? &k_full[buf] : &v_full[buf], (pos / S::kVBufs) & 1)) { failed = true; break; }
-                // 32 scores of this row; the keys that it sees, as bits (cut)
+                // 32 scores of this row (8-bit: times the factors' product, each of which may be as far from 1 as the other makes up for); the keys that it
+                // sees, as bits (cut)
                 auto scores = [&](int c, float (&x)[32]) {
                     uint32_t r[32];
                     tmem_ld_x32(s_col + c, r);
@@ -506,7 +507,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                         for (int k = 0; k < 32; k += 4) {
                             const float4 ks = *reinterpret_cast<const float4*>(sc + c + k);
-                            x[k] *= ks.x; x[k + 1] *= ks.y; x[k + 2] *= ks.z; x[k + 3] *= ks.w;
+                            x[k] *= ks.x * mul; x[k + 1] *= ks.y * mul; x[k + 2] *= ks.z * mul; x[k + 3] *= ks.w * mul;
                         }
                     }
                 };
@@ -524,8 +525,10 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     for (int c = 0; c < S::kHalf; c += 32) {
                         float (&x)[32] = kept[c / 32];
                         scores(c, x);
+                        if constexpr (!kEight) {
 #pragma unroll
-                        for (int k = 0; k < 32; ++k) x[k] *= mul;
+                            for (int k = 0; k < 32; ++k) x[k] *= mul;
+                        }
                         if (cut) {
                             const uint32_t v = seen(c);
 #pragma unroll

@@ -233,3 +233,16 @@ def test_queries_at_the_ends_of_bf16(form, Hq, T, power):
     q = ((torch.rand((2, Hq, T, 64), generator=g, device="cuda") * 3.9 - 1.95) * 2.0 ** power).to(BF)
     sees = None if T == 1 else torch.ones((2, T, T), dtype=torch.bool, device="cuda").tril()
     assert_close(q, cache, lens_of([140, 77]), sees, (2.0 if power > 0 else 0.125) * 2.0 ** -power)
+
+
+@pytest.mark.parametrize("form", [I8, E4])
+@pytest.mark.parametrize("Hq,T", [(4, 1), (32, 4)])
+@pytest.mark.parametrize("power", [110, 119, -90])
+def test_keys_of_any_size(form, Hq, T, power):
+    """Rows of K between the ends of what kv_append keeps; only their products with the scale are ordinary numbers."""
+    g = ref.seeded(69)
+    k, v = (torch.randn((2, 2, 150, 64), generator=g, device="cuda") for _ in range(2))
+    cache = rows_cache(k * 2.0 ** power, v, form)
+    q = ref.normal(g, (2, Hq, T, 64), BF)
+    sees = None if T == 1 else torch.ones((2, T, T), dtype=torch.bool, device="cuda").tril()
+    assert_close(q, cache, lens_of([140, 77]), sees, 0.125 * 2.0 ** -power)
