@@ -399,9 +399,9 @@ int forge_kv_read(const forge_kv_cache* cache, void* k_out, void* v_out, int dty
  * smaller than the largest such part of that token; FORGE_KV_F16: a weight is, where it is more than 2^30 smaller than the token's largest.
  *
  * workspace: at least forge_attn_kv_workspace_bytes(B, Hq, Hkv, T, D) bytes, 16-byte aligned; T = 1 for the single token.  Its
- * arrival counters (the first max(256 KiB, 4 B Hkv ceil(G / min(G, floor(128 / T)))) bytes, G = Hq / Hkv) must be ZERO when a call
- * starts and are zero when it has completed: clear a new workspace once with forge_attn_kv_workspace_init; every shape with
- * up to 65536 counters can use it then.  After a call that ended in FORGE_ERR_TIMEOUT clear it again.  Two calls that may overlap on the GPU must not share it.
+ * arrival counters (the first 256 KiB) must be ZERO when a call starts and are zero when it has completed: clear a new workspace once with
+ * forge_attn_kv_workspace_init; calls of any shapes that it is large enough for can use it then, one after the other.  After a call that ended
+ * in FORGE_ERR_TIMEOUT clear it again.  Two calls that may overlap on the GPU must not share it.
  * The same inputs give the same bits, call after call (on GPUs with the same number of SMs).
  */
 size_t forge_attn_kv_workspace_bytes(int B, int Hq, int Hkv, int T, int D);

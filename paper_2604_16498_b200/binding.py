@@ -644,7 +644,8 @@ def _kv_workspace(workspace, cache, Hq, T, device):
 
 def attn_decode_kv(q, cache, lens, scale=None, out=None, workspace=None):
     """forge_attn_decode_kv: q [B,Hq,D] (bf16 or fp16) over the first lens[b] rows of a KVCache.  A workspace passed in must have
-    been cleared once (attn_kv_workspace_init); without one, a fresh cleared workspace is allocated."""
+    been cleared once (attn_kv_workspace_init) and may serve calls of any shapes, one after the other; without one, a fresh cleared
+    workspace is allocated."""
     if _host_calls is not None:
         st = _host_calls.decode_kv(cache.address, cache.device, q, lens, scale, out, workspace)
         if st >= 0:

@@ -17,9 +17,11 @@ RowSplit split_rows(int G, int T) {
     s.tiles = (G + s.heads - 1) / s.heads;
     return s;
 }
+// What a workspace has for counters: kKvCounterBytes, and for more (sequence, KV head, row tile) items than that has counters four bytes for each, which
+// nothing uses any more (workspaces keep the sizes that they had when each item had a counter of its own).
 size_t counter_bytes(size_t items) {
-    const size_t n = items > kKvMinCounters ? items : kKvMinCounters;
-    return (n * sizeof(unsigned int) + 255) & ~(size_t)255;
+    const size_t n = items * sizeof(unsigned int);
+    return ((n > kKvCounterBytes ? n : kKvCounterBytes) + 255) & ~(size_t)255;
 }
 
 // Floats of what a CTA leaves of an item: O, m and l of the rows that its kernel works on.
@@ -60,7 +62,7 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     a.q_f16 = dtype == FORGE_DTYPE_F16;
     a.scale_log2 = scale * 1.4426950408889634f;
     a.counters = static_cast<unsigned int*>(workspace);
-    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + counter_bytes((size_t)items));
+    a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKvCounterBytes);
     a.status = device_status_word();
     const int sms = sm_count();
     if (!a.status || sms <= 0) return FORGE_ERR_CUDA;

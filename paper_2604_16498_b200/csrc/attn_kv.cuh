@@ -23,7 +23,10 @@ namespace forge {
 
 constexpr int kKvMaxCtas = 160;         // what the workspace has room for
 constexpr int kKvMaxTokens = 64;
-constexpr size_t kKvMinCounters = 65536;
+// The workspace: arrival counters, one for each part of an item that several CTAs share (that of the item's first part is used), then the parts.  The
+// counters' place does not depend on the shape, so that calls of any shapes leave each other's at zero.
+constexpr size_t kKvCounterBytes = 65536 * sizeof(unsigned int);
+static_assert(kKvMaxCtas * 2 * sizeof(unsigned int) <= kKvCounterBytes, "a counter for each part");
 
 struct KvAttnArgs {
     const void* q;

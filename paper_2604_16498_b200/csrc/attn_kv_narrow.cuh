@@ -784,8 +784,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         const Left left = cuts[warp];
         cut_last[warp] = 0;
         if (left.blocks > 0) {
-            const int ctas = shares.of(left.start + left.blocks - 1) - shares.of(left.start) + 1;
-            unsigned int* counter = a.counters + left.b * a.Hkv + left.kvh;
+            const int cta0 = shares.of(left.start), ctas = shares.of(left.start + left.blocks - 1) - cta0 + 1;
+            unsigned int* counter = a.counters + cta0 * 2 + (left.start > shares.first(cta0) ? 1 : 0);  // that of its first part
             unsigned int before;
             asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(counter) : "memory");
             if (before + 1 == (unsigned)ctas) {

@@ -110,7 +110,7 @@ struct RowsPieces {
 };
 // Piece number idx.
 struct RowsPiece {
-    int b, kvh, rt, item;          // item: number of the (sequence, KV head, row tile)
+    int b, kvh, rt;
     int first, tiles;              // its steps
     int start, of;                 // the item's pieces: number of the first, and how many
     int past, rows;
@@ -136,7 +136,6 @@ __device__ __forceinline__ RowsPiece rows_piece(const KvAttnArgs& a, const RowsP
             const int first = (before + __shfl_sync(0xffffffffu, incl, src) - p.of) * per, in = at - first, item = in / p.of;
             p.kvh = item / a.row_tiles;
             p.rt = item - p.kvh * a.row_tiles;
-            p.item = p.b * per + item;
             p.start = first + item * p.of;  // (of items with several)
             p.first = (in - item * p.of) * ps.C;
             p.tiles = min(ps.C, __shfl_sync(0xffffffffu, tiles, src) - p.first);
@@ -173,7 +172,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     __shared__ uint64_t q_full, q_empty, q_ready, s_full[2], p_ready[2][2], pv_done[2];  // p_ready: [step % 2][group]
     __shared__ uint32_t tmem_slot;
     // items that the CTA had a piece of several of; whether it was the last to arrive
-    struct Cut { int item, start, of, b, kvh, rt; };
+    struct Cut { int start, of, b, kvh, rt; };
     __shared__ Cut cuts[2];
     __shared__ int cut_last[2];
     // halves of rows of V with elements that are not finite numbers, which some of the tokens see; pieces count in turns (see where they are cleared)
@@ -727,7 +726,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             tc_fence_before_sync();
             rows_sync();  // the parts are written; odd_keys and O have been read
             if (threadIdx.x == 0 && !whole)
-                cuts[idx / ctas] = {p.item, p.start, p.of, p.b, p.kvh, p.rt};  // at most two of them: they come first, and are no more than twice the CTAs
+                cuts[idx / ctas] = {p.start, p.of, p.b, p.kvh, p.rt};  // at most two of them: they come first, and are no more than twice the CTAs
         }
 
         // ---- items that other CTAs have parts of: the CTA that arrives last merges all of them
@@ -738,9 +737,9 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
             cut_last[e] = 0;
             if (cut.of > 0) {
                 unsigned int before;
-                asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.counters + cut.item) : "memory");
+                asm volatile("atom.add.acq_rel.gpu.global.u32 %0, [%1], 1;" : "=r"(before) : "l"(a.counters + cut.start) : "memory");
                 if (before + 1 == (unsigned)cut.of) {
-                    a.counters[cut.item] = 0;  // as the next call expects it
+                    a.counters[cut.start] = 0;  // as the next call expects it
                     cut_last[e] = 1;
                 }
             }

@@ -246,3 +246,24 @@ def test_keys_of_any_size(form, Hq, T, power):
     q = ref.normal(g, (2, Hq, T, 64), BF)
     sees = None if T == 1 else torch.ones((2, T, T), dtype=torch.bool, device="cuda").tril()
     assert_close(q, cache, lens_of([140, 77]), sees, 0.125 * 2.0 ** -power)
+
+
+@pytest.mark.parametrize("G,T", [(8, 1), (1, 9)])
+def test_a_shape_of_many_items_shares_a_workspace(G, T):
+    """More (sequence, KV head) pairs than 65536 in one call, few in the next, over the same workspace."""
+    g = ref.seeded(70)
+    B, Hkv, D, Smax = 2150, 32, 64, 160
+    big = ref.make_cache(g, B, Hkv, Smax, D, I8, binding)
+    qb, nb = ref.normal(g, (B, Hkv * G, T, D), BF), lens_of([90 + (7 * b) % (Smax - T - 89) for b in range(B)])
+    small = ref.make_cache(g, 1, 1, 5000, D, I8, binding)
+    qs, ns = ref.normal(g, (1, G, T, D), BF), lens_of([4900])
+    ws = torch.empty(binding.attn_kv_workspace_bytes(B, Hkv * G, Hkv, T, D), dtype=torch.uint8, device="cuda")
+    binding.attn_kv_workspace_init(ws)
+    first = [run_tree(qb, big, nb, workspace=ws), run_tree(qs, small, ns, workspace=ws)]
+    for _ in range(3):
+        for c, f in (((qb, big, nb), first[0]), ((qs, small, ns), first[1])):
+            out = torch.full_like(f, float("nan"))
+            run_tree(*c, out=out, workspace=ws)
+            assert torch.equal(out, f)
+    fresh = run_tree(qb, big, nb)
+    assert torch.equal(fresh, first[0])
