@@ -383,7 +383,7 @@ int forge_kv_read(const forge_kv_cache* cache, void* k_out, void* v_out, int dty
  * Attention of one token per sequence over a cache of any format (the operator of forge_attn_decode_splitkv):
  *     out[b,h,:] = sum_j softmax_j(scale * q[b,h,:].k[b,h/G,j,:]) v[b,h/G,j,:]   over rows j < lens[b]
  * q, out: [B, Hq, D] of `dtype` FORGE_DTYPE_BF16 or _F16 (that of a 16-bit cache); lens clamped to 0 .. Smax; a sequence
- * without rows gives zeros; rows at and beyond lens[b] may hold anything.  Any finite scale.  Hq / Hkv: any whole number.
+ * without rows gives zeros; rows at and beyond lens[b] may hold anything.  Any scale up to 2^127.  Hq / Hkv: any whole number.
  * out may not overlap q or the cache.
  *
  * forge_attn_tree: T tokens per sequence (1 .. 64) whose own rows are in the cache behind the lens[b] rows of their common

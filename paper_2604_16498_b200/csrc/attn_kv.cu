@@ -36,7 +36,8 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lens) & 3u)) return FORGE_ERR_INVALID_ARG;
     if (tree && ((reinterpret_cast<uintptr_t>(tree) & 7u) || (tree_B != 1 && tree_B != cache->B))) return FORGE_ERR_INVALID_ARG;
     if (!workspace || !aligned16(workspace)) return FORGE_ERR_INVALID_ARG;
-    if (T > kKvMaxTokens || Hq > 65535 || !(scale - scale == 0.f)) return FORGE_ERR_UNSUPPORTED;
+    const float scale_log2 = scale * 1.4426950408889634f;
+    if (T > kKvMaxTokens || Hq > 65535 || !(scale_log2 - scale_log2 == 0.f)) return FORGE_ERR_UNSUPPORTED;
     KvAttnArgs a = {};
     if ((st = check_strides(q_strides, Hq, T, cache->D, &a.qs)) != FORGE_OK) return st;
     if ((st = check_strides(out_strides, Hq, T, cache->D, &a.os)) != FORGE_OK) return st;
@@ -60,7 +61,7 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     a.tile_rows = rs.heads * T;
     a.tile_stride = (a.tile_rows + 31) / 32 * 32;
     a.q_f16 = dtype == FORGE_DTYPE_F16;
-    a.scale_log2 = scale * 1.4426950408889634f;
+    a.scale_log2 = scale_log2;
     a.counters = static_cast<unsigned int*>(workspace);
     a.parts = reinterpret_cast<float*>(static_cast<char*>(workspace) + kKvCounterBytes);
     a.status = device_status_word();

@@ -238,3 +238,10 @@ def test_tensors_of_another_device_are_refused(monkeypatch):
     binding._on_current(On(1), None, On(1))
     with pytest.raises(ValueError, match="cuda:0"):
         binding._on_current(On(1), None, On(0))
+
+
+def test_scales_that_the_exponentials_base_takes_out_of_range_are_refused(lib):
+    """Scores are kept in powers of two: scale * log2(e) has to be a finite fp32 number."""
+    for scale in (2.4e38, -3e38, 3.4028234e38):
+        assert lib.forge_attn_decode_kv(cache(), P, P, 0, 8, P, scale, P, 1 << 30, None) == binding.ERR_UNSUPPORTED
+        assert lib.forge_attn_tree(cache(), P, P, 0, 8, 5, None, None, P, None, 1, scale, P, 1 << 30, None) == binding.ERR_UNSUPPORTED
