@@ -175,7 +175,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     struct Cut { int start, of, b, kvh, rt; };
     __shared__ Cut cuts[2];
     __shared__ int cut_last[2];
-    // halves of rows of V with elements that are not finite numbers, which some of the tokens see; pieces count in turns (see where they are cleared)
+    // halves of rows of V with elements that are not finite numbers, which some of the tokens see (twice the token's number, and which half); pieces count in turns (see where they are cleared)
     __shared__ int odd_keys[kMaxOdd], odd_count[2];
     __shared__ float q_mul[128];                  // 8-bit: what a row's scores are multiplied by
     __shared__ float4 group_state[2][128];        // m, l and the unit of O
@@ -648,7 +648,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             }
                             if (odd && !out) {
                                 const int i = atomicAdd(&odd_count[parts & 1], 1);
-                                if (i < kMaxOdd) odd_keys[i] = (key0 + key) * 2 + (row & 1);
+                                if (i < kMaxOdd) odd_keys[i] = (key0 + key - p.past) * 2 + (row & 1);
                             }
                         }
                         fence_proxy_async_smem();
@@ -699,9 +699,9 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         }
                     }
                     for (int i = 0; i < odds; ++i) {
-                        const int key = odd_keys[i] >> 1;
-                        if ((odd_keys[i] & 1) != group || !(sees >> (key - p.past) & 1ull)) continue;
-                        const uint16_t* v = static_cast<const uint16_t*>(a.v) + ((int64_t)(p.b * a.Hkv + p.kvh) * a.Smax + key) * a.D + d;
+                        const int u = odd_keys[i] >> 1;
+                        if ((odd_keys[i] & 1) != group || !(sees >> u & 1ull)) continue;
+                        const uint16_t* v = static_cast<const uint16_t*>(a.v) + ((int64_t)(p.b * a.Hkv + p.kvh) * a.Smax + p.past + u) * a.D + d;
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
                             if (d + k >= a.D) continue;

@@ -267,3 +267,17 @@ def test_a_shape_of_many_items_shares_a_workspace(G, T):
             assert torch.equal(out, f)
     fresh = run_tree(qb, big, nb)
     assert torch.equal(fresh, first[0])
+
+
+def test_not_a_number_behind_more_rows_than_31_bits_count_twice():
+    """2^30 rows of 16 bits; a drafted row behind them is no number, and another is infinite."""
+    past, T, D = (1 << 30) + 5, 4, 8
+    k, v = (torch.zeros((1, 1, past + 8, D), dtype=BF, device="cuda") for _ in range(2))
+    v[0, 0, past + 1, 3] = float("nan")
+    v[0, 0, past + 2, 7] = -float("inf")
+    sees = torch.eye(T, dtype=torch.bool, device="cuda")
+    sees[:, 0] = True
+    out = run_tree(torch.zeros((1, 4, T, D), dtype=BF, device="cuda"), binding.KVCache(k, v), lens_of([past]), ref.tree_bits(sees)[None])
+    want = torch.zeros((T, D), device="cuda")
+    want[1, 3], want[2, 7] = float("nan"), -float("inf")
+    torch.testing.assert_close(out[0].float(), want.expand(4, T, D), rtol=0, atol=0, equal_nan=True)
