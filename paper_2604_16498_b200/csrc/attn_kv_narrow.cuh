@@ -484,9 +484,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
             }
             // ---- probabilities, and P^T as the B operand: keys 2c, 2c + 1 (and + 8) of row g
             const float sub[2] = {ref[0] == -INFINITY ? 0.f : ref[0], ref[1] == -INFINITY ? 0.f : ref[1]};
-            // P is rounded once to the products' type; where the output's type is no wider that would be as much as its own rounding, and what
-            // the rounding left is multiplied too (pl): fp16 outputs are off by 2.1e-4 of their size, the rounding alone, instead of 2.9e-4, for 3 % of the time.
-            const bool rest = !kEight || out_f16;
+            // P is rounded once to the products' type, and what that leaves is multiplied too (pl), so that outputs are off by their own rounding alone: fp16 ones
+            // by 2.1e-4 of their size instead of 2.9e-4, bf16 ones of 8-bit rows by 1.67e-3 instead of 1.69e-3, for 1 to 3 % of the time.
             uint32_t pf[KG][2], pl[KG][2];
             float pr[KG][4];
 #pragma unroll
@@ -532,12 +531,9 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                 for (int u = 0; u < 2; ++u) {
                     const uint32_t p16 = pack16<kF16>(pr[k][2 * u], pr[k][2 * u + 1]);
                     pf[k][u] = transpose8x8(p16);
-                    pl[k][u] = 0;
-                    if (rest) {
-                        const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&p16))
-                                                 : make_float2(__uint_as_float(p16 << 16), __uint_as_float(p16 & 0xffff0000u));
-                        pl[k][u] = transpose8x8(pack16<kF16>(pr[k][2 * u] - back.x, pr[k][2 * u + 1] - back.y));
-                    }
+                    const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&p16))
+                                             : make_float2(__uint_as_float(p16 << 16), __uint_as_float(p16 & 0xffff0000u));
+                    pl[k][u] = transpose8x8(pack16<kF16>(pr[k][2 * u] - back.x, pr[k][2 * u + 1] - back.y));
                 }
             }
             // ---- O^T += V^T P^T
@@ -553,7 +549,7 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                             value_codes<kE4m3>(vr[4 * k][w4], vr[4 * k + 1][w4], hi, f[0], f[1]);
                             value_codes<kE4m3>(vr[4 * k + 2][w4], vr[4 * k + 3][w4], hi, f[2], f[3]);
                             mma_16816<true>(st.o[2 * w4 + hi], f, pf[k][0], pf[k][1]);
-                            if (rest) mma_16816<true>(st.o[2 * w4 + hi], f, pl[k][0], pl[k][1]);
+                            mma_16816<true>(st.o[2 * w4 + hi], f, pl[k][0], pl[k][1]);
                         }
                     }
             } else {

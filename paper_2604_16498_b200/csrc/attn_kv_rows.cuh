@@ -211,11 +211,6 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     const int ctas = gridDim.x;
     const RowsPieces<S::kStep> pieces(a, ctas, lane);
     bool failed = false;
-    // P is rounded once to the products' type; where the output's type is no wider that would be as much as its own rounding, and what the rounding
-    // left is multiplied too, from the columns of S that P leaves free.  Errors against 64 bits, without
-    // and with it: 4 x 32/8 x 64 tokens of bf16 2.3e-3 and 1.66e-3, 8 x 28/4 x 16 fp16 tokens over int8 rows 2.9e-4 and 2.1e-4; times
-    // 29.0 and 30.2 us, 24.2 and 25.1.
-    const bool rest = !kEight || a.q_f16;
 
     if (warp == 8) {
         // ------------------------------------------------------------------ copies
@@ -311,12 +306,10 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         for (int k = 0; k < S::kHalf / 16; ++k)
                             mma_ts(tmem + kColO + h * DW, tmem + kColS + (pos & 1) * S::kStep + h * S::kHalf + k * 8,
                                    vd + (h * (S::kHalf / 16) + k) * (2048 >> 4), idesc_o, g > 0 || k != 0);
-                        if (rest) {
 #pragma unroll
-                            for (int k = 0; k < S::kHalf / 16; ++k)
-                                mma_ts(tmem + kColO + h * DW, tmem + kColS + (pos & 1) * S::kStep + h * S::kHalf + S::kHalf / 2 + k * 8,
-                                       vd + (h * (S::kHalf / 16) + k) * (2048 >> 4), idesc_o, 1);
-                        }
+                        for (int k = 0; k < S::kHalf / 16; ++k)  // what rounding P left
+                            mma_ts(tmem + kColO + h * DW, tmem + kColS + (pos & 1) * S::kStep + h * S::kHalf + S::kHalf / 2 + k * 8,
+                                   vd + (h * (S::kHalf / 16) + k) * (2048 >> 4), idesc_o, 1);
                         mma_commit(&pv_done[h]);
                     }
                     if (failed) break;
@@ -610,15 +603,16 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                         for (int k = 0; k < 16; ++k) packed[k] = pack16<kF16>(x[2 * k], x[2 * k + 1]);
                         tmem_st_x16(s_col + c / 2, packed);
-                        if (rest) {
+                        // P is rounded once to the products' type, and what that leaves is multiplied too, from the columns of S that P leaves free, so that outputs are
+                        // off by their own rounding alone.  Errors against 64 bits, without and with it: 4 x 32/8 x 64 tokens of bf16 2.3e-3 and 1.66e-3, 8 x 28/4 x 16 fp16
+                        // tokens over int8 rows 2.9e-4 and 2.1e-4; times 29.0 and 30.2 us, 24.2 and 25.1.
 #pragma unroll
-                            for (int k = 0; k < 16; ++k) {
-                                const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&packed[k]))
-                                                         : make_float2(__uint_as_float(packed[k] << 16), __uint_as_float(packed[k] & 0xffff0000u));
-                                packed[k] = pack16<kF16>(x[2 * k] - back.x, x[2 * k + 1] - back.y);
-                            }
-                            tmem_st_x16(s_col + S::kHalf / 2 + c / 2, packed);
+                        for (int k = 0; k < 16; ++k) {
+                            const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&packed[k]))
+                                                     : make_float2(__uint_as_float(packed[k] << 16), __uint_as_float(packed[k] & 0xffff0000u));
+                            packed[k] = pack16<kF16>(x[2 * k] - back.x, x[2 * k + 1] - back.y);
                         }
+                        tmem_st_x16(s_col + S::kHalf / 2 + c / 2, packed);
                     }
                 }
                 if constexpr (!kEight) {

@@ -50,9 +50,9 @@ def test_not_a_number_in_every_item_of_a_long_run(dtype, form, B, Hq, Hkv, T):
 # ------------------------------------------------------------------------------------------------------- as close as it is said to be
 def definition(q, cache, past, sees=None, scale=None):
     """q [B,Hq,T,D], the rows as in kv_reference.attention -> (out in 64 bits, bound), both from the rows that a token sees alone.
-    Weights (softmax, times the row's scale with 8-bit rows) are rounded to the operands' type, twice (what the first leaves is multiplied
-    too) where the output is no narrower than them: 2^-8 or 2^-11, or their squares; in fp16 to 2^-24 at least, where the token's largest
-    has come to 2^5 or more: 2^-30 of it.  The output is rounded once.  Scores and sums as in kv_reference.attention."""
+    Weights (softmax, times the row's scale with 8-bit rows) are rounded to the operands' type, and what that leaves once more: 2^-8 or
+    2^-11, squared; in fp16 to half of 2^-24 at least, where the token's largest has come to 2^5 or more: 2^-30 of it.  The output is
+    rounded once.  Scores and sums as in kv_reference.attention."""
     B, Hq, T, D = q.shape
     k, v = ref.decode_values(cache.k, cache.k_scale), ref.decode_values(cache.v, cache.v_scale)
     Smax, Hkv = k.shape[2], k.shape[1]
@@ -61,7 +61,7 @@ def definition(q, cache, past, sees=None, scale=None):
     past = past.clamp(0, Smax)
     smallest = 2.0 ** -25 if q.dtype == HF else 2.0 ** -134  # half of the type's smallest number
     operand = torch.float16 if eight else q.dtype
-    u = ref.HALF[operand] if eight and q.dtype == BF else ref.HALF[operand] ** 2
+    u = ref.HALF[operand] ** 2
     top = cache.v_scale.double().abs() * ref.TOP[cache.v.dtype] if eight else v.abs().amax(-1)  # of a row's elements
     out, bound = torch.zeros(q.shape, dtype=torch.float64, device="cuda"), torch.zeros(q.shape, dtype=torch.float64, device="cuda")
     for b in range(B):
