@@ -26,7 +26,7 @@ namespace {
 // Steps that joining the pieces of an item is worth.  8 x 32/8 heads x 16 tokens over int8 rows: 400 rows of the past take 16.3 us cut and 15.7
 // whole (4 steps more), 600 take 17.6 and 19.0 (7 more); 1 x 32/8 x 5 tokens over 16-bit rows: 600 take 11.7 and 11.3 (4 more), 800 take
 // 13.7 and 14.8 (6 more).
-constexpr int kRowsMerge = 4;
+constexpr int kRowsMerge = 3;
 // p reaches 2^8 above what the reference m stands for.  16-bit rows: that is 2^14.  8-bit rows: 1, and m is a whole number.
 constexpr float kRowsAbove = 8.f;
 
