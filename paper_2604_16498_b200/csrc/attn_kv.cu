@@ -1,4 +1,4 @@
-// C entry points of the attention over a KV cache of any format.  The kernel is in attn_kv.cuh.
+// C entry points of the attention over a KV cache of any format.  The kernels are in attn_kv_narrow.cuh and attn_kv_rows.cuh.
 #include "attn_kv.cuh"
 
 namespace forge {

@@ -166,7 +166,7 @@ struct KvSchedule {
         N = kv_sum(total) * a.Hkv;
         most = kv_max(most);
         // Adding one part to a merge takes as long as a tile: n + most / n is smallest at sqrt(most).  8/1 heads of 128, one sequence, with 8 tiles at
-        // least and with this: 32,000 int8 rows 24.6 and 16.5 us, 8000 11.2 and 11.3; 8000 bf16 rows 14.8 and 10.8.
+        // least and with this: 32,000 int8 rows 24.8 and 16.7 us, 8000 11.4 and 11.3; 8000 bf16 rows 14.7 and 10.8.
         const int least = max(LEAST, (int)__fsqrt_rn((float)most));
         W = min((int)gridDim.x, (N + least - 1) / least);
         const int items = a.B * a.Hkv;

@@ -1,4 +1,4 @@
-// Attention over a KV cache, format FORGE_KV_BF16.  The kernel is in attn_kv.cuh.
+// Attention over a KV cache, format FORGE_KV_BF16.  The kernels are in attn_kv_narrow.cuh and attn_kv_rows.cuh.
 #include "attn_kv.cuh"
 
 namespace forge {

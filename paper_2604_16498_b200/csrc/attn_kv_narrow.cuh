@@ -8,24 +8,24 @@
 // registers.  A CTA's share of the call's blocks is cut into eight runs, one per warp, and no warp waits for another until all have
 // finished theirs: only then, once per CTA, are the warps' results merged (through the rings, which are free by then).  The running
 // reference of a row is raised only where a score exceeds it by 2^8, so that an ordinary block needs no exchange between
-// lanes but one vote.
+// lanes but a vote (8-bit rows: two, the other on the unit of P).
 //
 // What bounds it: the copies' latency times the 128 KB of them that an SM has in flight while it streams, and before and after that some 5 us of
 // dependent steps (lengths, shares and queries; the warps' merge; the CTAs').  int8 rows, heads of 128: 16 x 32/8 x 1024 .. 4096 rows (87 MB)
-// 23.7 us, 1 x 32/8 x 32,768 e4m3 rows (69 MB) 23.1; 12/12 heads of 64, 40 x up to 1000 rows (34 MB) 19.2.  Twelve warps with smaller rings took
-// 31.9 us for the first of these when eight took 27.3; a warp that only copies would leave the others 168 registers of the 242 they use.
+// 24.8 us, 1 x 32/8 x 32,768 e4m3 rows (69 MB) 23.2; 12/12 heads of 64, 40 x up to 1000 rows (34 MB) 19.7; bf16 rows, the first of these (168 MB) 32.0.
+// Twelve warps with smaller rings took 31.9 us for the first when eight took 27.3; a warp that only copies would leave the others 168 registers of the 246 they use.
 #pragma once
 
 namespace forge {
 namespace {
 
 // What the instructions have room for.  With few rows this kernel is the faster one: 16 sequences of 32/8 heads of 128, 8 rows (4 heads x 2 tokens), 4000
-// cached rows: int8 29.3 us, on the other kernel 77.8; bf16 47.3 and 48.3, 1000 rows 11.2 and 16.2.
+// cached rows: int8 31.7 us, on the other kernel 94; bf16 47.9 and 52.0, 1000 bf16 rows 14.1 and 18.8.
 constexpr int kNarrowRows = 8;
 constexpr int kNarrowWarps = 8;
 constexpr int kNarrowThreads = kNarrowWarps * 32;
-// Blocks that joining the parts of several CTAs is worth.  int8 rows of 128, 32/8 heads: 16 x 1000 rows take 15.8 us in even shares and 11.8
-// as whole items (5 blocks more than the share), 8 x 1000 rows 12.7 and 11.7 (19 more), 2 x 1000 rows 8.4 and 11.5 (25 more).
+// Blocks that joining the parts of several CTAs is worth.  int8 rows of 128, 32/8 heads: 16 x 1000 rows take 16.8 us in even shares and 12.6
+// as whole items (5 blocks more than the share), 8 x 1000 rows 13.3 and 12.0 (19 more), 2 x 1000 rows 8.6 and 11.7 (25 more).
 constexpr int kNarrowMerge = 20;
 // The scales of a block of 32 keys, copied from the 16-byte boundary at or before the first: up to 3 others come first.
 constexpr int kScaleKeys = 36, kScaleBox = 256;
@@ -321,7 +321,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 1));
                 big = max(big, __shfl_xor_sync(0xffffffffu, big, 2));
                 const float top = a.q_f16 ? __half2float(__ushort_as_half((unsigned short)big)) : __uint_as_float(big << 16);
-                const int e = (int)(__float_as_uint(top) >> 23) - 127;  // the largest goes to [2^14, 2^15) (bf16's goes up to 2^127; one below 2^-96 stays smaller); rows of zeros or with infinities stay
+                // the largest goes to [2^14, 2^15) (bf16's goes up to 2^127; one below 2^-96 stays smaller); rows of zeros or with infinities stay
+                const int e = (int)(__float_as_uint(top) >> 23) - 127;
                 const int up = top == 0.f || e == 128 ? 0 : min(max(14 - e, -113), 110);
                 const float f = __int_as_float((127 + up) << 23);
                 q_mul = a.scale_log2 * __int_as_float((127 - up) << 23);

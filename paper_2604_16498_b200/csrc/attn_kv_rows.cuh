@@ -15,17 +15,17 @@
 // 8-bit rows stay codes in the products (exact in fp16; int8 elements come in the order 0 2 1 3 of each four, in Q and O too); their scales
 // multiply the scores and the probabilities.  Q comes by TMA, an item ahead: plain loads would wait behind the copies in flight.
 //
-// What bounds it: the chain of a step (scores, softmax of a row per thread, P into tensor memory, product with V; 2350 cycles for 128 keys where the
-// tensor cores need 1024), and some 8 us around the steps: start, first copies, the output and the merge of pieces.  4 x 32/8 heads x 64 tokens behind
-// 1024 .. 4096 16-bit rows take 28.6 us, 8 x 28/4 x 16 behind 600 .. 2400 int8 rows 23.6, 1 x 32/8 x 5 behind some 600 12.4.
+// What bounds it: the chain of a step (scores, softmax of a row per thread, P into tensor memory, product with V; 1.23 us for 128 keys of 16-bit rows,
+// where the tensor cores need 0.8, and 1.33 for 64 of 8-bit ones), and some 8 us around the steps: start, first copies, the output and the merge of pieces.
+// 4 x 32/8 heads x 64 tokens behind 1024 .. 4096 16-bit rows take 30.0 us, 8 x 28/4 x 16 behind 600 .. 2400 int8 rows 24.1, 1 x 32/8 x 5 behind some 600 12.9.
 #pragma once
 
 namespace forge {
 namespace {
 
-// Steps that joining the pieces of an item is worth.  8 x 32/8 heads x 16 tokens over int8 rows: 400 rows of the past take 16.3 us cut and 15.7
-// whole (4 steps more), 600 take 17.6 and 19.0 (7 more); 1 x 32/8 x 5 tokens over 16-bit rows: 600 take 11.7 and 11.3 (4 more), 800 take
-// 13.7 and 14.8 (6 more).
+// Steps that joining the pieces of an item is worth.  Whole and cut: 8 x 32/8 heads x 16 tokens over int8 rows, 400 rows of the past 17.4 and 17.1 us (3 steps
+// more), 480 18.6 and 17.1 (4 more); over 16-bit rows 4 x 32/8 x 64 tokens, 640 rows 16.1 and 17.8 (3 more), 1 x 32/8 x 5, 470 rows 11.5 and 11.2 (3 more),
+// 600 12.9 and 11.5 (4 more), 800 16.8 and 13.5 (6 more).
 constexpr int kRowsMerge = 3;
 // p reaches 2^8 above what the reference m stands for.  16-bit rows: that is 2^14.  8-bit rows: 1, and m is a whole number.
 constexpr float kRowsAbove = 8.f;
@@ -81,8 +81,7 @@ struct RowsPieces {
         }
         most = kv_max(most);
         // Adding one part to a merge takes as long as half a step: C + most / C / 2 is smallest at sqrt(most / 2).  16/1 heads of 128 over int8 rows of
-        // one sequence, with as many pieces as CTAs and with this: 1000 rows 17.8 and 14.8 us, 4000 42.1 and 20.3, 32,000 77.4 and 42.7 (13.8 and 18.6 for the
-        // first two since a part takes a third less).
+        // one sequence, with as many pieces as CTAs and with this: 1000 rows 16.5 and 14.9 us, 4000 36.9 and 21.7, 8000 63.2 and 27.2, 32,000 67.6 and 47.2.
         const int N = kv_sum(total) * per, low = max((N + ctas - 1) / ctas, (int)__fsqrt_rn(0.5f * most));
         C = a.B * per <= ctas && most <= low + kRowsMerge ? most : low;
         count(a, lane);
@@ -175,7 +174,8 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     struct Cut { int start, of, b, kvh, rt; };
     __shared__ Cut cuts[2];
     __shared__ int cut_last[2];
-    // halves of rows of V with elements that are not finite numbers, which some of the tokens see (twice the token's number, and which half); pieces count in turns (see where they are cleared)
+    // halves of rows of V with elements that are not finite numbers, which some of the tokens see (twice the token's number, and which half);
+    // pieces count in turns (see where they are cleared)
     __shared__ int odd_keys[kMaxOdd], odd_count[2];
     __shared__ float q_mul[128];                  // 8-bit: what a row's scores are multiplied by
     __shared__ float4 group_state[2][128];        // m, l and the unit of O
@@ -603,9 +603,9 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
 #pragma unroll
                         for (int k = 0; k < 16; ++k) packed[k] = pack16<kF16>(x[2 * k], x[2 * k + 1]);
                         tmem_st_x16(s_col + c / 2, packed);
-                        // P is rounded once to the products' type, and what that leaves is multiplied too, from the columns of S that P leaves free, so that outputs are
-                        // off by their own rounding alone.  Errors against 64 bits, without and with it: 4 x 32/8 x 64 tokens of bf16 2.3e-3 and 1.66e-3, 8 x 28/4 x 16 fp16
-                        // tokens over int8 rows 2.9e-4 and 2.1e-4; times 29.0 and 30.2 us, 24.2 and 25.1.
+                        // P is rounded once to the products' type, and what that leaves is multiplied too, from the columns of S that P leaves free, so that
+                        // outputs are off by their own rounding alone.  Errors against 64 bits, without and with it: 4 x 32/8 x 64 tokens of bf16 2.3e-3
+                        // and 1.66e-3, 8 x 28/4 x 16 fp16 tokens over int8 rows 2.9e-4 and 2.1e-4; times 29.0 and 30.2 us, 24.2 and 25.1.
 #pragma unroll
                         for (int k = 0; k < 16; ++k) {
                             const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&packed[k]))
