@@ -648,6 +648,9 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         fence_proxy_async_smem();
                     }
                 }
+                // The group's product of the step before, while the next one still waits for this P: a wait tells a phase from the next one only, and the tensor
+                // cores, which take the groups in turns, may be a step behind this group where the other one's P is late.
+                if (g > 0 && !warp_wait(&pv_done[group], (steps - 2) & 1)) { failed = true; break; }
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
