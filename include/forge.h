@@ -395,8 +395,8 @@ int forge_kv_read(const forge_kv_cache* cache, void* k_out, void* v_out, int dty
  * beyond Smax are not there.  q, out: [B, Hq, T, D] views.  A row of the cache that a token does not see has no part in
  * its output, whatever the row holds.
  *
- * Scores, sums and outputs are kept in fp32; outputs are rounded once, and weights on their way to the product with V to within 2^-16 of themselves
- * (FORGE_KV_BF16) or 2^-22 (the other formats).
+ * Scores, sums and outputs are kept in fp32; outputs are rounded once, and weights on their way to the product with V to within 2^-15 of themselves
+ * (FORGE_KV_BF16), 2^-21 (FORGE_KV_F16) or 2^-22 (8-bit formats).
  * Rows may be of any sizes.  8-bit formats: what a row adds to a token's output (its weight times its scale) is lost where it is more than 2^30
  * smaller than the largest such part of that token; FORGE_KV_F16: a weight is, where it is more than 2^30 smaller than the token's largest.
  *

@@ -129,6 +129,37 @@ __device__ __forceinline__ float kv_raise_unit(float& unit_inv, float most) {
     return kv_pow2(unit - now);
 }
 
+// Two elements of P as the operand of the product with V, and what that leaves of them, for a second product.  16-bit rows may hold infinities, and times
+// a rest of zero or below they would become NaN: P is rounded towards zero there, and the rest is above zero where P is (bf16: 2^-23 of P at
+// least; fp16: its smallest number).
+template <bool F16, bool INFINITIES>
+__device__ __forceinline__ uint32_t kv_operand(float x, float y) {
+    if constexpr (!INFINITIES) {
+        return pack16<F16>(x, y);
+    } else if constexpr (F16) {
+        uint32_t p;
+        asm("cvt.rz.f16x2.f32 %0, %1, %2;" : "=r"(p) : "f"(y), "f"(x));
+        return p;
+    } else {
+        return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
+    }
+}
+template <bool F16, bool INFINITIES>
+__device__ __forceinline__ uint32_t kv_rest(float x, float y, uint32_t p) {
+    float2 was;
+    if constexpr (F16) was = __half22float2(*reinterpret_cast<const __half2*>(&p));
+    else was = make_float2(__uint_as_float(p << 16), __uint_as_float(p & 0xffff0000u));
+    if constexpr (!INFINITIES) {
+        return pack16<F16>(x - was.x, y - was.y);
+    } else if constexpr (F16) {
+        constexpr float kLeast = 5.9604644775390625e-8f;  // 2^-24
+        return pack16<true>(fmaxf(x - was.x, fminf(x, kLeast)), fmaxf(y - was.y, fminf(y, kLeast)));
+    } else {
+        constexpr float kMore = 1.00000011920928955078125f;  // 1 + 2^-23
+        return pack16<false>(fmaf(x, kMore, -was.x), fmaf(y, kMore, -was.y));
+    }
+}
+
 // n / d for quotients up to a few thousand: the float quotient is off by one at most.
 __device__ __forceinline__ int kv_small_quotient(int n, int d) {
     const int q = (int)__fdividef((float)n, (float)d), rest = n - q * d;

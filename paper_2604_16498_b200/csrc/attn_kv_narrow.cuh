@@ -530,11 +530,9 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
             for (int k = 0; k < KG; ++k) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const uint32_t p16 = pack16<kF16>(pr[k][2 * u], pr[k][2 * u + 1]);
+                    const uint32_t p16 = kv_operand<kF16, !kEight>(pr[k][2 * u], pr[k][2 * u + 1]);
                     pf[k][u] = transpose8x8(p16);
-                    const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&p16))
-                                             : make_float2(__uint_as_float(p16 << 16), __uint_as_float(p16 & 0xffff0000u));
-                    pl[k][u] = transpose8x8(pack16<kF16>(pr[k][2 * u] - back.x, pr[k][2 * u + 1] - back.y));
+                    pl[k][u] = transpose8x8(kv_rest<kF16, !kEight>(pr[k][2 * u], pr[k][2 * u + 1], p16));
                 }
             }
             // ---- O^T += V^T P^T

@@ -599,19 +599,15 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                             }
                             l += (add[0] + add[1]) + (add[2] + add[3]);
                         }
+                        // What rounding P to the products' type leaves is multiplied too, from the columns of S that P leaves free, so that outputs are off by
+                        // their own rounding alone.  Errors against 64 bits, without and with it: 4 x 32/8 x 64 tokens of bf16 2.3e-3 and 1.66e-3,
+                        // 8 x 28/4 x 16 fp16 tokens over int8 rows 2.9e-4 and 2.1e-4; times 29.0 and 30.2 us, 24.2 and 25.1.
                         uint32_t packed[16];
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) packed[k] = pack16<kF16>(x[2 * k], x[2 * k + 1]);
+                        for (int k = 0; k < 16; ++k) packed[k] = kv_operand<kF16, !kEight>(x[2 * k], x[2 * k + 1]);
                         tmem_st_x16(s_col + c / 2, packed);
-                        // P is rounded once to the products' type, and what that leaves is multiplied too, from the columns of S that P leaves free, so that
-                        // outputs are off by their own rounding alone.  Errors against 64 bits, without and with it: 4 x 32/8 x 64 tokens of bf16 2.3e-3
-                        // and 1.66e-3, 8 x 28/4 x 16 fp16 tokens over int8 rows 2.9e-4 and 2.1e-4; times 29.0 and 30.2 us, 24.2 and 25.1.
 #pragma unroll
-                        for (int k = 0; k < 16; ++k) {
-                            const float2 back = kF16 ? __half22float2(*reinterpret_cast<const __half2*>(&packed[k]))
-                                                     : make_float2(__uint_as_float(packed[k] << 16), __uint_as_float(packed[k] & 0xffff0000u));
-                            packed[k] = pack16<kF16>(x[2 * k] - back.x, x[2 * k + 1] - back.y);
-                        }
+                        for (int k = 0; k < 16; ++k) packed[k] = kv_rest<kF16, !kEight>(x[2 * k], x[2 * k + 1], packed[k]);
                         tmem_st_x16(s_col + S::kHalf / 2 + c / 2, packed);
                     }
                 }

@@ -50,9 +50,10 @@ def test_not_a_number_in_every_item_of_a_long_run(dtype, form, B, Hq, Hkv, T):
 # ------------------------------------------------------------------------------------------------------- as close as it is said to be
 def definition(q, cache, past, sees=None, scale=None):
     """q [B,Hq,T,D], the rows as in kv_reference.attention -> (out in 64 bits, bound), both from the rows that a token sees alone.
-    Weights (softmax, times the row's scale with 8-bit rows) are rounded to the operands' type, and what that leaves once more: 2^-8 or
-    2^-11, squared; in fp16 to half of 2^-24 at least, where the token's largest has come to 2^5 or more: 2^-30 of it.  The output is
-    rounded once.  Scores and sums as in kv_reference.attention."""
+    Weights (softmax, times the row's scale with 8-bit rows) are rounded to the operands' type, and what that leaves once more: off by half a
+    step of half a step, 2^-11 squared for 8-bit rows; for 16-bit ones, whose weights are rounded towards zero first, by half a step of a
+    whole one, twice 2^-8 or 2^-11 squared.  In fp16 also by half of 2^-24, where the token's largest has come to 2^5 or more: 2^-30 of it;
+    with 16-bit rows by 2^-24, where it has come to 2^6: as much.  The output is rounded once.  Scores and sums as in kv_reference.attention."""
     B, Hq, T, D = q.shape
     k, v = ref.decode_values(cache.k, cache.k_scale), ref.decode_values(cache.v, cache.v_scale)
     Smax, Hkv = k.shape[2], k.shape[1]
@@ -61,7 +62,7 @@ def definition(q, cache, past, sees=None, scale=None):
     past = past.clamp(0, Smax)
     smallest = 2.0 ** -25 if q.dtype == HF else 2.0 ** -134  # half of the type's smallest number
     operand = torch.float16 if eight else q.dtype
-    u = ref.HALF[operand] ** 2
+    u = ref.HALF[operand] ** 2 * (1 if eight else 2)
     top = cache.v_scale.double().abs() * ref.TOP[cache.v.dtype] if eight else v.abs().amax(-1)  # of a row's elements
     out, bound = torch.zeros(q.shape, dtype=torch.float64, device="cuda"), torch.zeros(q.shape, dtype=torch.float64, device="cuda")
     for b in range(B):
@@ -306,3 +307,22 @@ def test_the_same_bits_whatever_ran_before(dtype, form):
         torch.sort(a[:64].flatten())
         for c, f in zip(cases, first):
             assert torch.equal(run_tree(*c), f)
+
+
+@pytest.mark.parametrize("dtype", [BF, HF])
+@pytest.mark.parametrize("Hq,T", [(4, 1), (4, 3), (16, 5), (8, 16)])
+@pytest.mark.parametrize("size", [0.0, 1.0])
+def test_an_infinity_that_all_see_is_one_in_the_output(dtype, Hq, T, size):
+    """Elements of V that are infinite, among the past rows: the output's element is infinite, the others are what they were.  With queries of
+    zeros all weights are one power of two."""
+    g = ref.seeded(71)
+    B, Hkv, D, Smax = 3, 2, 64, 420
+    cache = ref.make_cache(g, B, Hkv, Smax, D, dtype, binding)
+    q, n = ref.normal(g, (B, Hq, T, D), dtype, size), lens_of([400, 256, 33])
+    sees = None if T == 1 else torch.ones((B, T, T), dtype=torch.bool, device="cuda").tril()
+    want, bound = definition(q, cache, n, sees, 0.125)
+    cache.v[:, :, 5, 3], cache.v[:, :, 20, 7] = float("inf"), -float("inf")
+    got = run_decode(q[:, :, 0].contiguous(), cache, n, scale=0.125)[:, :, None] if T == 1 else run_tree(q, cache, n, ref.tree_bits(sees), scale=0.125)
+    assert (got[..., 3] == float("inf")).all() and (got[..., 7] == -float("inf")).all()
+    got[..., 3], got[..., 7] = want[..., 3].to(dtype), want[..., 7].to(dtype)
+    ref.assert_within(got, want, bound)
