@@ -168,7 +168,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     __shared__ uint64_t load_full[kLoads], load_empty[kLoads], k_full[S::kKBufs], k_empty[S::kKBufs], v_full[S::kVBufs], v_empty[S::kVBufs];
     constexpr int kMergeSlots = 4;
     __shared__ uint64_t merge_full[kMergeSlots];
-    __shared__ uint64_t q_full, q_empty, q_ready, s_full[2], p_ready[2][2], pv_done[2];  // p_ready: [step % 2][group]
+    __shared__ uint64_t q_full, q_empty, q_ready, s_full[2], p_ready[2][2], pv_done[2][2];  // the last two: [step % 2][group]
     __shared__ uint32_t tmem_slot;
     // items that the CTA had a piece of several of; whether it was the last to arrive
     struct Cut { int start, of, b, kvh, rt; };
@@ -188,7 +188,10 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         mbar_init(&q_full, 1);
         for (int i = 0; i < kMergeSlots; ++i) mbar_init(&merge_full[i], 1);
         mbar_init(&q_empty, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_ready[i][0], 4); mbar_init(&p_ready[i][1], 4); mbar_init(&pv_done[i], 1); }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(&s_full[i], 1);
+            for (int h = 0; h < 2; ++h) { mbar_init(&p_ready[i][h], 4); mbar_init(&pv_done[i][h], 1); }
+        }
         mbar_init(&q_ready, 4);
         fence_mbar_init();
         prefetch_tmap(&tmap_q);
@@ -310,7 +313,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         for (int k = 0; k < S::kHalf / 16; ++k)  // what rounding P left
                             mma_ts(tmem + kColO + h * DW, tmem + kColS + (pos & 1) * S::kStep + h * S::kHalf + S::kHalf / 2 + k * 8,
                                    vd + (h * (S::kHalf / 16) + k) * (2048 >> 4), idesc_o, 1);
-                        mma_commit(&pv_done[h]);
+                        mma_commit(&pv_done[pos & 1][h]);
                     }
                     if (failed) break;
                     mma_commit(kEight ? &k_empty[buf] : &v_empty[buf]);
@@ -407,8 +410,12 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         *reinterpret_cast<const uint4*>(out_stage + r * 64 + ((piece ^ (r >> 1 & 3)) << 4));
             }
         };
+        // Waits for this group's product of a step whose scores it has seen.  A wait tells a phase from the next one only, and the tensor cores may be a step behind
+        // this group where the other one's P is late: so steps take two barriers in turns.  The phase before, of step pos - 2, is over then: the scores of
+        // step pos were asked for behind that product, or it was one of the piece before.
+        auto product_done = [&](int pos) { return warp_wait(&pv_done[pos & 1][group], (pos / 2) & 1); };
         auto rows_sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
-        int base = 0, parts = 0, steps = 0;  // steps: of this group
+        int base = 0, parts = 0;  // steps and pieces before this one
         unsigned long long next_sees = 0;
         for (int idx = blockIdx.x; idx < pieces.all; idx += ctas) {
             const RowsPiece p = rows_piece(a, pieces, idx, lane);
@@ -569,7 +576,7 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 }
                 if (g > 0 && __any_sync(0xffffffffu, alpha != 1.f)) {
                     // O must hold the group's products so far
-                    if (!warp_wait(&pv_done[group], (steps - 1) & 1)) { failed = true; break; }
+                    if (!product_done(pos - 1)) { failed = true; break; }
                     tc_fence_after_sync();
 #pragma unroll 1
                     for (int c = 0; c < DW / 32; ++c) {
@@ -581,7 +588,6 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         tmem_st_x32(o_col + c * 32, r);
                     }
                 }
-                ++steps;
                 if (!idle) {
                     const float ref = m == -INFINITY ? 0.f : m - kLift;
 #pragma unroll
@@ -644,15 +650,12 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         fence_proxy_async_smem();
                     }
                 }
-                // The group's product of the step before, while the next one still waits for this P: a wait tells a phase from the next one only, and the tensor
-                // cores, which take the groups in turns, may be a step behind this group where the other one's P is late.
-                if (g > 0 && !warp_wait(&pv_done[group], (steps - 2) & 1)) { failed = true; break; }
                 tmem_st_wait();
                 tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&p_ready[pos & 1][group]);
             }
-            if (!failed && !warp_wait(&pv_done[group], (steps - 1) & 1)) failed = true;
+            if (!failed && !product_done(base + n - 1)) failed = true;
             tc_fence_after_sync();
             base += n;
             group_state[group][row] = make_float4(m, l, kv_unit(unit_inv), 0.f);
