@@ -17,7 +17,7 @@
 //
 // What bounds it: the chain of a step (scores, softmax of a row per thread, P into tensor memory, product with V; 1.23 us for 128 keys of 16-bit rows,
 // where the tensor cores need 0.8, and 1.33 for 64 of 8-bit ones), and some 8 us around the steps: start, first copies, the output and the merge of pieces.
-// 4 x 32/8 heads x 64 tokens behind 1024 .. 4096 16-bit rows take 30.0 us, 8 x 28/4 x 16 behind 600 .. 2400 int8 rows 24.1, 1 x 32/8 x 5 behind some 600 12.9.
+// 4 x 32/8 heads x 64 tokens behind 1024 .. 4096 16-bit rows take 30.3 us, 8 x 28/4 x 16 behind 600 .. 2400 int8 rows 24.0, 1 x 32/8 x 5 behind some 600 12.9.
 #pragma once
 
 namespace forge {
