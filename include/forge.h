@@ -415,6 +415,106 @@ int forge_attn_tree(const forge_kv_cache* cache, const void* q, void* out, int d
                     void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * ---- A step of many requests: a KV cache in pages, and adapters of their own -----------------------------
+ * A server that takes requests in and out at every step gives a request's cache its memory in pages.  The step's tokens are packed,
+ * request after request: activations are [T, ...].  The run of a step: forge_kv_assign_pages, the projections (with
+ * forge_linear_adapters where requests have adapters), forge_kv_append_pages, forge_attn_decode_pages; when requests end,
+ * forge_kv_release_pages.  None of them needs the lengths on the host.
+ *
+ * forge_kv_pages: k and v [num_pages, Hkv, page_size, D], formats and scales ([num_pages, Hkv, page_size]) as in forge_kv_cache.  page_size: a power of
+ * two, 16 to 2^20; num_pages * Hkv * page_size < 2^31.  A slot is page * page_size + the row's place in the page.
+ * A table is int32 [B, max_pages] on the device: row j of request b lies in page table[b, j / page_size], at place j % page_size.
+ * max_pages * page_size <= 2^30.  An entry outside 0 .. num_pages - 1 names no page: what is written there is dropped, the attention takes
+ * its rows as zeros, and reading back leaves them out.  Entries behind a request's last row are not used, whatever they are.  Requests
+ * may share pages that none of them writes.
+ */
+typedef struct forge_kv_pages {
+    void *k, *v;
+    float *k_scale, *v_scale; /* 8-bit formats only */
+    int num_pages, Hkv, page_size, D;
+    int format;               /* FORGE_KV_* */
+} forge_kv_pages;
+
+/*
+ * A batch's tables and the pages that are free: free_pages, int32 [num_pages], of which the first free_count[0] (int32, on the device;
+ * clamped to 0 .. num_pages) are free, handed out from the last one on.  The struct is HOST memory, its pointers are DEVICE.
+ *
+ * forge_kv_assign_pages makes room for counts[b] more rows (NULL: one each; below 0: none) behind the lens[b] rows (clamped to
+ * 0 .. max_pages * page_size) of each request: the pages it needs beyond the ceil(lens[b] / page_size) that it has come from the free ones,
+ * in the order of the requests, and into its row of the table.  A request gets all its rows or none:
+ *   none, where its table or T has no room for them; the others still may;
+ *   none, where it needs pages and there are too few; so does every later request that needs any.
+ *   new_lens  int32 [B]      lens[b] + counts[b], or lens[b] where it got none.  May be lens itself.
+ *   starts    int32 [B + 1]  where each request's tokens begin: running sums of counts, refused requests' too, at most T.  May be NULL.
+ *   slots     int32 [T]      the slot of each token's row; -1 for tokens of refused requests and behind the last one
+ *   positions int32 [T]      its place lens[b] + i in the request (0 behind the last one).  May be NULL.
+ *   requests  int32 [T]      whose it is (-1 behind the last one).  May be NULL.
+ *   free_left int32 [1]      how many pages are free now.  NULL, or free_count itself: free_count is set.
+ * T: 1 to 2^30, the tokens that the buffers have room for.  Nothing else of the table is written.  B up to 65535.
+ *
+ * forge_kv_release_pages gives the pages of the lens[b] rows of requests with done[b] != 0 back (entries that name no page are left
+ * out), behind the free ones, in the order of requests and rows; free_left as above.  A page must come back once.  The table and lens stay:
+ * a request that takes the place starts with lens[b] = 0.
+ */
+typedef struct forge_kv_page_tables {
+    int32_t *table, *free_pages, *free_count;
+    int B, max_pages, page_size, num_pages;
+} forge_kv_page_tables;
+int forge_kv_assign_pages(const forge_kv_page_tables* tables, const int32_t* lens, const int32_t* counts, int T, int32_t* new_lens,
+                          int32_t* starts, int32_t* slots, int32_t* positions, int32_t* requests, int32_t* free_left, void* stream);
+int forge_kv_release_pages(const forge_kv_page_tables* tables, const int32_t* lens, const int32_t* done, int32_t* free_left, void* stream);
+
+/*
+ * forge_kv_append for packed tokens and a cache in pages: row slots[t] becomes token t of k and v, for every KV head; with `rotary`, k is
+ * rotated first, by positions[t] (required then).  A token whose slot is no slot of the cache is left out, its row of q_out too.  Two tokens may not have
+ * the same slot.  k, v [T, Hkv, D], q, q_out [T, Hq, D]: views of `dtype`, strides in elements for {token, head}, positive
+ * multiples of 8; NULL is dense.  Everything else as forge_kv_append.
+ *
+ * forge_kv_read_pages: forge_kv_read through a table; rows in entries that name no page are left as they were.
+ */
+typedef struct forge_kv_append_pages_desc {
+    const void *k, *v, *q;
+    void* q_out;
+    const int64_t *k_strides, *v_strides, *q_strides, *q_out_strides;
+    const int32_t *slots, *positions;
+    const forge_rotary* rotary;
+    int dtype, Hq, T;
+} forge_kv_append_pages_desc;
+int forge_kv_append_pages(const forge_kv_pages* cache, const forge_kv_append_pages_desc* desc, void* stream);
+int forge_kv_read_pages(const forge_kv_pages* cache, const int32_t* table, int B, int max_pages, void* k_out, void* v_out, int dtype, int S,
+                        const int64_t* k_strides, const int64_t* v_strides, const int32_t* first, const int32_t* counts, void* stream);
+
+/*
+ * forge_attn_decode_kv and forge_attn_tree over a cache in pages: request b's rows are those of its row of the table, lens clamped to
+ * 0 .. max_pages * page_size; a tree's own rows lie behind the lens[b] ones, in the table's order too.  Everything else, the
+ * workspace and its size included, as there: one workspace serves calls of both kinds, one after the other.
+ */
+int forge_attn_decode_pages(const forge_kv_pages* cache, const int32_t* table, int B, int max_pages, const void* q, void* out, int dtype,
+                            int Hq, const int32_t* lens, float scale, void* workspace, size_t workspace_bytes, void* stream);
+int forge_attn_tree_pages(const forge_kv_pages* cache, const int32_t* table, int B, int max_pages, const void* q, void* out, int dtype,
+                          int Hq, int T, const int64_t* q_strides, const int64_t* out_strides, const int32_t* lens, const int64_t* tree,
+                          int tree_B, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Low-rank adapters of many requests beside a projection that they share, whose output is y (forge_linear_act and its kind):
+ *     out[t,:] = y[t,:] + scales[i] * (x[t,:] A_i^T) B_i^T        with i = adapters[requests[t]]
+ * x [T, K], y and out [T, N], a [n, rank, K], b [n, N, rank] of `dtype` FORGE_DTYPE_BF16 or _F16; scales fp32 [n] or NULL (1).  requests:
+ * int32 [T], what forge_kv_assign_pages gives, and adapters int32 [R]; requests NULL: i = adapters[t] (R = T then).  A token whose request is outside
+ * 0 .. R - 1, or its adapter outside 0 .. n - 1, has none: out[t,:] = y[t,:].  Neighbouring tokens of one adapter share its reads;
+ * any order is right.  x, y, out: rows of x_stride, y_stride, out_stride elements (0: dense), multiples of 8; out may be y
+ * itself with the same stride, but may not overlap it otherwise, nor x.  K, N, rank: multiples of 8, rank up to 128.
+ * Sums are kept in fp32, x A_i^T times the scale to within 2^-15 of itself (bf16) or 2^-21 (fp16), and out is rounded once.  The same inputs give
+ * the same bits.
+ */
+typedef struct forge_adapters {
+    const void *a, *b;
+    const float* scales;
+    int n, rank, K, N, dtype;
+} forge_adapters;
+int forge_linear_adapters(const forge_adapters* set, const void* x, const void* y, void* out, int T, int64_t x_stride, int64_t y_stride,
+                          int64_t out_stride, const int32_t* requests, const int32_t* adapters, int R, void* stream);
+
+/*
  * Buffer planning for a fixed sequence of operators (Section 4.5, "Liveness Analysis" and "Linear-Scan
  * Buffer Allocation").  Host code only; nothing is launched.
  *

@@ -121,6 +121,43 @@ SIGNATURES.update({
     "forge_attn_tree": (_i, [ctypes.POINTER(KVCacheDesc), _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _f, _vp, _sz, _vp]),
 })
 
+class KVPagesDesc(ctypes.Structure):
+    """forge_kv_pages"""
+    _fields_ = [("k", _vp), ("v", _vp), ("k_scale", _vp), ("v_scale", _vp), ("num_pages", _i), ("Hkv", _i), ("page_size", _i), ("D", _i),
+                ("format", _i)]
+
+
+class PageTablesDesc(ctypes.Structure):
+    """forge_kv_page_tables"""
+    _fields_ = [("table", _vp), ("free_pages", _vp), ("free_count", _vp), ("B", _i), ("max_pages", _i), ("page_size", _i),
+                ("num_pages", _i)]
+
+
+class KVAppendPagesDesc(ctypes.Structure):
+    """forge_kv_append_pages_desc"""
+    _fields_ = [("k", _vp), ("v", _vp), ("q", _vp), ("q_out", _vp),
+                ("k_strides", ctypes.POINTER(ctypes.c_int64)), ("v_strides", ctypes.POINTER(ctypes.c_int64)),
+                ("q_strides", ctypes.POINTER(ctypes.c_int64)), ("q_out_strides", ctypes.POINTER(ctypes.c_int64)),
+                ("slots", _vp), ("positions", _vp), ("rotary", ctypes.POINTER(RotaryDesc)), ("dtype", _i), ("Hq", _i), ("T", _i)]
+
+
+class AdaptersDesc(ctypes.Structure):
+    """forge_adapters"""
+    _fields_ = [("a", _vp), ("b", _vp), ("scales", _vp), ("n", _i), ("rank", _i), ("K", _i), ("N", _i), ("dtype", _i)]
+
+
+_i64 = ctypes.c_int64
+SIGNATURES.update({
+    "forge_kv_assign_pages": (_i, [ctypes.POINTER(PageTablesDesc), _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "forge_kv_release_pages": (_i, [ctypes.POINTER(PageTablesDesc), _vp, _vp, _vp, _vp]),
+    "forge_kv_append_pages": (_i, [ctypes.POINTER(KVPagesDesc), ctypes.POINTER(KVAppendPagesDesc), _vp]),
+    "forge_kv_read_pages": (_i, [ctypes.POINTER(KVPagesDesc), _vp, _i, _i, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp]),
+    "forge_attn_decode_pages": (_i, [ctypes.POINTER(KVPagesDesc), _vp, _i, _i, _vp, _vp, _i, _i, _vp, _f, _vp, _sz, _vp]),
+    "forge_attn_tree_pages": (_i, [ctypes.POINTER(KVPagesDesc), _vp, _i, _i, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _f, _vp, _sz,
+                                   _vp]),
+    "forge_linear_adapters": (_i, [ctypes.POINTER(AdaptersDesc), _vp, _vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _i, _vp]),
+})
+
 _lib = None
 # host_calls.cpp: the frequent calls' marshalling in native code.  Its functions return -1 where a call is not plain (anything but
 # dense, contiguous CUDA tensors of matching shapes with the output given); then the Python below does it, with every check.
@@ -694,6 +731,255 @@ def attn_tree(q, cache, lens, tree=None, scale=None, out=None, workspace=None):
     _check("forge_attn_tree", load().forge_attn_tree(
         cache.desc, qp, op, _DTYPES[q.dtype], Hq, T, qs, os_, lp, tp, tree_B, float(D ** -0.5 if scale is None else scale),
         _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return out
+
+
+# ---- a step of many requests: a KV cache in pages, adapters of their own ----
+class KVPages:
+    """forge_kv_pages: k, v [num_pages, Hkv, page_size, D] in bf16, fp16, int8 or float8_e4m3fn; 8-bit ones with k_scale, v_scale
+    [num_pages, Hkv, page_size] in fp32.  The tensors are kept and belong to the caller."""
+
+    def __init__(self, k, v, k_scale=None, v_scale=None):
+        if k.dim() != 4 or tuple(v.shape) != tuple(k.shape):
+            raise ValueError("k, v [num_pages,Hkv,page_size,D] expected")
+        if k.dtype not in _KV_TYPES:
+            raise ValueError(f"k: expected one of {_KV_TYPES}")
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.format = _KV_TYPES.index(k.dtype)
+        self.num_pages, self.Hkv, self.page_size, self.D = k.shape
+        eight = self.format in (KV_INT8, KV_E4M3)
+        if eight != (k_scale is not None) or eight != (v_scale is not None):
+            raise ValueError("k_scale and v_scale [num_pages,Hkv,page_size] belong to 8-bit caches, and to no others")
+        kp, vp = _dev(k, k.dtype, "k"), _dev(v, k.dtype, "v")
+        shape = (self.num_pages, self.Hkv, self.page_size)
+        self.desc = KVPagesDesc(k=kp, v=vp, k_scale=_dev_or_none(k_scale, torch.float32, "k_scale", shape),
+                                v_scale=_dev_or_none(v_scale, torch.float32, "v_scale", shape),
+                                num_pages=self.num_pages, Hkv=self.Hkv, page_size=self.page_size, D=self.D, format=self.format)
+        if len({t.device for t in (k, v, k_scale, v_scale) if t is not None}) != 1:
+            raise ValueError("the tensors of a cache must be on one device")
+        self.address, self.device = ctypes.addressof(self.desc), k.device.index
+
+    @classmethod
+    def empty(cls, num_pages, Hkv, page_size, D, format=KV_BF16, device="cuda"):
+        """A new cache (of zeros: 8-bit rows that were never written stand for zeros)."""
+        kv = [torch.zeros((num_pages, Hkv, page_size, D), dtype=_KV_TYPES[format], device=device) for _ in range(2)]
+        scales = [torch.zeros((num_pages, Hkv, page_size), dtype=torch.float32, device=device) for _ in range(2)] if format in (KV_INT8, KV_E4M3) else []
+        return cls(*kv, *scales)
+
+
+class PageTables:
+    """forge_kv_page_tables: table int32 [B, max_pages], free_pages int32 [num_pages], free_count int32 [1].  The tensors are kept and belong
+    to the caller."""
+
+    def __init__(self, table, free_pages, free_count, page_size):
+        if table.dim() != 2 or free_pages.dim() != 1 or tuple(free_count.shape) != (1,):
+            raise ValueError("table [B,max_pages], free_pages [num_pages] and free_count [1] expected")
+        self.table, self.free_pages, self.free_count, self.page_size = table, free_pages, free_count, int(page_size)
+        self.B, self.max_pages = table.shape
+        self.desc = PageTablesDesc(table=_dev(table, torch.int32, "table"), free_pages=_dev(free_pages, torch.int32, "free_pages"),
+                                   free_count=_dev(free_count, torch.int32, "free_count"), B=self.B, max_pages=self.max_pages,
+                                   page_size=self.page_size, num_pages=free_pages.numel())
+        if len({t.device for t in (table, free_pages, free_count)}) != 1:
+            raise ValueError("the tensors of the tables must be on one device")
+        self.address, self.device = ctypes.addressof(self.desc), table.device.index
+
+    @classmethod
+    def empty(cls, B, max_pages, num_pages, page_size, device="cuda"):
+        """Tables of no pages (-1), all of num_pages free; page 0 is handed out first."""
+        free = torch.arange(num_pages - 1, -1, -1, dtype=torch.int32, device=device)
+        count = torch.full((1,), num_pages, dtype=torch.int32, device=device)
+        return cls(torch.full((B, max_pages), -1, dtype=torch.int32, device=device), free, count, page_size)
+
+
+class PageSlots:
+    """What assign_pages says of a step: lens int32 [B], starts [B + 1], slots, positions and requests [T] (starts, positions and
+    requests may be None).  The tensors are kept."""
+
+    def __init__(self, lens, starts, slots, positions=None, requests=None):
+        B, T = lens.numel(), slots.numel()
+        self.lens, self.starts, self.slots, self.positions, self.requests, self.B, self.T = lens, starts, slots, positions, requests, B, T
+        i32 = torch.int32
+        self.pointers = (_dev_or_none(lens, i32, "lens", (B,)), _dev_or_none(starts, i32, "starts", (B + 1,)),
+                         _dev_or_none(slots, i32, "slots", (T,)), _dev_or_none(positions, i32, "positions", (T,)),
+                         _dev_or_none(requests, i32, "requests", (T,)))
+        if len({t.device for t in (lens, starts, slots, positions, requests) if t is not None}) != 1:
+            raise ValueError("the tensors of a step must be on one device")
+        self.device = lens.device.index
+
+    @classmethod
+    def empty(cls, B, T, device="cuda"):
+        return cls(*(torch.zeros(n, dtype=torch.int32, device=device) for n in (B, B + 1, T, T, T)))
+
+
+def assign_pages(tables, lens, out, counts=None, free_left=None):
+    """forge_kv_assign_pages: room for counts[b] (int32 [B]; None: one) more rows behind the lens[b] (int32 [B]) rows of each request.  What
+    they got goes into `out`, a PageSlots whose T is the tokens that there is room for; out.lens may be lens.  free_left int32 [1]: where the
+    number of pages left goes (None: into tables.free_count).  Returns out."""
+    if out.B != tables.B:
+        raise ValueError("out: a PageSlots of the tables' B expected")
+    i32 = torch.int32
+    lp, cp = _dev_or_none(lens, i32, "lens", (tables.B,)), _dev_or_none(counts, i32, "counts", (tables.B,))
+    fp = _dev_or_none(free_left, i32, "free_left", (1,))
+    _on_current(tables.table, out.lens, lens, counts, free_left)
+    o = out.pointers
+    _check("forge_kv_assign_pages", load().forge_kv_assign_pages(tables.desc, lp, cp, out.T, o[0], o[1], o[2], o[3], o[4], fp, _stream()))
+    return out
+
+
+def release_pages(tables, lens, done, free_left=None):
+    """forge_kv_release_pages: the pages of the first lens[b] rows of requests with done[b] != 0 (int32 [B]) are free again."""
+    i32 = torch.int32
+    lp, dp = _dev_or_none(lens, i32, "lens", (tables.B,)), _dev_or_none(done, i32, "done", (tables.B,))
+    fp = _dev_or_none(free_left, i32, "free_left", (1,))
+    _on_current(tables.table, lens, done, free_left)
+    _check("forge_kv_release_pages", load().forge_kv_release_pages(tables.desc, lp, dp, fp, _stream()))
+
+
+def _token_view(t: torch.Tensor, dtype, name: str, shape):
+    """Address and {token, head} strides of a [T, H, D] view with contiguous rows."""
+    if not (t.is_cuda and t.dtype == dtype and t.dim() == 3 and tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{name}: expected a CUDA tensor {list(shape)} of {dtype}")
+    T, H, D = shape
+    st = t.stride()
+    if st[2] != 1 and D != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return t.data_ptr(), (ctypes.c_int64 * 2)(st[0] if T > 1 else 8, st[1] if H > 1 else 8)
+
+
+def kv_append_pages(cache, k, v, slots, positions=None, rotary=None, q=None, q_out=None):
+    """forge_kv_append_pages: k, v [T,Hkv,D] views (bf16 or fp16) of packed tokens become rows slots[t] (int32 [T]) of a KVPages, k rotated
+    first by positions[t] (int32 [T]) if `rotary` is given; q [T,Hq,D] is rotated into q_out in the same launch.  Returns q_out
+    (None without q)."""
+    if k.dim() != 3 or k.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("k [T,Hkv,D] in bf16 or fp16 expected")
+    T, H, D = k.shape
+    if (H, D) != (cache.Hkv, cache.D):
+        raise ValueError("k, v [T,Hkv,D] of the cache's Hkv and D expected")
+    d = KVAppendPagesDesc(dtype=_DTYPES[k.dtype], T=T)
+    d.k, ks = _token_view(k, k.dtype, "k", (T, H, D))
+    d.v, vs = _token_view(v, k.dtype, "v", (T, H, D))
+    d.k_strides, d.v_strides = ks, vs
+    if q is not None:
+        q_out = torch.empty_like(q) if q_out is None else q_out
+        d.Hq = q.shape[1]
+        d.q, qs = _token_view(q, k.dtype, "q", (T, d.Hq, D))
+        d.q_out, qos = _token_view(q_out, k.dtype, "q_out", (T, d.Hq, D))
+        d.q_strides, d.q_out_strides = qs, qos
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    d.slots = _dev_or_none(slots, torch.int32, "slots", (T,))
+    d.positions = _dev_or_none(positions, torch.int32, "positions", (T,))
+    if rotary is not None:
+        d.rotary = ctypes.pointer(rotary.desc)
+    _on_current(cache.k, k, v, q, q_out, slots, positions, None if rotary is None else rotary.inv_freq)
+    _check("forge_kv_append_pages", load().forge_kv_append_pages(cache.desc, d, _stream()))
+    return q_out
+
+
+def _table(table):
+    if table.dim() != 2:
+        raise ValueError("table [B,max_pages] expected")
+    return _dev(table, torch.int32, "table"), table.shape[0], table.shape[1]
+
+
+def kv_read_pages(cache, table, k_out, v_out, first=None, counts=None):
+    """forge_kv_read_pages: kv_read of a KVPages through table int32 [B,max_pages]."""
+    tp, B, max_pages = _table(table)
+    if k_out.dim() != 4 or k_out.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("k_out [B,Hkv,S,D] in bf16 or fp16 expected")
+    shape = (B, cache.Hkv, k_out.shape[2], cache.D)
+    kp, ks = _view(k_out, k_out.dtype, "k_out", shape)
+    vp, vs = _view(v_out, k_out.dtype, "v_out", shape)
+    fp, cp = _dev_or_none(first, torch.int32, "first", (B,)), _dev_or_none(counts, torch.int32, "counts", (B,))
+    _on_current(cache.k, table, k_out, v_out, first, counts)
+    _check("forge_kv_read_pages", load().forge_kv_read_pages(cache.desc, tp, B, max_pages, kp, vp, _DTYPES[k_out.dtype], shape[2], ks, vs, fp, cp,
+                                                             _stream()))
+    return k_out, v_out
+
+
+def _pages_workspace(workspace, cache, B, Hq, T, device):
+    if workspace is None:
+        workspace = torch.empty(max(attn_kv_workspace_bytes(B, Hq, cache.Hkv, T, cache.D), 16), dtype=torch.uint8, device=device)
+        attn_kv_workspace_init(workspace)
+    return workspace
+
+
+def attn_decode_pages(q, cache, table, lens, scale=None, out=None, workspace=None):
+    """forge_attn_decode_pages: attn_decode_kv over a KVPages, the rows of request b in the pages of table[b] (int32 [B,max_pages])."""
+    tp, B, max_pages = _table(table)
+    if q.dim() != 3 or (q.shape[0], q.shape[2]) != (B, cache.D):
+        raise ValueError("q [B,Hq,D] of the table's B and the cache's D expected")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("q: bf16 or fp16 expected")
+    Hq, D = q.shape[1:]
+    out = torch.empty_like(q) if out is None else out
+    if tuple(out.shape) != tuple(q.shape):
+        raise ValueError("out: the shape of q expected")
+    qp, op, lp = _dev(q, q.dtype, "q"), _dev(out, q.dtype, "out"), _dev_or_none(lens, torch.int32, "lens", (B,))
+    _on_current(cache.k, table, q, out, lens, workspace)
+    workspace = _pages_workspace(workspace, cache, B, Hq, 1, q.device)
+    _check("forge_attn_decode_pages", load().forge_attn_decode_pages(
+        cache.desc, tp, B, max_pages, qp, op, _DTYPES[q.dtype], Hq, lp, float(D ** -0.5 if scale is None else scale),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return out
+
+
+def attn_tree_pages(q, cache, table, lens, tree=None, scale=None, out=None, workspace=None):
+    """forge_attn_tree_pages: attn_tree over a KVPages, the rows of request b in the pages of table[b] (int32 [B,max_pages])."""
+    tp, B, max_pages = _table(table)
+    if q.dim() != 4 or (q.shape[0], q.shape[3]) != (B, cache.D):
+        raise ValueError("q [B,Hq,T,D] of the table's B and the cache's D expected")
+    if q.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("q: bf16 or fp16 expected")
+    _, Hq, T, D = q.shape
+    if tree is not None and (tree.dim() != 2 or tree.shape[0] not in (1, B)):
+        raise ValueError("tree [B or 1, T] expected")
+    out = torch.empty_like(q) if out is None else out
+    qp, qs = _view(q, q.dtype, "q", (B, Hq, T, D))
+    op, os_ = _view(out, q.dtype, "out", (B, Hq, T, D))
+    tree_B = 1 if tree is None else tree.shape[0]
+    lp, trp = _dev_or_none(lens, torch.int32, "lens", (B,)), _dev_or_none(tree, torch.int64, "tree", (tree_B, T))
+    _on_current(cache.k, table, q, out, lens, tree, workspace)
+    workspace = _pages_workspace(workspace, cache, B, Hq, T, q.device)
+    _check("forge_attn_tree_pages", load().forge_attn_tree_pages(
+        cache.desc, tp, B, max_pages, qp, op, _DTYPES[q.dtype], Hq, T, qs, os_, lp, trp, tree_B, float(D ** -0.5 if scale is None else scale),
+        _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream()))
+    return out
+
+
+def _rows(t: torch.Tensor, dtype, name: str, shape):
+    """Address and row stride of a [T, n] view with contiguous rows."""
+    if not (t.is_cuda and t.dtype == dtype and tuple(t.shape) == tuple(shape)):
+        raise ValueError(f"{name}: expected a CUDA tensor {list(shape)} of {dtype}")
+    if t.stride(1) != 1 and shape[1] != 1:
+        raise ValueError(f"{name}: the last dimension must be contiguous")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else 0
+
+
+def linear_adapters(x, y, a, b, adapters, requests=None, scales=None, out=None):
+    """forge_linear_adapters: y + scales[i] * (x A_i^T) B_i^T with i = adapters[requests[t]] (requests None: adapters[t]); x [T,K] and
+    y, out [T,N] views with contiguous rows, a [n,rank,K], b [n,N,rank], all bf16 or fp16; adapters int32 [R], requests int32 [T], scales
+    fp32 [n] or None.  Tokens without an adapter (-1) keep y.  out may be y itself."""
+    if x.dim() != 2 or y.dim() != 2 or a.dim() != 3 or b.dim() != 3 or adapters.dim() != 1:
+        raise ValueError("x [T,K], y [T,N], a [n,rank,K], b [n,N,rank], adapters [R] expected")
+    if x.dtype not in (torch.bfloat16, torch.float16):
+        raise ValueError("x: bf16 or fp16 expected")
+    (T, K), N, (n, rank) = x.shape, y.shape[1], a.shape[:2]
+    if tuple(a.shape) != (n, rank, K) or tuple(b.shape) != (n, N, rank):
+        raise ValueError("a [n,rank,K], b [n,N,rank] expected")
+    out = torch.empty((T, N), dtype=x.dtype, device=x.device) if out is None else out
+    t = x.dtype
+    xp, xs = _rows(x, t, "x", (T, K))
+    yp, ys = _rows(y, t, "y", (T, N))
+    op, os_ = _rows(out, t, "out", (T, N))
+    R = adapters.shape[0]
+    if requests is None and R != T:
+        raise ValueError("adapters [T] expected without requests")
+    d = AdaptersDesc(a=_dev(a, t, "a"), b=_dev(b, t, "b"), scales=_dev_or_none(scales, torch.float32, "scales", (n,)), n=n, rank=rank, K=K, N=N,
+                     dtype=_DTYPES[t])
+    rp, ap = _dev_or_none(requests, torch.int32, "requests", (T,)), _dev(adapters, torch.int32, "adapters")
+    _on_current(x, y, out, a, b, scales, requests, adapters)
+    _check("forge_linear_adapters", load().forge_linear_adapters(d, xp, yp, op, T, xs, ys, os_, rp, ap, R, _stream()))
     return out
 
 

@@ -1,11 +1,14 @@
-// C entry points of the attention over a KV cache of any format.  The kernels are in attn_kv_narrow.cuh and attn_kv_rows.cuh.
+// C entry points of the attention over a KV cache of any format, in one block or in pages.  The kernels are in attn_kv_narrow.cuh and attn_kv_rows.cuh.
 #include "attn_kv.cuh"
 
 namespace forge {
-template <> int run_attn_kv<FORGE_KV_BF16>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
-template <> int run_attn_kv<FORGE_KV_F16>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
-template <> int run_attn_kv<FORGE_KV_INT8>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
-template <> int run_attn_kv<FORGE_KV_E4M3>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t);
+#define FORGE_RUN_ATTN_KV(fmt)                                                               \
+    template <> int run_attn_kv<fmt, false>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t); \
+    template <> int run_attn_kv<fmt, true>(const forge_kv_cache&, const KvAttnArgs&, int, cudaStream_t)
+FORGE_RUN_ATTN_KV(FORGE_KV_BF16);
+FORGE_RUN_ATTN_KV(FORGE_KV_F16);
+FORGE_RUN_ATTN_KV(FORGE_KV_INT8);
+FORGE_RUN_ATTN_KV(FORGE_KV_E4M3);
 
 namespace {
 
@@ -27,11 +30,21 @@ size_t counter_bytes(size_t items) {
 // Floats of what a CTA leaves of an item: O, m and l of the rows that its kernel works on.
 size_t part_floats(long long rows, int D) { return (size_t)(rows <= kNarrowRows ? 8 : 128) * ((D <= 64 ? 64 : 128) + 4); }
 
-int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, bool own_rows, const int64_t* q_strides,
-            const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale, void* workspace,
-            size_t workspace_bytes, void* stream) {
-    int st = check_cache(cache, dtype);
-    if (st != FORGE_OK) return st;
+template <bool PAGED>
+int run_format(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s) {
+    switch (cache.format) {
+        case FORGE_KV_BF16: return run_attn_kv<FORGE_KV_BF16, PAGED>(cache, a, ctas, s);
+        case FORGE_KV_F16: return run_attn_kv<FORGE_KV_F16, PAGED>(cache, a, ctas, s);
+        case FORGE_KV_INT8: return run_attn_kv<FORGE_KV_INT8, PAGED>(cache, a, ctas, s);
+        default: return run_attn_kv<FORGE_KV_E4M3, PAGED>(cache, a, ctas, s);
+    }
+}
+
+// cache: as the tokens see it.  pages: the memory, where that is in pages that `table` puts in order.
+int attn_kv(const forge_kv_cache* cache, const forge_kv_pages* pages, const int32_t* table, const void* q, void* out, int dtype, int Hq, int T,
+            bool own_rows, const int64_t* q_strides, const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale,
+            void* workspace, size_t workspace_bytes, void* stream) {
+    int st;
     if (!q || !out || !lens || Hq <= 0 || T <= 0 || Hq % cache->Hkv != 0) return FORGE_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lens) & 3u)) return FORGE_ERR_INVALID_ARG;
     if (tree && ((reinterpret_cast<uintptr_t>(tree) & 7u) || (tree_B != 1 && tree_B != cache->B))) return FORGE_ERR_INVALID_ARG;
@@ -70,12 +83,32 @@ int attn_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, in
     int ctas = sms < kKvMaxCtas ? sms : kKvMaxCtas;
     if (tiles < ctas) ctas = (int)tiles;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    switch (cache->format) {
-        case FORGE_KV_BF16: return run_attn_kv<FORGE_KV_BF16>(*cache, a, ctas, s);
-        case FORGE_KV_F16: return run_attn_kv<FORGE_KV_F16>(*cache, a, ctas, s);
-        case FORGE_KV_INT8: return run_attn_kv<FORGE_KV_INT8>(*cache, a, ctas, s);
-        default: return run_attn_kv<FORGE_KV_E4M3>(*cache, a, ctas, s);
-    }
+    if (!pages) return run_format<false>(*cache, a, ctas, s);
+    a.table = table;
+    a.num_pages = pages->num_pages;
+    a.max_pages = cache->Smax / pages->page_size;
+    a.page_shift = log2_of(pages->page_size);
+    const forge_kv_cache memory = {pages->k, pages->v, pages->k_scale, pages->v_scale, pages->num_pages, pages->Hkv, pages->page_size, pages->D, pages->format};
+    return run_format<true>(memory, a, ctas, s);
+}
+
+int attn_cache(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, bool own_rows, const int64_t* q_strides,
+               const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale, void* workspace,
+               size_t workspace_bytes, void* stream) {
+    const int st = check_cache(cache, dtype);
+    if (st != FORGE_OK) return st;
+    return attn_kv(cache, nullptr, nullptr, q, out, dtype, Hq, T, own_rows, q_strides, out_strides, lens, tree, tree_B, scale, workspace,
+                   workspace_bytes, stream);
+}
+int attn_pages(const forge_kv_pages* pages, const int32_t* table, int B, int max_pages, const void* q, void* out, int dtype, int Hq, int T,
+               bool own_rows, const int64_t* q_strides, const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B,
+               float scale, void* workspace, size_t workspace_bytes, void* stream) {
+    int st = check_pages(pages, dtype), rows = 0;
+    if (st != FORGE_OK) return st;
+    if ((st = check_table(table, B, max_pages, pages->page_size, &rows)) != FORGE_OK) return st;
+    const forge_kv_cache seen = {pages->k, pages->v, pages->k_scale, pages->v_scale, B, pages->Hkv, rows, pages->D, pages->format};
+    return attn_kv(&seen, pages, table, q, out, dtype, Hq, T, own_rows, q_strides, out_strides, lens, tree, tree_B, scale, workspace,
+                   workspace_bytes, stream);
 }
 
 }  // namespace
@@ -96,12 +129,26 @@ extern "C" int forge_attn_kv_workspace_init(void* workspace, size_t workspace_by
 
 extern "C" int forge_attn_decode_kv(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, const int32_t* lens,
                                     float scale, void* workspace, size_t workspace_bytes, void* stream) {
-    return forge::attn_kv(cache, q, out, dtype, Hq, 1, false, nullptr, nullptr, lens, nullptr, 1, scale, workspace, workspace_bytes, stream);
+    return forge::attn_cache(cache, q, out, dtype, Hq, 1, false, nullptr, nullptr, lens, nullptr, 1, scale, workspace, workspace_bytes, stream);
 }
 
 extern "C" int forge_attn_tree(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, const int64_t* q_strides,
                                const int64_t* out_strides, const int32_t* lens, const int64_t* tree, int tree_B, float scale,
                                void* workspace, size_t workspace_bytes, void* stream) {
-    return forge::attn_kv(cache, q, out, dtype, Hq, T, true, q_strides, out_strides, lens, tree, tree_B, scale, workspace,
-                          workspace_bytes, stream);
+    return forge::attn_cache(cache, q, out, dtype, Hq, T, true, q_strides, out_strides, lens, tree, tree_B, scale, workspace,
+                             workspace_bytes, stream);
+}
+
+extern "C" int forge_attn_decode_pages(const forge_kv_pages* cache, const int32_t* table, int B, int max_pages, const void* q, void* out,
+                                       int dtype, int Hq, const int32_t* lens, float scale, void* workspace, size_t workspace_bytes,
+                                       void* stream) {
+    return forge::attn_pages(cache, table, B, max_pages, q, out, dtype, Hq, 1, false, nullptr, nullptr, lens, nullptr, 1, scale, workspace,
+                             workspace_bytes, stream);
+}
+
+extern "C" int forge_attn_tree_pages(const forge_kv_pages* cache, const int32_t* table, int B, int max_pages, const void* q, void* out,
+                                     int dtype, int Hq, int T, const int64_t* q_strides, const int64_t* out_strides, const int32_t* lens,
+                                     const int64_t* tree, int tree_B, float scale, void* workspace, size_t workspace_bytes, void* stream) {
+    return forge::attn_pages(cache, table, B, max_pages, q, out, dtype, Hq, T, true, q_strides, out_strides, lens, tree, tree_B, scale,
+                             workspace, workspace_bytes, stream);
 }

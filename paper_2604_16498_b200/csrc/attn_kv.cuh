@@ -16,6 +16,7 @@
 
 #include "attn_math.cuh"
 #include "kv_cache.cuh"
+#include "mma_16816.cuh"
 #include "sm100_ptx.cuh"
 #include "tmap.cuh"
 
@@ -45,9 +46,21 @@ struct KvAttnArgs {
     unsigned int* counters;
     float* parts;                    // [cta][2]: what a CTA leaves of the items at the ends of its run
     int* status;
+    // a cache in pages: the rows of a sequence are those of the pages that its row of the table names, in that order
+    const int32_t* table;            // [B, max_pages]
+    int max_pages, num_pages, page_shift;
 };
 
 namespace {
+
+// A cache in pages.  Copies take boxes of rows that lie in one page: as many as a page has, up to the rows of a block.  An entry of the table that names
+// no page, and one behind the sequence's last row, becomes box -1, which the copy engine fills with zeros.
+__device__ __forceinline__ int page_entry(const KvAttnArgs& a, int b, int page) {
+    return page < a.max_pages ? __ldcg(a.table + (int64_t)b * a.max_pages + page) : -1;  // L2's: the kernel before this one may have had old ones in L1
+}
+__device__ __forceinline__ int page_box(const KvAttnArgs& a, int entry, int kvh) {
+    return (unsigned)entry < (unsigned)a.num_pages ? entry * a.Hkv + kvh : -1;
+}
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -63,18 +76,6 @@ __device__ __forceinline__ void lds4(uint32_t addr, uint32_t (&r)[4]) {
 __device__ __forceinline__ void lds2(uint32_t addr, uint32_t& a, uint32_t& b) {
     asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(a), "=r"(b) : "r"(addr) : "memory");
 }
-// D(16 x 8, fp32) += A(16 x 16) B(16 x 8); lane = (g = lane / 4, c = lane % 4) holds of A rows g, g + 8 and k 2c, 2c+1, 2c+8, 2c+9;
-// of B column g and the same k; of D rows g, g + 8 and columns 2c, 2c + 1.
-template <bool F16>
-__device__ __forceinline__ void mma_16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    if constexpr (F16)
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                     : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-
 __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, uint32_t bytes, uint64_t* bar) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                  ::"r"(smem_dst), "l"(src), "r"(bytes), "r"(ptx::smem_u32(bar))
@@ -253,14 +254,15 @@ struct KvSchedule {
 namespace forge {
 
 // One per format, each in a file of its own (they compile side by side).
-template <int FMT>
+// PAGED: `cache` has the pages as its sequences, of a page's rows each.
+template <int FMT, bool PAGED>
 int run_attn_kv(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s);
-#define FORGE_ATTN_KV_FORMAT(fmt)                                                                         \
+#define FORGE_ATTN_KV_FORMAT(fmt, paged)                                                                  \
     template <>                                                                                           \
-    int run_attn_kv<fmt>(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s) {    \
+    int run_attn_kv<fmt, paged>(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s) { \
         if (a.rows <= kNarrowRows)                                                                        \
-            return cache.D <= 64 ? launch_attn_kv_narrow<64, fmt>(cache, a, ctas, s) : launch_attn_kv_narrow<128, fmt>(cache, a, ctas, s); \
-        return cache.D <= 64 ? launch_attn_kv_rows<64, fmt>(cache, a, ctas, s) : launch_attn_kv_rows<128, fmt>(cache, a, ctas, s); \
+            return cache.D <= 64 ? launch_attn_kv_narrow<64, fmt, paged>(cache, a, ctas, s) : launch_attn_kv_narrow<128, fmt, paged>(cache, a, ctas, s); \
+        return cache.D <= 64 ? launch_attn_kv_rows<64, fmt, paged>(cache, a, ctas, s) : launch_attn_kv_rows<128, fmt, paged>(cache, a, ctas, s); \
     }
 
 }  // namespace forge

@@ -2,5 +2,5 @@
 #include "attn_kv.cuh"
 
 namespace forge {
-FORGE_ATTN_KV_FORMAT(FORGE_KV_INT8)
+FORGE_ATTN_KV_FORMAT(FORGE_KV_INT8, false)
 }

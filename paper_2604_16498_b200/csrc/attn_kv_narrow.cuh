@@ -120,7 +120,7 @@ struct NarrowWalk {
     }
 };
 
-template <int DW, int FMT>
+template <int DW, int FMT, bool PAGED>
 __global__ void __launch_bounds__(kNarrowThreads, 1)
 attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                       const __grid_constant__ CUtensorMap tmap_ks, const __grid_constant__ CUtensorMap tmap_vs, const KvAttnArgs a) {
@@ -215,7 +215,68 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     NarrowWalk ahead = cur;
     int issued = 0;
     const uint64_t policy = ptx::l2_policy_evict_first();
+    // PAGED: 32 entries of the table, one in each lane, those of the item's pages from entries0 on; and the ones that come after them in the run, asked
+    // for when the first of these is used: behind the copies in flight they are long in coming.
+    int entries = -1, entries0 = 0, entries_then = -1;
+    auto ask_entries = [&]() {
+        int b = ahead.b, from = entries0 + 32;
+        if ((int64_t)from << a.page_shift >= kv_rows(a, ahead.past)) {  // the item after this one
+            from = 0;
+            b += ahead.kvh + 1 == a.Hkv;
+        }
+        entries_then = b < a.B ? page_entry(a, b, from + lane) : -1;
+    };
+    const int sub = PAGED ? min(1 << a.page_shift, KEYS) : KEYS;  // rows of a copy
+    if constexpr (PAGED) {
+        if (cur.u < cur.end) {
+            entries0 = (cur.tile * KEYS) >> a.page_shift;
+            entries = page_entry(a, cur.b, entries0 + lane);
+            ask_entries();
+        }
+    }
+    auto issue_paged = [&]() {
+        if (ahead.u >= ahead.end) return;
+        const int j0 = ahead.tile * KEYS, rows = kv_rows(a, ahead.past), st = issued % S::kStages;
+        const int page = j0 >> a.page_shift;
+        const bool item = issued > 0 && ahead.tile == 0;
+        if (item || page >= entries0 + 32) {
+            entries = entries_then;
+            entries0 = item ? 0 : entries0 + 32;
+            ask_entries();
+        }
+        const uint32_t dst = ring + st * S::kStageBytes;
+        if (j0 >= rows) {  // a sequence without rows
+            if (lane == 0) ptx::mbar_arrive(&full[st]);
+        } else {
+            if (lane == 0) ptx::mbar_expect_tx(&full[st], S::kStageBytes + (kEight ? 2 * KEYS * 4 : 0));
+#pragma unroll
+            for (int i = 0; i < KG; ++i) {  // KG copies of 16 rows, or one of all
+                if (i * sub >= KEYS) break;
+                const int entry = __shfl_sync(0xffffffffu, entries, (page + i - entries0) & 31);
+                const int box = j0 + i * sub < rows ? page_box(a, entry, ahead.kvh) : -1, y = (j0 + i * sub) & ((1 << a.page_shift) - 1);
+                if (lane != 0) continue;
+                if constexpr (kEight) {
+                    ptx::tma_load_2d_addr(scales + st * (2 * kScaleBox) + i * 128, &tmap_ks, &full[st], y, box);
+                    ptx::tma_load_2d_addr(scales + st * (2 * kScaleBox) + kScaleBox + i * 128, &tmap_vs, &full[st], y, box);
+                    ptx::tma_load_3d_addr_hint(dst + i * (16 * DW), &tmap_k, &full[st], 0, y, box, policy);
+                    ptx::tma_load_3d_addr_hint(dst + S::kKBytes + i * (16 * DW), &tmap_v, &full[st], 0, y, box, policy);
+                } else {
+#pragma unroll
+                    for (int cb = 0; cb < DW / 64; ++cb) {
+                        ptx::tma_load_3d_addr_hint(dst + cb * (KEYS * 128), &tmap_k, &full[st], cb * 64, y, box, policy);
+                        ptx::tma_load_3d_addr_hint(dst + S::kKBytes + cb * (KEYS * 128), &tmap_v, &full[st], cb * 64, y, box, policy);
+                    }
+                }
+            }
+        }
+        ++issued;
+        ahead.step<KEYS>(a, sched, 1);
+    };
     auto issue = [&]() {
+        if constexpr (PAGED) {
+            issue_paged();
+            return;
+        }
         if (ahead.u >= ahead.end) return;
         const int j0 = ahead.tile * KEYS, bk = ahead.b * a.Hkv + ahead.kvh, rows = kv_rows(a, ahead.past) - j0;
         const int st = issued % S::kStages;
@@ -383,7 +444,9 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
 #pragma unroll
                         for (int x = 0; x < 4; ++x) kr[i][h * 4 + x] = w[x];
                     }
-                    const uint32_t sc = scales + stage * (2 * kScaleBox) + (((p.b * a.Hkv + p.kvh) * a.Smax + j0) & 3) * 4 + row * 4;
+                    const uint32_t sc = scales + stage * (2 * kScaleBox) +
+                                        (PAGED ? (i >> 1) * (sub == 16 ? 128 : 64) + (row & 15) * 4
+                                               : (((p.b * a.Hkv + p.kvh) * a.Smax + j0) & 3) * 4 + row * 4);
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(ks[i >> 1][i & 1]) : "r"(sc) : "memory");
                     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(vs[i >> 1][i & 1]) : "r"(sc + kScaleBox) : "memory");
                 }
@@ -804,24 +867,27 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     }
 }
 
-template <int DW, int FMT>
+template <int DW, int FMT, bool PAGED>
 int launch_attn_kv_narrow(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s) {
     using S = NarrowShape<DW, FMT>;
     CUtensorMap tk, tv;
     const uint64_t es = S::kEight ? 1 : 2;
-    const uint32_t box[3] = {S::kEight ? (uint32_t)DW : 64u, (uint32_t)S::kKeys, 1};
+    const uint32_t keys = PAGED && cache.Smax < S::kKeys ? cache.Smax : S::kKeys;
+    const uint32_t box[3] = {S::kEight ? (uint32_t)DW : 64u, keys, 1};
     const uint64_t dims[3] = {(uint64_t)cache.D, (uint64_t)cache.Smax, (uint64_t)cache.B * cache.Hkv};
     const uint64_t strides[2] = {(uint64_t)cache.D * es, (uint64_t)cache.Smax * cache.D * es};
     const auto encode = !S::kEight ? encode_tmap_bf16_sw128 : DW == 128 ? encode_tmap_u8_sw128 : encode_tmap_u8_sw64;
     if (!encode(&tk, cache.k, 3, dims, strides, box) || !encode(&tv, cache.v, 3, dims, strides, box)) return FORGE_ERR_CUDA;
     CUtensorMap tks = {}, tvs = {};
     if (S::kEight) {
-        const uint32_t sbox[1] = {kScaleKeys};
-        const uint64_t n[1] = {(uint64_t)cache.B * cache.Hkv * cache.Smax};
-        if (!encode_tmap_f32_plain(&tks, cache.k_scale, 1, n, nullptr, sbox) || !encode_tmap_f32_plain(&tvs, cache.v_scale, 1, n, nullptr, sbox))
+        const uint32_t sbox[2] = {PAGED ? keys : (uint32_t)kScaleKeys, 1};
+        const uint64_t n[2] = {PAGED ? (uint64_t)cache.Smax : (uint64_t)cache.B * cache.Hkv * cache.Smax, (uint64_t)cache.B * cache.Hkv};
+        const uint64_t row[1] = {(uint64_t)cache.Smax * 4};
+        if (!encode_tmap_f32_plain(&tks, cache.k_scale, PAGED ? 2 : 1, n, PAGED ? row : nullptr, sbox) ||
+            !encode_tmap_f32_plain(&tvs, cache.v_scale, PAGED ? 2 : 1, n, PAGED ? row : nullptr, sbox))
             return FORGE_ERR_CUDA;
     }
-    auto kernel = attn_kv_narrow_kernel<DW, FMT>;
+    auto kernel = attn_kv_narrow_kernel<DW, FMT, PAGED>;
     FORGE_SET_SMEM_ONCE(kernel, S::kSmem);
     FORGE_CUDA_TRY(launch_pdl(kernel, dim3(ctas), dim3(kNarrowThreads), S::kSmem, s, tk, tv, tks, tvs, a));
     return finish_launch(1);

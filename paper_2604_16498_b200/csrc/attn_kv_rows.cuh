@@ -150,7 +150,7 @@ __device__ __forceinline__ RowsPiece rows_piece(const KvAttnArgs& a, const RowsP
 // Where element 8 i of row r of a [rows][64] chunk lies: 16-byte pieces swizzled over 128-byte lines.
 __device__ __forceinline__ uint32_t sw128(int r, int piece) { return r * 128 + ((piece ^ (r & 7)) << 4); }
 
-template <int DW, int FMT>
+template <int DW, int FMT, bool PAGED>
 __global__ void __launch_bounds__(RowsShape<DW, FMT>::kThreads, 1)
 attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_constant__ CUtensorMap tmap_k, const __grid_constant__ CUtensorMap tmap_v,
                     const __grid_constant__ CUtensorMap tmap_ks, const __grid_constant__ CUtensorMap tmap_vs, const KvAttnArgs a) {
@@ -220,10 +220,29 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
         // rows that only one row tile reads are marked first to go from L2
         const uint64_t policy = a.row_tiles == 1 ? l2_policy_evict_first() : l2_policy_evict_normal();
         int n = 0, parts = 0;
+        // PAGED: a step's rows come in copies of `sub` rows, which lie in one page; the table's entries of a step are asked for a step ahead.
+        constexpr int kSubs = PAGED ? S::kStep / 16 : 1;
+        const int sub = PAGED ? min(1 << a.page_shift, S::kStep) : S::kStep;
+        const int scale_step = sub == 16 ? 8 : 4;  // a copy lands on a 128-byte line: the scales of 16 rows take half of one
         for (int idx = blockIdx.x; idx < pieces.all; idx += ctas) {
             const RowsPiece p = rows_piece(a, pieces, idx, lane);
             if (elect_one()) {
                 const int bk = p.b * a.Hkv + p.kvh;
+                int entries[kSubs], entries_then[kSubs];
+                auto ask_entries = [&](int t) {
+#pragma unroll
+                    for (int i = 0; i < kSubs; ++i) {
+                        const int j = (p.first + t) * S::kStep + i * sub;
+                        entries_then[i] = i * sub < S::kStep && j < p.rows ? page_entry(a, p.b, j >> a.page_shift) : -1;
+                    }
+                };
+                if constexpr (PAGED) ask_entries(0);
+                // all copies of a step's rows (of 64 elements of them): copy(row of the step, row of the box, box)
+                auto by_pages = [&](int j0, auto copy) {
+#pragma unroll
+                    for (int i = 0; i < kSubs; ++i)
+                        if (i * sub < S::kStep) copy(i * sub, (j0 + i * sub) & ((1 << a.page_shift) - 1), page_box(a, entries[i], p.kvh));
+                };
                 if (parts > 0 && !failed && !mbar_wait_relaxed(&q_empty, (parts - 1) & 1)) failed = true;
                 if (!failed) mbar_expect_tx(&q_full, a.tile_rows * (DW * 2));
 #pragma unroll
@@ -232,11 +251,26 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 for (int t = 0; t < p.tiles && !failed; ++t) {
                     const int j0 = (p.first + t) * S::kStep;
                     const bool none = j0 >= p.rows;  // a sequence without rows
+                    if constexpr (PAGED) {
+#pragma unroll
+                        for (int i = 0; i < kSubs; ++i) entries[i] = entries_then[i];
+                        if (t + 1 < p.tiles) ask_entries(t + 1);
+                    }
                     if constexpr (kEight) {
                         const int pos = n + t, st = pos % kLoads;
                         if (pos >= kLoads && !mbar_wait_relaxed(&load_empty[st], (pos / kLoads - 1) & 1)) { failed = true; break; }
                         if (none) { mbar_arrive(&load_full[st]); continue; }
                         const uint32_t dst = smem_u32(smem + S::kLoadOff + st * S::kLoadBytes);
+                        if constexpr (PAGED) {
+                            mbar_expect_tx(&load_full[st], 2 * S::kRawBytes + 2 * S::kStep * 4);
+                            by_pages(j0, [&](int row, int y, int box) {
+                                tma_load_3d_addr_hint(dst + row * DW, &tmap_k, &load_full[st], 0, y, box, policy);
+                                tma_load_2d_addr(dst + 2 * S::kRawBytes + row * scale_step, &tmap_ks, &load_full[st], y, box);
+                                tma_load_3d_addr_hint(dst + S::kRawBytes + row * DW, &tmap_v, &load_full[st], 0, y, box, policy);
+                                tma_load_2d_addr(dst + 2 * S::kRawBytes + S::kScaleBox + row * scale_step, &tmap_vs, &load_full[st], y, box);
+                            });
+                            continue;
+                        }
                         const int x = (bk * a.Smax + j0) & ~3;
                         mbar_expect_tx(&load_full[st], 2 * S::kRawBytes + 2 * S::kScaleKeys * 4);
                         tma_load_3d_addr_hint(dst, &tmap_k, &load_full[st], 0, j0, bk, policy);
@@ -251,8 +285,13 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         } else {
                             mbar_expect_tx(&k_full[kb], S::kOpBytes);
 #pragma unroll
-                            for (int c = 0; c < DW / 64; ++c)
-                                tma_load_3d_addr_hint(smem_u32(smem + S::kKOff + kb * S::kKEach + c * S::kOpChunk), &tmap_k, &k_full[kb], c * 64, j0, bk, policy);
+                            for (int c = 0; c < DW / 64; ++c) {
+                                const uint32_t dst = smem_u32(smem + S::kKOff + kb * S::kKEach + c * S::kOpChunk);
+                                if constexpr (PAGED)
+                                    by_pages(j0, [&](int row, int y, int box) { tma_load_3d_addr_hint(dst + row * 128, &tmap_k, &k_full[kb], c * 64, y, box, policy); });
+                                else
+                                    tma_load_3d_addr_hint(dst, &tmap_k, &k_full[kb], c * 64, j0, bk, policy);
+                            }
                         }
                         if (pos >= S::kVBufs && !mbar_wait_relaxed(&v_empty[vb], (pos / S::kVBufs - 1) & 1)) { failed = true; break; }
                         if (none) {
@@ -260,8 +299,13 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                         } else {
                             mbar_expect_tx(&v_full[vb], S::kOpBytes);
 #pragma unroll
-                            for (int c = 0; c < DW / 64; ++c)
-                                tma_load_3d_addr_hint(smem_u32(smem + S::kVOff + vb * S::kVEach + c * S::kOpChunk), &tmap_v, &v_full[vb], c * 64, j0, bk, policy);
+                            for (int c = 0; c < DW / 64; ++c) {
+                                const uint32_t dst = smem_u32(smem + S::kVOff + vb * S::kVEach + c * S::kOpChunk);
+                                if constexpr (PAGED)
+                                    by_pages(j0, [&](int row, int y, int box) { tma_load_3d_addr_hint(dst + row * 128, &tmap_v, &v_full[vb], c * 64, y, box, policy); });
+                                else
+                                    tma_load_3d_addr_hint(dst, &tmap_v, &v_full[vb], c * 64, j0, bk, policy);
+                            }
                         }
                     }
                 }
@@ -365,8 +409,11 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                 if (warp < 12) {
                     float* sc = reinterpret_cast<float*>(smem + S::kScaleOff + buf * S::kScaleBytes) + (warp - 10) * S::kStep;
                     const float* from = reinterpret_cast<const float*>(smem + S::kLoadOff + st * S::kLoadBytes + 2 * S::kRawBytes + (warp - 10) * S::kScaleBox) +
-                                        (((p.b * a.Hkv + p.kvh) * a.Smax + j0) & 3);
-                    const float x0 = j0 + lane < p.rows ? from[lane] : 0.f, x1 = j0 + 32 + lane < p.rows ? from[32 + lane] : 0.f;
+                                        (PAGED ? 0 : ((p.b * a.Hkv + p.kvh) * a.Smax + j0) & 3);
+                    // PAGED, copies of 16 rows: their scales lie 32 apart
+                    const bool apart = PAGED && a.page_shift == 4;
+                    const int l0 = apart ? lane + (lane & 16) : lane, l1 = apart ? 64 + l0 : 32 + lane;
+                    const float x0 = j0 + lane < p.rows ? from[l0] : 0.f, x1 = j0 + 32 + lane < p.rows ? from[l1] : 0.f;
                     sc[lane] = x0;
                     sc[32 + lane] = x1;
                 }
@@ -697,7 +744,13 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
                     for (int i = 0; i < odds; ++i) {
                         const int u = odd_keys[i] >> 1;
                         if ((odd_keys[i] & 1) != group || !(sees >> u & 1ull)) continue;
-                        const uint16_t* v = static_cast<const uint16_t*>(a.v) + ((int64_t)(p.b * a.Hkv + p.kvh) * a.Smax + p.past + u) * a.D + d;
+                        int64_t v_row = (int64_t)(p.b * a.Hkv + p.kvh) * a.Smax + p.past + u;
+                        if constexpr (PAGED) {
+                            const int j = p.past + u, box = page_box(a, page_entry(a, p.b, j >> a.page_shift), p.kvh);
+                            if (box < 0) continue;
+                            v_row = ((int64_t)box << a.page_shift) + (j & ((1 << a.page_shift) - 1));
+                        }
+                        const uint16_t* v = static_cast<const uint16_t*>(a.v) + v_row * a.D + d;
 #pragma unroll
                         for (int k = 0; k < 32; ++k) {
                             if (d + k >= a.D) continue;
@@ -807,12 +860,13 @@ attn_kv_rows_kernel(const __grid_constant__ CUtensorMap tmap_q, const __grid_con
     if (warp == 9) tmem_dealloc(tmem, kTmemCols);
 }
 
-template <int DW, int FMT>
+template <int DW, int FMT, bool PAGED>
 int launch_attn_kv_rows(const forge_kv_cache& cache, const KvAttnArgs& a, int ctas, cudaStream_t s) {
     using S = RowsShape<DW, FMT>;
     CUtensorMap tq, tk, tv, tks = {}, tvs = {};
     const uint64_t es = S::kEight ? 1 : 2;
-    const uint32_t box[3] = {S::kEight ? (uint32_t)DW : 64u, (uint32_t)S::kStep, 1};
+    const uint32_t keys = PAGED && cache.Smax < S::kStep ? cache.Smax : S::kStep;
+    const uint32_t box[3] = {S::kEight ? (uint32_t)DW : 64u, keys, 1};
     const uint64_t dims[3] = {(uint64_t)cache.D, (uint64_t)cache.Smax, (uint64_t)cache.B * cache.Hkv};
     const uint64_t strides[2] = {(uint64_t)cache.D * es, (uint64_t)cache.Smax * cache.D * es};
     const auto encode = !S::kEight ? encode_tmap_bf16_sw128 : DW == 128 ? encode_tmap_u8_sw128 : encode_tmap_u8_sw64;
@@ -825,12 +879,14 @@ int launch_attn_kv_rows(const forge_kv_cache& cache, const KvAttnArgs& a, int ct
         if (!encode_tmap_bf16_sw128(&tq, a.q, 4, qdims, qstrides, qbox)) return FORGE_ERR_CUDA;
     }
     if (S::kEight) {
-        const uint32_t sbox[1] = {(uint32_t)S::kScaleKeys};
-        const uint64_t n[1] = {(uint64_t)cache.B * cache.Hkv * cache.Smax};
-        if (!encode_tmap_f32_plain(&tks, cache.k_scale, 1, n, nullptr, sbox) || !encode_tmap_f32_plain(&tvs, cache.v_scale, 1, n, nullptr, sbox))
+        const uint32_t sbox[2] = {PAGED ? keys : (uint32_t)S::kScaleKeys, 1};
+        const uint64_t n[2] = {PAGED ? (uint64_t)cache.Smax : (uint64_t)cache.B * cache.Hkv * cache.Smax, (uint64_t)cache.B * cache.Hkv};
+        const uint64_t row[1] = {(uint64_t)cache.Smax * 4};
+        if (!encode_tmap_f32_plain(&tks, cache.k_scale, PAGED ? 2 : 1, n, PAGED ? row : nullptr, sbox) ||
+            !encode_tmap_f32_plain(&tvs, cache.v_scale, PAGED ? 2 : 1, n, PAGED ? row : nullptr, sbox))
             return FORGE_ERR_CUDA;
     }
-    auto kernel = attn_kv_rows_kernel<DW, FMT>;
+    auto kernel = attn_kv_rows_kernel<DW, FMT, PAGED>;
     FORGE_SET_SMEM_ONCE(kernel, S::kSmem);
     FORGE_CUDA_TRY(launch_pdl(kernel, dim3(ctas), dim3(S::kThreads), S::kSmem, s, tq, tk, tv, tks, tvs, a));
     return finish_launch(1);

@@ -35,6 +35,8 @@ struct RotArgs {
     float amplitude, sin_sign;
     int half, interleaved;
     int B, Hq, Hkv, S, S_src, Smax, D, parts;
+    const int32_t* slots;            // a cache in pages: the row of token s, as page * rows of a page + place in it
+    int num_slots, page_shift;
 };
 
 template <typename T>
@@ -161,6 +163,11 @@ __global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_append_kernel(const 
         src = a.rows[token];
         if (src < 0 || src >= a.S_src) return;
     }
+    int slot = 0;
+    if (FMT != kNoCache && a.slots) {
+        slot = a.slots[token];
+        if (slot < 0 || slot >= a.num_slots) return;
+    }
     int64_t start = a.first ? a.first[b] : 0;
     if (FMT != kNoCache) start = min(max(start, (int64_t)0), (int64_t)a.Smax);
     const int64_t dst = start + s;  // the row of the cache
@@ -173,7 +180,11 @@ __global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_append_kernel(const 
     const bool in0 = d0 < a.D, in1 = d1 < a.D;
 
     const int iters = (H + RPW - 1) / RPW;
-    const int64_t cache_row = FMT == kNoCache ? 0 : ((int64_t)b * a.Hkv) * a.Smax + dst;  // of KV head 0
+    int64_t cache_row = 0, head_rows = 0;  // that of KV head 0; rows from a head to the next
+    if (FMT != kNoCache) {
+        head_rows = a.slots ? 1 << a.page_shift : a.Smax;
+        cache_row = a.slots ? ((int64_t)(slot >> a.page_shift) * a.Hkv << a.page_shift) + (slot & ((1 << a.page_shift) - 1)) : ((int64_t)b * a.Hkv) * a.Smax + dst;
+    }
     const T* const q_row = static_cast<const T*>(a.q) + b * a.qs.b + s * a.qs.s;
     const T* const k_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.k) + b * a.kst.b + src * a.kst.s;
     const T* const v_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.v) + b * a.vst.b + src * a.vst.s;
@@ -262,7 +273,7 @@ __global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_append_kernel(const 
                 if constexpr (FMT == kNoCache || FMT == kCache16) continue;
             }
             if constexpr (FMT != kNoCache) {
-                const int64_t row = cache_row + (int64_t)(is_v ? h - a.Hq - a.Hkv : h - a.Hq) * a.Smax;
+                const int64_t row = cache_row + (int64_t)(is_v ? h - a.Hq - a.Hkv : h - a.Hq) * head_rows;
                 if constexpr (FMT == kCache16) {
                     T* p = static_cast<T*>(is_v ? a.vc : a.kc) + row * a.D;
                     if (here && in0 && dst < a.Smax) Vec8<T>::store(p + d0, x[0]);
@@ -347,6 +358,8 @@ struct ReadArgs {
     Strides kst, vst;
     const int32_t *first, *counts;
     int Hkv, Smax, S, D, blocks, pieces;  // blocks of rows per (batch, head); 16-byte pieces per cached row
+    const int32_t* table;                 // a cache in pages
+    int max_pages, num_pages, page_shift;
 };
 
 template <bool F16>
@@ -380,6 +393,7 @@ __global__ void __launch_bounds__(kReadThreads) read_rows_kernel(const ReadArgs 
     float sc[kReadUnroll];
     int row[kReadUnroll], piece[kReadUnroll];
     bool ok[kReadUnroll];
+    int entry[kReadUnroll];
 #pragma unroll
     for (int u = 0; u < kReadUnroll; ++u) {
         const unsigned at = ((unsigned)block * kReadUnroll + u) * kReadThreads + threadIdx.x;
@@ -387,8 +401,14 @@ __global__ void __launch_bounds__(kReadThreads) read_rows_kernel(const ReadArgs 
         piece[u] = (int)(at - (unsigned)row[u] * (unsigned)a.pieces);
         const int64_t src = first + row[u];
         ok[u] = row[u] < count && src >= 0 && src < a.Smax;
+        if (a.table) entry[u] = ok[u] ? __ldcg(a.table + (int64_t)b * a.max_pages + (src >> a.page_shift)) : -1;
+    }
+#pragma unroll
+    for (int u = 0; u < kReadUnroll; ++u) {
+        const int64_t src = first + row[u];
+        if (a.table) ok[u] = (unsigned)entry[u] < (unsigned)a.num_pages;
         if (ok[u]) {
-            const int64_t r = (int64_t)bh * a.Smax + src;
+            const int64_t r = a.table ? (((int64_t)entry[u] * a.Hkv + h) << a.page_shift) + (src & ((1 << a.page_shift) - 1)) : (int64_t)bh * a.Smax + src;
             raw[u] = *reinterpret_cast<const uint4*>(cache + (r * a.pieces + piece[u]) * 16);
             if constexpr (FMT != kCache16) sc[u] = scales[r];
         }
@@ -424,6 +444,25 @@ int launch_read(ReadArgs& a, int B, cudaStream_t s) {
     a.blocks = (int)blocks;
     FORGE_CUDA_TRY(launch_pdl(read_rows_kernel<FMT, F16>, dim3((unsigned)(blocks * B * a.Hkv), 2), dim3(kReadThreads), 0, s, a));
     return finish_launch(1);
+}
+
+// The cache's part of `a` is set, and the other arguments are checked but for the strides.
+int read_rows(ReadArgs& a, int Hkv, int D, int format, int B, void* k_out, void* v_out, int dtype, int S, const int64_t* k_strides,
+              const int64_t* v_strides, const int32_t* first, const int32_t* counts, void* stream) {
+    int st;
+    if ((st = check_strides(k_strides, Hkv, S, D, &a.kst)) != FORGE_OK) return st;
+    if ((st = check_strides(v_strides, Hkv, S, D, &a.vst)) != FORGE_OK) return st;
+    a.k_out = k_out; a.v_out = v_out;
+    a.first = first; a.counts = counts;
+    a.Hkv = Hkv; a.S = S; a.D = D;
+    a.pieces = eight_bit(format) ? D / 16 : D / 8;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const bool f16 = dtype == FORGE_DTYPE_F16;
+    switch (format) {
+        case FORGE_KV_INT8: return f16 ? launch_read<kCacheInt8, true>(a, B, s) : launch_read<kCacheInt8, false>(a, B, s);
+        case FORGE_KV_E4M3: return f16 ? launch_read<kCacheE4m3, true>(a, B, s) : launch_read<kCacheE4m3, false>(a, B, s);
+        default: return launch_read<kCache16, false>(a, B, s);
+    }
 }
 
 }  // namespace
@@ -553,19 +592,73 @@ extern "C" int forge_kv_read(const forge_kv_cache* cache, void* k_out, void* v_o
     if (st != FORGE_OK) return st;
     if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || S <= 0 || misaligned4(first) || misaligned4(counts)) return FORGE_ERR_INVALID_ARG;
     ReadArgs a = {};
-    if ((st = check_strides(k_strides, cache->Hkv, S, cache->D, &a.kst)) != FORGE_OK) return st;
-    if ((st = check_strides(v_strides, cache->Hkv, S, cache->D, &a.vst)) != FORGE_OK) return st;
     a.kc = cache->k; a.vc = cache->v;
     a.ks = cache->k_scale; a.vs = cache->v_scale;
-    a.k_out = k_out; a.v_out = v_out;
-    a.first = first; a.counts = counts;
-    a.Hkv = cache->Hkv; a.Smax = cache->Smax; a.S = S; a.D = cache->D;
-    a.pieces = eight_bit(cache->format) ? cache->D / 16 : cache->D / 8;
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
-    const bool f16 = dtype == FORGE_DTYPE_F16;
-    switch (cache->format) {
-        case FORGE_KV_INT8: return f16 ? launch_read<kCacheInt8, true>(a, cache->B, s) : launch_read<kCacheInt8, false>(a, cache->B, s);
-        case FORGE_KV_E4M3: return f16 ? launch_read<kCacheE4m3, true>(a, cache->B, s) : launch_read<kCacheE4m3, false>(a, cache->B, s);
-        default: return launch_read<kCache16, false>(a, cache->B, s);
+    a.Smax = cache->Smax;
+    return read_rows(a, cache->Hkv, cache->D, cache->format, cache->B, k_out, v_out, dtype, S, k_strides, v_strides, first, counts, stream);
+}
+
+extern "C" int forge_kv_append_pages(const forge_kv_pages* cache, const forge_kv_append_pages_desc* desc, void* stream) {
+    using namespace forge;
+    if (!desc) return FORGE_ERR_INVALID_ARG;
+    const forge_kv_append_pages_desc& d = *desc;
+    int st = check_pages(cache, d.dtype);
+    if (st != FORGE_OK) return st;
+    if (!d.k || !d.v || !aligned16(d.k) || !aligned16(d.v) || !d.slots || d.T <= 0) return FORGE_ERR_INVALID_ARG;
+    if (misaligned4(d.slots) || misaligned4(d.positions) || (d.rotary && !d.positions)) return FORGE_ERR_INVALID_ARG;
+    RotArgs a = {};
+    if (d.rotary && (st = check_rotary(d.rotary, cache->D)) != FORGE_OK) return st;
+    // {token, head} strides as those of one sequence
+    auto strides = [&](const int64_t* in, int H, Strides* out) {
+        const int64_t given[3] = {8, in ? in[1] : cache->D, in ? in[0] : (int64_t)H * cache->D};
+        const int st = check_strides(given, H, d.T, cache->D, out);
+        out->b = 0;
+        return st;
+    };
+    if ((st = strides(d.k_strides, cache->Hkv, &a.kst)) != FORGE_OK) return st;
+    if ((st = strides(d.v_strides, cache->Hkv, &a.vst)) != FORGE_OK) return st;
+    if (d.q) {
+        if (!d.q_out || !d.rotary || d.Hq <= 0 || !aligned16(d.q) || !aligned16(d.q_out)) return FORGE_ERR_INVALID_ARG;
+        if (d.Hq > 65535) return FORGE_ERR_UNSUPPORTED;
+        if ((st = strides(d.q_strides, d.Hq, &a.qs)) != FORGE_OK) return st;
+        if ((st = strides(d.q_out_strides, d.Hq, &a.qos)) != FORGE_OK) return st;
+        if (d.q == d.q_out && (a.qs.h != a.qos.h || a.qs.s != a.qos.s)) return FORGE_ERR_INVALID_ARG;
+    } else if (d.q_out) {
+        return FORGE_ERR_INVALID_ARG;
     }
+    a.q = d.q; a.k = d.k; a.v = d.v;
+    a.q_out = d.q_out;
+    a.kc = cache->k; a.vc = cache->v;
+    a.ks = cache->k_scale; a.vs = cache->v_scale;
+    a.positions = d.positions;
+    a.B = 1;
+    a.Hq = d.q ? d.Hq : 0;
+    a.Hkv = cache->Hkv;
+    a.S = a.S_src = d.T;
+    a.Smax = 0x7fffffff;
+    a.D = cache->D;
+    a.slots = d.slots;
+    a.num_slots = cache->num_pages * cache->page_size;
+    a.page_shift = log2_of(cache->page_size);
+    if (d.rotary) set_rotary(a, *d.rotary, 0);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return d.dtype == FORGE_DTYPE_F16 ? dispatch_append<__half>(cache->format, a, s) : dispatch_append<__nv_bfloat16>(cache->format, a, s);
+}
+
+extern "C" int forge_kv_read_pages(const forge_kv_pages* cache, const int32_t* table, int B, int max_pages, void* k_out, void* v_out, int dtype,
+                                   int S, const int64_t* k_strides, const int64_t* v_strides, const int32_t* first, const int32_t* counts,
+                                   void* stream) {
+    using namespace forge;
+    int st = check_pages(cache, dtype);
+    ReadArgs a = {};
+    if (st != FORGE_OK) return st;
+    if ((st = check_table(table, B, max_pages, cache->page_size, &a.Smax)) != FORGE_OK) return st;
+    if (!k_out || !v_out || !aligned16(k_out) || !aligned16(v_out) || S <= 0 || misaligned4(first) || misaligned4(counts)) return FORGE_ERR_INVALID_ARG;
+    a.kc = cache->k; a.vc = cache->v;
+    a.ks = cache->k_scale; a.vs = cache->v_scale;
+    a.table = table;
+    a.max_pages = max_pages;
+    a.num_pages = cache->num_pages;
+    a.page_shift = log2_of(cache->page_size);
+    return read_rows(a, cache->Hkv, cache->D, cache->format, B, k_out, v_out, dtype, S, k_strides, v_strides, first, counts, stream);
 }

@@ -10,9 +10,10 @@ namespace forge {
 
 inline bool eight_bit(int format) { return format == FORGE_KV_INT8 || format == FORGE_KV_E4M3; }
 
-// A cache and the activations' type that goes with it.
-inline int check_cache(const forge_kv_cache* c, int dtype) {
-    if (!c || !c->k || !c->v || c->B <= 0 || c->Hkv <= 0 || c->Smax <= 0 || c->D <= 0) return FORGE_ERR_INVALID_ARG;
+// What a cache's rows are, and the activations' type that goes with them.
+template <typename Cache>
+inline int check_rows(const Cache* c, int dtype) {
+    if (!c->k || !c->v || c->Hkv <= 0 || c->D <= 0) return FORGE_ERR_INVALID_ARG;
     if (c->format < FORGE_KV_BF16 || c->format > FORGE_KV_E4M3) return FORGE_ERR_INVALID_ARG;
     if (dtype != FORGE_DTYPE_BF16 && dtype != FORGE_DTYPE_F16) return dtype == FORGE_DTYPE_F32 ? FORGE_ERR_UNSUPPORTED : FORGE_ERR_INVALID_ARG;
     if (!aligned16(c->k) || !aligned16(c->v)) return FORGE_ERR_INVALID_ARG;
@@ -22,9 +23,40 @@ inline int check_cache(const forge_kv_cache* c, int dtype) {
     } else if (dtype != (c->format == FORGE_KV_F16 ? FORGE_DTYPE_F16 : FORGE_DTYPE_BF16)) {
         return FORGE_ERR_INVALID_ARG;
     }
-    if (c->D > 128 || c->D % 8 != 0 || c->B > 65535 || c->Hkv > 65535) return FORGE_ERR_UNSUPPORTED;
+    return c->D > 128 || c->D % 8 != 0 || c->Hkv > 65535 ? FORGE_ERR_UNSUPPORTED : FORGE_OK;
+}
+inline int check_cache(const forge_kv_cache* c, int dtype) {
+    if (!c || c->B <= 0 || c->Smax <= 0) return FORGE_ERR_INVALID_ARG;
+    const int st = check_rows(c, dtype);
+    if (st != FORGE_OK) return st;
+    if (c->B > 65535) return FORGE_ERR_UNSUPPORTED;
     // rows of the whole cache are counted in 32 bits (their elements are not)
     if ((long long)c->B * c->Hkv * (((long long)c->Smax + 127) / 128 * 128) >= (1LL << 31)) return FORGE_ERR_UNSUPPORTED;
+    return FORGE_OK;
+}
+
+// A page's rows: a power of two, so that a row's page and its place there are bits of its number, and at least what one copy of the attention brings.
+constexpr int kLeastPage = 16, kLargestPage = 1 << 20;
+inline bool page_size_ok(int p) { return p >= kLeastPage && p <= kLargestPage && (p & (p - 1)) == 0; }
+inline int log2_of(int p) {
+    int n = 0;
+    while (1 << n < p) ++n;
+    return n;
+}
+inline int check_pages(const forge_kv_pages* c, int dtype) {
+    if (!c || c->num_pages <= 0 || c->page_size <= 0) return FORGE_ERR_INVALID_ARG;
+    const int st = check_rows(c, dtype);
+    if (st != FORGE_OK) return st;
+    if (!page_size_ok(c->page_size)) return FORGE_ERR_UNSUPPORTED;
+    // rows of the whole cache are counted in 32 bits (their elements are not)
+    if ((long long)c->num_pages * c->page_size >= (1LL << 31) / c->Hkv) return FORGE_ERR_UNSUPPORTED;
+    return FORGE_OK;
+}
+// A table of B requests; `rows` that a request may have.
+inline int check_table(const int32_t* table, int B, int max_pages, int page_size, int* rows) {
+    if (!table || (reinterpret_cast<uintptr_t>(table) & 3u) || B <= 0 || max_pages <= 0) return FORGE_ERR_INVALID_ARG;
+    if (B > 65535 || (long long)max_pages * page_size > (1LL << 30)) return FORGE_ERR_UNSUPPORTED;
+    *rows = max_pages * page_size;
     return FORGE_OK;
 }
 
