@@ -443,7 +443,8 @@ typedef struct forge_kv_pages {
  * 0 .. max_pages * page_size) of each request: the pages it needs beyond the ceil(lens[b] / page_size) that it has come from the free ones,
  * in the order of the requests, and into its row of the table.  A request gets all its rows or none:
  *   none, where its table or T has no room for them; the others still may;
- *   none, where it needs pages and there are too few; so does every later request that needs any.
+ *   none, where it needs pages and there are too few; nor does any later request that needs some.
+ * What they got goes into `out` (HOST memory, its pointers DEVICE):
  *   new_lens  int32 [B]      lens[b] + counts[b], or lens[b] where it got none.  May be lens itself.
  *   starts    int32 [B + 1]  where each request's tokens begin: running sums of counts, refused requests' too, at most T.  May be NULL.
  *   slots     int32 [T]      the slot of each token's row; -1 for tokens of refused requests and behind the last one
@@ -460,8 +461,12 @@ typedef struct forge_kv_page_tables {
     int32_t *table, *free_pages, *free_count;
     int B, max_pages, page_size, num_pages;
 } forge_kv_page_tables;
-int forge_kv_assign_pages(const forge_kv_page_tables* tables, const int32_t* lens, const int32_t* counts, int T, int32_t* new_lens,
-                          int32_t* starts, int32_t* slots, int32_t* positions, int32_t* requests, int32_t* free_left, void* stream);
+typedef struct forge_kv_page_slots {
+    int32_t *new_lens, *starts, *slots, *positions, *requests;
+    int T;
+} forge_kv_page_slots;
+int forge_kv_assign_pages(const forge_kv_page_tables* tables, const int32_t* lens, const int32_t* counts, const forge_kv_page_slots* out,
+                          int32_t* free_left, void* stream);
 int forge_kv_release_pages(const forge_kv_page_tables* tables, const int32_t* lens, const int32_t* done, int32_t* free_left, void* stream);
 
 /*

@@ -133,6 +133,11 @@ class PageTablesDesc(ctypes.Structure):
                 ("num_pages", _i)]
 
 
+class PageSlotsDesc(ctypes.Structure):
+    """forge_kv_page_slots"""
+    _fields_ = [("new_lens", _vp), ("starts", _vp), ("slots", _vp), ("positions", _vp), ("requests", _vp), ("T", _i)]
+
+
 class KVAppendPagesDesc(ctypes.Structure):
     """forge_kv_append_pages_desc"""
     _fields_ = [("k", _vp), ("v", _vp), ("q", _vp), ("q_out", _vp),
@@ -148,7 +153,7 @@ class AdaptersDesc(ctypes.Structure):
 
 _i64 = ctypes.c_int64
 SIGNATURES.update({
-    "forge_kv_assign_pages": (_i, [ctypes.POINTER(PageTablesDesc), _vp, _vp, _i, _vp, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "forge_kv_assign_pages": (_i, [ctypes.POINTER(PageTablesDesc), _vp, _vp, ctypes.POINTER(PageSlotsDesc), _vp, _vp]),
     "forge_kv_release_pages": (_i, [ctypes.POINTER(PageTablesDesc), _vp, _vp, _vp, _vp]),
     "forge_kv_append_pages": (_i, [ctypes.POINTER(KVPagesDesc), ctypes.POINTER(KVAppendPagesDesc), _vp]),
     "forge_kv_read_pages": (_i, [ctypes.POINTER(KVPagesDesc), _vp, _i, _i, _vp, _vp, _i, _i, _vp, _vp, _vp, _vp, _vp]),
@@ -166,6 +171,9 @@ _HOST_CALLS_ENTRIES = ("forge_attn_fused", "forge_attn_fused_f16", "forge_attn_f
                        "forge_attn_decode_splitkv_f16", "forge_linear_act", "forge_linear_act_f16", "forge_linear_act_w8a16",
                        "forge_linear_swiglu")
 _HOST_CALLS_KV_ENTRIES = ("forge_rotary_apply", "forge_kv_append", "forge_kv_read", "forge_attn_decode_kv", "forge_attn_tree")
+
+_HOST_CALLS_PAGES_ENTRIES = ("forge_kv_assign_pages", "forge_kv_append_pages", "forge_kv_read_pages", "forge_attn_decode_pages",
+                             "forge_attn_tree_pages", "forge_linear_adapters")
 
 
 class ForgeError(RuntimeError):
@@ -204,6 +212,7 @@ def _bind_host_calls(lib) -> None:
     if getattr(host_calls, "built_for", None) != host_calls_stamp():
         return
     host_calls.bind(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _HOST_CALLS_ENTRIES))
+    host_calls.bind_pages(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _HOST_CALLS_PAGES_ENTRIES))
     host_calls.bind_kv(*(ctypes.cast(getattr(lib, name), ctypes.c_void_p).value for name in _HOST_CALLS_KV_ENTRIES))
     _host_calls = host_calls
 
@@ -799,12 +808,12 @@ class PageSlots:
         B, T = lens.numel(), slots.numel()
         self.lens, self.starts, self.slots, self.positions, self.requests, self.B, self.T = lens, starts, slots, positions, requests, B, T
         i32 = torch.int32
-        self.pointers = (_dev_or_none(lens, i32, "lens", (B,)), _dev_or_none(starts, i32, "starts", (B + 1,)),
-                         _dev_or_none(slots, i32, "slots", (T,)), _dev_or_none(positions, i32, "positions", (T,)),
-                         _dev_or_none(requests, i32, "requests", (T,)))
+        self.desc = PageSlotsDesc(new_lens=_dev_or_none(lens, i32, "lens", (B,)), starts=_dev_or_none(starts, i32, "starts", (B + 1,)),
+                                  slots=_dev_or_none(slots, i32, "slots", (T,)), positions=_dev_or_none(positions, i32, "positions", (T,)),
+                                  requests=_dev_or_none(requests, i32, "requests", (T,)), T=T)
         if len({t.device for t in (lens, starts, slots, positions, requests) if t is not None}) != 1:
             raise ValueError("the tensors of a step must be on one device")
-        self.device = lens.device.index
+        self.address, self.device = ctypes.addressof(self.desc), lens.device.index
 
     @classmethod
     def empty(cls, B, T, device="cuda"):
@@ -815,14 +824,18 @@ def assign_pages(tables, lens, out, counts=None, free_left=None):
     """forge_kv_assign_pages: room for counts[b] (int32 [B]; None: one) more rows behind the lens[b] (int32 [B]) rows of each request.  What
     they got goes into `out`, a PageSlots whose T is the tokens that there is room for; out.lens may be lens.  free_left int32 [1]: where the
     number of pages left goes (None: into tables.free_count).  Returns out."""
+    if _host_calls is not None:
+        st = _host_calls.assign_pages(tables.address, tables.device, lens, counts, out.address, out.device, out.B, free_left)
+        if st >= 0:
+            _check("forge_kv_assign_pages", st)
+            return out
     if out.B != tables.B:
         raise ValueError("out: a PageSlots of the tables' B expected")
     i32 = torch.int32
     lp, cp = _dev_or_none(lens, i32, "lens", (tables.B,)), _dev_or_none(counts, i32, "counts", (tables.B,))
     fp = _dev_or_none(free_left, i32, "free_left", (1,))
     _on_current(tables.table, out.lens, lens, counts, free_left)
-    o = out.pointers
-    _check("forge_kv_assign_pages", load().forge_kv_assign_pages(tables.desc, lp, cp, out.T, o[0], o[1], o[2], o[3], o[4], fp, _stream()))
+    _check("forge_kv_assign_pages", load().forge_kv_assign_pages(tables.desc, lp, cp, out.desc, fp, _stream()))
     return out
 
 
@@ -850,6 +863,12 @@ def kv_append_pages(cache, k, v, slots, positions=None, rotary=None, q=None, q_o
     """forge_kv_append_pages: k, v [T,Hkv,D] views (bf16 or fp16) of packed tokens become rows slots[t] (int32 [T]) of a KVPages, k rotated
     first by positions[t] (int32 [T]) if `rotary` is given; q [T,Hq,D] is rotated into q_out in the same launch.  Returns q_out
     (None without q)."""
+    if _host_calls is not None:
+        st = _host_calls.append_pages(cache.address, cache.device, k, v, slots, positions, None if rotary is None else rotary.address,
+                                      None if rotary is None else rotary.device, q, q_out)
+        if st >= 0:
+            _check("forge_kv_append_pages", st)
+            return q_out
     if k.dim() != 3 or k.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError("k [T,Hkv,D] in bf16 or fp16 expected")
     T, H, D = k.shape
@@ -884,6 +903,11 @@ def _table(table):
 
 def kv_read_pages(cache, table, k_out, v_out, first=None, counts=None):
     """forge_kv_read_pages: kv_read of a KVPages through table int32 [B,max_pages]."""
+    if _host_calls is not None:
+        st = _host_calls.read_pages(cache.address, cache.device, table, k_out, v_out, first, counts)
+        if st >= 0:
+            _check("forge_kv_read_pages", st)
+            return k_out, v_out
     tp, B, max_pages = _table(table)
     if k_out.dim() != 4 or k_out.dtype not in (torch.bfloat16, torch.float16):
         raise ValueError("k_out [B,Hkv,S,D] in bf16 or fp16 expected")
@@ -906,6 +930,11 @@ def _pages_workspace(workspace, cache, B, Hq, T, device):
 
 def attn_decode_pages(q, cache, table, lens, scale=None, out=None, workspace=None):
     """forge_attn_decode_pages: attn_decode_kv over a KVPages, the rows of request b in the pages of table[b] (int32 [B,max_pages])."""
+    if _host_calls is not None:
+        st = _host_calls.decode_pages(cache.address, cache.device, q, table, lens, scale, out, workspace)
+        if st >= 0:
+            _check("forge_attn_decode_pages", st)
+            return out
     tp, B, max_pages = _table(table)
     if q.dim() != 3 or (q.shape[0], q.shape[2]) != (B, cache.D):
         raise ValueError("q [B,Hq,D] of the table's B and the cache's D expected")
@@ -926,6 +955,11 @@ def attn_decode_pages(q, cache, table, lens, scale=None, out=None, workspace=Non
 
 def attn_tree_pages(q, cache, table, lens, tree=None, scale=None, out=None, workspace=None):
     """forge_attn_tree_pages: attn_tree over a KVPages, the rows of request b in the pages of table[b] (int32 [B,max_pages])."""
+    if _host_calls is not None:
+        st = _host_calls.tree_pages(cache.address, cache.device, q, table, lens, tree, scale, out, workspace)
+        if st >= 0:
+            _check("forge_attn_tree_pages", st)
+            return out
     tp, B, max_pages = _table(table)
     if q.dim() != 4 or (q.shape[0], q.shape[3]) != (B, cache.D):
         raise ValueError("q [B,Hq,T,D] of the table's B and the cache's D expected")
@@ -960,6 +994,11 @@ def linear_adapters(x, y, a, b, adapters, requests=None, scales=None, out=None):
     """forge_linear_adapters: y + scales[i] * (x A_i^T) B_i^T with i = adapters[requests[t]] (requests None: adapters[t]); x [T,K] and
     y, out [T,N] views with contiguous rows, a [n,rank,K], b [n,N,rank], all bf16 or fp16; adapters int32 [R], requests int32 [T], scales
     fp32 [n] or None.  Tokens without an adapter (-1) keep y.  out may be y itself."""
+    if _host_calls is not None:
+        st = _host_calls.adapters(x, y, a, b, adapters, requests, scales, out)
+        if st >= 0:
+            _check("forge_linear_adapters", st)
+            return out
     if x.dim() != 2 or y.dim() != 2 or a.dim() != 3 or b.dim() != 3 or adapters.dim() != 1:
         raise ValueError("x [T,K], y [T,N], a [n,rank,K], b [n,N,rank], adapters [R] expected")
     if x.dtype not in (torch.bfloat16, torch.float16):

@@ -200,17 +200,17 @@ struct KvEntries {
 bool kv_bound = false;
 bool kv_ready(Py_ssize_t n, Py_ssize_t want) { return kv_bound && ready(n, want); }
 
-// A [B,H,S,D] tensor of `type` with contiguous rows, plain but for its strides; these as {batch, head, token}, where a dimension of size
-// 1 gets one that the library takes.
-const at::Tensor* plain_view(PyObject* o, at::ScalarType type, int64_t* strides) {
+// A tensor of `type` of `dims` dimensions ([B,H,S,D], [T,H,D], [T,N]) with contiguous rows, plain but for its strides; these in order, where a
+// dimension of size 1 gets one that the library takes.
+const at::Tensor* plain_view(PyObject* o, at::ScalarType type, int64_t* strides, int dims = 4) {
     if (!THPVariable_CheckExact(o)) return nullptr;
     const at::Tensor& t = THPVariable_Unpack(o);
     static const uint64_t dense = c10::DispatchKeySet({c10::DispatchKey::CUDA, c10::DispatchKey::AutogradCUDA,
                                                        c10::DispatchKey::ADInplaceOrView, c10::DispatchKey::AutocastCUDA}).raw_repr();
-    if (!t.defined() || (t.key_set().raw_repr() & ~dense) != 0 || !t.is_cuda() || t.scalar_type() != type || t.dim() != 4) return nullptr;
+    if (!t.defined() || (t.key_set().raw_repr() & ~dense) != 0 || !t.is_cuda() || t.scalar_type() != type || t.dim() != dims) return nullptr;
     const auto n = t.sizes(), st = t.strides();
-    if (st[3] != 1) return nullptr;
-    for (int i = 0; i < 3; ++i) strides[i] = n[i] > 1 ? st[i] : 8;
+    if (st[dims - 1] != 1) return nullptr;
+    for (int i = 0; i < dims - 1; ++i) strides[i] = n[i] > 1 ? st[i] : 8;
     return &t;
 }
 bool is_16_bit(PyObject* o, at::ScalarType* type) {
@@ -376,6 +376,200 @@ PyObject* py_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// ---- a step of many requests
+struct PagesEntries {
+    decltype(&forge_kv_assign_pages) assign;
+    decltype(&forge_kv_append_pages) append;
+    decltype(&forge_kv_read_pages) read;
+    decltype(&forge_attn_decode_pages) decode;
+    decltype(&forge_attn_tree_pages) tree;
+    decltype(&forge_linear_adapters) adapters;
+} pages;
+bool pages_bound = false;
+bool pages_ready(Py_ssize_t n, Py_ssize_t want) { return pages_bound && ready(n, want); }
+const int32_t* ints(const at::Tensor* t) { return static_cast<const int32_t*>(address(t)); }
+
+// assign_pages(tables, device, lens, counts, slots, their device, their B, free_left)
+PyObject* py_assign_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_page_tables* t;
+        const forge_kv_page_slots* out;
+        int B;
+        bool no_c, no_f;
+        if (!pages_ready(n, 8) || !handle(a[0], a[1], &t) || !handle(a[4], a[5], &out) || !as_int(a[6], &B) || B != t->B) return not_plain();
+        const at::Tensor *lens = plain(a[2], at::kInt, 1), *c = plain_or_none(a[3], at::kInt, 1, &no_c), *f = plain_or_none(a[7], at::kInt, 1, &no_f);
+        if (!lens || (!c && !no_c) || (!f && !no_f) || !sized(lens, B) || !sized(c, B) || !sized(f, 1) || !here({lens, c, f})) return not_plain();
+        const int32_t *pl = ints(lens), *pc = ints(c);
+        int32_t* pf = static_cast<int32_t*>(address(f));
+        void* s = stream();
+        return run([&] { return pages.assign(t, pl, pc, out, pf, s); });
+    });
+}
+
+// append_pages(cache, device, k, v, slots, positions, rotary or None, its device, q or None, q_out or None)
+PyObject* py_append_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_pages* cache;
+        at::ScalarType ty;
+        if (!pages_ready(n, 10) || !handle(a[0], a[1], &cache) || !is_16_bit(a[2], &ty)) return not_plain();
+        forge_kv_append_pages_desc d = {};
+        int64_t ks[2], vs[2], qs[2], qos[2];
+        bool no_p;
+        const at::Tensor *k = plain_view(a[2], ty, ks, 3), *v = plain_view(a[3], ty, vs, 3), *slots = plain(a[4], at::kInt, 1);
+        const at::Tensor *p = plain_or_none(a[5], at::kInt, 1, &no_p), *q = nullptr, *qo = nullptr;
+        if (!k || !v || !slots || (!p && !no_p)) return not_plain();
+        if (a[6] != Py_None && !handle(a[6], a[7], &d.rotary)) return not_plain();
+        const auto sz = k->sizes();
+        if (sz[1] != cache->Hkv || sz[2] != cache->D || v->sizes() != sz || !small(sz[0], &d.T)) return not_plain();
+        if (a[8] != Py_None) {
+            q = plain_view(a[8], ty, qs, 3);
+            qo = plain_view(a[9], ty, qos, 3);
+            if (!q || !qo || qo->sizes() != q->sizes() || q->size(0) != sz[0] || q->size(2) != sz[2] || !small(q->size(1), &d.Hq)) return not_plain();
+            d.q = address(q);
+            d.q_out = address(qo);
+            d.q_strides = qs;
+            d.q_out_strides = qos;
+        } else if (a[9] != Py_None) {
+            return not_plain();
+        }
+        if (!sized(slots, sz[0]) || !sized(p, sz[0]) || !here({k, v, q, qo, slots, p})) return not_plain();
+        d.k = address(k);
+        d.v = address(v);
+        d.k_strides = ks;
+        d.v_strides = vs;
+        d.slots = ints(slots);
+        d.positions = ints(p);
+        d.dtype = dtype_of(ty);
+        void* s = stream();
+        return run([&] { return pages.append(cache, &d, s); });
+    });
+}
+
+// The table's sizes.
+bool table_sizes(const at::Tensor* t, int* B, int* max_pages) { return t && small(t->size(0), B) && small(t->size(1), max_pages); }
+
+// read_pages(cache, device, table, k_out, v_out, first, counts)
+PyObject* py_read_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_pages* cache;
+        at::ScalarType ty;
+        int S, B, columns;
+        bool no_f, no_c;
+        int64_t ks[3], vs[3];
+        if (!pages_ready(n, 7) || !handle(a[0], a[1], &cache) || !is_16_bit(a[3], &ty)) return not_plain();
+        const at::Tensor *t = plain(a[2], at::kInt, 2), *k = plain_view(a[3], ty, ks), *v = plain_view(a[4], ty, vs);
+        const at::Tensor *f = plain_or_none(a[5], at::kInt, 1, &no_f), *c = plain_or_none(a[6], at::kInt, 1, &no_c);
+        if (!table_sizes(t, &B, &columns) || !k || !v || (!f && !no_f) || (!c && !no_c)) return not_plain();
+        const auto sz = k->sizes();
+        if (sz[0] != B || sz[1] != cache->Hkv || sz[3] != cache->D || v->sizes() != sz || !small(sz[2], &S) || !sized(f, B) || !sized(c, B) ||
+            !here({t, k, v, f, c}))
+            return not_plain();
+        void *pk = address(k), *pv = address(v), *s = stream();
+        const int32_t *pt = ints(t), *pf = ints(f), *pc = ints(c);
+        return run([&] { return pages.read(cache, pt, B, columns, pk, pv, dtype_of(ty), S, ks, vs, pf, pc, s); });
+    });
+}
+
+// decode_pages(cache, device, q, table, lens, scale, out, workspace)
+PyObject* py_decode_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_pages* cache;
+        at::ScalarType ty;
+        int Hq, B, columns;
+        float scale;
+        if (!pages_ready(n, 8) || !handle(a[0], a[1], &cache) || !is_16_bit(a[2], &ty) || !as_scale(a[5], cache->D, &scale)) return not_plain();
+        const at::Tensor *q = plain(a[2], ty, 3), *t = plain(a[3], at::kInt, 2), *lens = plain(a[4], at::kInt, 1);
+        const at::Tensor *out = plain(a[6], ty, 3), *ws = plain(a[7], at::kByte, 1);
+        if (!q || !table_sizes(t, &B, &columns) || !lens || !out || !ws) return not_plain();
+        const auto sz = q->sizes();
+        if (sz[0] != B || sz[2] != cache->D || out->sizes() != sz || !small(sz[1], &Hq) || !sized(lens, B) || !here({q, t, lens, out, ws}))
+            return not_plain();
+        void *pq = address(q), *po = address(out), *pw = address(ws), *s = stream();
+        const int32_t *pt = ints(t), *pl = ints(lens);
+        const size_t bytes = (size_t)ws->numel();
+        return run([&] { return pages.decode(cache, pt, B, columns, pq, po, dtype_of(ty), Hq, pl, scale, pw, bytes, s); });
+    });
+}
+
+// tree_pages(cache, device, q, table, lens, tree or None, scale, out, workspace)
+PyObject* py_tree_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        const forge_kv_pages* cache;
+        at::ScalarType ty;
+        int Hq, T, B, columns, tree_B = 1;
+        float scale;
+        bool no_t;
+        int64_t qs[3], os[3];
+        if (!pages_ready(n, 9) || !handle(a[0], a[1], &cache) || !is_16_bit(a[2], &ty) || !as_scale(a[6], cache->D, &scale)) return not_plain();
+        const at::Tensor *q = plain_view(a[2], ty, qs), *t = plain(a[3], at::kInt, 2), *lens = plain(a[4], at::kInt, 1);
+        const at::Tensor *tree = plain_or_none(a[5], at::kLong, 2, &no_t), *out = plain_view(a[7], ty, os), *ws = plain(a[8], at::kByte, 1);
+        if (!q || !table_sizes(t, &B, &columns) || !lens || (!tree && !no_t) || !out || !ws) return not_plain();
+        const auto sz = q->sizes();
+        if (sz[0] != B || sz[3] != cache->D || out->sizes() != sz || !small(sz[1], &Hq) || !small(sz[2], &T) || !sized(lens, B) ||
+            !here({q, t, out, lens, tree, ws}))
+            return not_plain();
+        if (tree) {
+            if (tree->size(1) != sz[2] || (tree->size(0) != 1 && tree->size(0) != B)) return not_plain();
+            tree_B = (int)tree->size(0);
+        }
+        void *pq = address(q), *po = address(out), *pw = address(ws), *s = stream();
+        const int32_t *pt = ints(t), *pl = ints(lens);
+        const int64_t* pm = static_cast<const int64_t*>(address(tree));
+        const size_t bytes = (size_t)ws->numel();
+        return run([&] { return pages.tree(cache, pt, B, columns, pq, po, dtype_of(ty), Hq, T, qs, os, pl, pm, tree_B, scale, pw, bytes, s); });
+    });
+}
+
+// adapters(x, y, a, b, adapters, requests or None, scales or None, out)
+PyObject* py_adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded([&]() -> PyObject* {
+        at::ScalarType ty;
+        forge_adapters d = {};
+        int T, R;
+        bool no_r, no_s;
+        int64_t xs[1], ys[1], os[1];
+        if (!pages_ready(n, 8) || !is_16_bit(a[0], &ty)) return not_plain();
+        const at::Tensor *x = plain_view(a[0], ty, xs, 2), *y = plain_view(a[1], ty, ys, 2), *out = plain_view(a[7], ty, os, 2);
+        const at::Tensor *wa = plain(a[2], ty, 3), *wb = plain(a[3], ty, 3), *ad = plain(a[4], at::kInt, 1);
+        const at::Tensor *r = plain_or_none(a[5], at::kInt, 1, &no_r), *sc = plain_or_none(a[6], at::kFloat, 1, &no_s);
+        if (!x || !y || !out || !wa || !wb || !ad || (!r && !no_r) || (!sc && !no_s)) return not_plain();
+        const auto as = wa->sizes(), bs = wb->sizes();
+        if (!small(x->size(0), &T) || !small(x->size(1), &d.K) || !small(y->size(1), &d.N) || !small(as[0], &d.n) || !small(as[1], &d.rank) ||
+            !small(ad->size(0), &R) || !sized(y, T) || !sized(out, T, d.N) || as[2] != d.K || bs[0] != d.n || bs[1] != d.N || bs[2] != d.rank ||
+            !sized(r, T) || !sized(sc, d.n) || (!r && R != T) || !here({x, y, out, wa, wb, ad, r, sc}))
+            return not_plain();
+        const int64_t sx = T > 1 ? xs[0] : 0, sy = T > 1 ? ys[0] : 0, so = T > 1 ? os[0] : 0;
+        d.a = address(wa);
+        d.b = address(wb);
+        d.scales = static_cast<const float*>(address(sc));
+        d.dtype = dtype_of(ty);
+        void *px = address(x), *py = address(y), *po = address(out), *s = stream();
+        const int32_t *pr = ints(r), *pa = ints(ad);
+        return run([&] { return pages.adapters(&d, px, py, po, T, sx, sy, so, pr, pa, R, s); });
+    });
+}
+
+// bind_pages(addresses of the six entry points, in the order of PagesEntries); after bind()
+PyObject* py_bind_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    void* p[6];
+    if (n != 6) { PyErr_SetString(PyExc_TypeError, "six addresses expected"); return nullptr; }
+    for (int i = 0; i < 6; ++i) {
+        p[i] = PyLong_AsVoidPtr(a[i]);
+        if (!p[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "address expected");
+            return nullptr;
+        }
+    }
+    pages.assign = reinterpret_cast<decltype(pages.assign)>(p[0]);
+    pages.append = reinterpret_cast<decltype(pages.append)>(p[1]);
+    pages.read = reinterpret_cast<decltype(pages.read)>(p[2]);
+    pages.decode = reinterpret_cast<decltype(pages.decode)>(p[3]);
+    pages.tree = reinterpret_cast<decltype(pages.tree)>(p[4]);
+    pages.adapters = reinterpret_cast<decltype(pages.adapters)>(p[5]);
+    pages_bound = true;
+    Py_RETURN_NONE;
+}
+
 // bind_kv(addresses of the five entry points, in the order of KvEntries); after bind()
 PyObject* py_bind_kv(PyObject*, PyObject* const* a, Py_ssize_t n) {
     void* p[5];
@@ -423,6 +617,9 @@ PyMethodDef methods[] = {{"attn", FAST(py_attn)},           {"decode", FAST(py_d
                          {"linear_w8", FAST(py_linear_w8)}, {"swiglu", FAST(py_swiglu)}, {"bind", FAST(py_bind)},
                          {"rotary", FAST(py_rotary)},       {"append", FAST(py_append)}, {"read", FAST(py_read)},
                          {"decode_kv", FAST(py_decode_kv)}, {"tree", FAST(py_tree)},     {"bind_kv", FAST(py_bind_kv)},
+                         {"assign_pages", FAST(py_assign_pages)}, {"append_pages", FAST(py_append_pages)}, {"read_pages", FAST(py_read_pages)},
+                         {"decode_pages", FAST(py_decode_pages)}, {"tree_pages", FAST(py_tree_pages)}, {"adapters", FAST(py_adapters)},
+                         {"bind_pages", FAST(py_bind_pages)},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "host_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -194,25 +194,25 @@ int tables_args(const forge_kv_page_tables* t, const int32_t* lens, int32_t* fre
 }  // namespace
 }  // namespace forge
 
-extern "C" int forge_kv_assign_pages(const forge_kv_page_tables* tables, const int32_t* lens, const int32_t* counts, int T, int32_t* new_lens,
-                                     int32_t* starts, int32_t* slots, int32_t* positions, int32_t* requests, int32_t* free_left,
-                                     void* stream) {
+extern "C" int forge_kv_assign_pages(const forge_kv_page_tables* tables, const int32_t* lens, const int32_t* counts,
+                                     const forge_kv_page_slots* out, int32_t* free_left, void* stream) {
     using namespace forge;
     PagesArgs a;
     const int st = tables_args(tables, lens, free_left, &a);
     if (st != FORGE_OK) return st;
-    if (!new_lens || !slots || T <= 0 || odd4(counts) || odd4(new_lens) || odd4(starts) || odd4(slots) || odd4(positions) || odd4(requests))
+    if (!out || !out->new_lens || !out->slots || out->T <= 0 || odd4(counts) || odd4(out->new_lens) || odd4(out->starts) || odd4(out->slots) ||
+        odd4(out->positions) || odd4(out->requests))
         return FORGE_ERR_INVALID_ARG;
-    if (T > 1 << 30) return FORGE_ERR_UNSUPPORTED;
+    if (out->T > 1 << 30) return FORGE_ERR_UNSUPPORTED;
     a.counts = counts;
-    a.new_lens = new_lens;
-    a.starts = starts;
-    a.slots = slots;
-    a.positions = positions;
-    a.requests = requests;
-    a.T = T;
+    a.new_lens = out->new_lens;
+    a.starts = out->starts;
+    a.slots = out->slots;
+    a.positions = out->positions;
+    a.requests = out->requests;
+    a.T = out->T;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (T < kManyTokens)
+    if (a.T < kManyTokens)
         FORGE_CUDA_TRY(launch_pdl(assign_pages_kernel<1>, dim3(1), dim3(kPagesThreads), 0, s, a));
     else
         FORGE_CUDA_TRY(launch_pdl_cluster(assign_pages_kernel<kManyCtas>, dim3(kManyCtas), dim3(kPagesThreads), 0, kManyCtas, s, a));

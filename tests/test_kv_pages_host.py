@@ -37,8 +37,8 @@ def tables(**kw):
 
 def test_assign_and_release_refusals(lib):
     def assign(t=tables(), lens=P, counts=None, T=8, new_lens=P, starts=None, slots=P, positions=None, requests=None, left=None):
-        return lib.forge_kv_assign_pages(None if t is None else ctypes.byref(t), lens, counts, T, new_lens, starts, slots, positions, requests, left,
-                                         None)
+        out = binding.PageSlotsDesc(new_lens, starts, slots, positions, requests, T)
+        return lib.forge_kv_assign_pages(None if t is None else ctypes.byref(t), lens, counts, ctypes.byref(out), left, None)
 
     def release(t=tables(), lens=P, done=P, left=None):
         return lib.forge_kv_release_pages(None if t is None else ctypes.byref(t), lens, done, left, None)
@@ -56,6 +56,7 @@ def test_assign_and_release_refusals(lib):
                dict(slots=P + 3), dict(positions=P + 2), dict(requests=P + 1)):
         assert assign(**kw) == BAD, kw
     assert assign(T=(1 << 30) + 1) == UNS
+    assert lib.forge_kv_assign_pages(ctypes.byref(tables()), P, None, None, None, None) == BAD
     assert release(done=None) == BAD and release(done=P + 2) == BAD
 
 
@@ -166,3 +167,27 @@ def test_the_binding_checks_shapes_and_places():
         binding.linear_adapters(x[:, 0].float(), x[:, 0], x, x, i32)
     with pytest.raises(ValueError):
         binding.linear_adapters(x, x, x, x, i32)
+
+
+# ------------------------------------------------------------------------------------------------------- native marshalling
+def test_what_is_not_plain_goes_the_general_way():
+    binding.load()
+    c = binding._host_calls
+    assert c is not None
+    for bad in ((), (1,) * 5, (1,) * 7, (0,) * 6, ("x",) * 6):
+        with pytest.raises((TypeError, ValueError)):
+            c.bind_pages(*bad)
+    x, i, t = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32), torch.zeros(4, 3, dtype=torch.int32)
+    ws = torch.zeros(64, dtype=torch.uint8)
+    for desc in (pages(), tables()):
+        at = ctypes.addressof(desc)
+        for dev in (0, None, "0", 1 << 40):
+            assert c.assign_pages(at, dev, i, None, at, dev, 3, None) == -1
+            assert c.append_pages(at, dev, x, x, i, None, None, None, None, None) == -1
+            assert c.read_pages(at, dev, t, x[None], x[None], None, None) == -1
+            assert c.decode_pages(at, dev, x, t, i, None, x, ws) == -1
+            assert c.tree_pages(at, dev, x[None], t, i, None, None, x[None], ws) == -1
+    assert c.adapters(x[:, 0], x[:, 0], x, x, i, None, None, x[:, 0]) == -1
+    for fn in (c.assign_pages, c.append_pages, c.read_pages, c.decode_pages, c.tree_pages, c.adapters):
+        for bad in ((), (None,), (None,) * 7, (None,) * 8, (None,) * 9, (None,) * 10, (x,) * 8, (0,) * 10):
+            assert fn(*bad) == -1
