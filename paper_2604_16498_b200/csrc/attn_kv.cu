@@ -27,6 +27,21 @@ size_t counter_bytes(size_t items) {
     return ((n > kKvCounterBytes ? n : kKvCounterBytes) + 255) & ~(size_t)255;
 }
 
+// A cache in pages: the query heads of a KV head that are worked on in parts of up to 8 rows each, on the kernel for those, although it then reads K
+// and V once for each part (all but the first from L2): how many parts, 1 where the other kernel is the one.  Measured, parts and tile of 128 rows:
+//   8-bit rows, 2 parts, 16/1 heads of 128: 2 x up to 65,536 rows 36.9 and 65.5 us, 64 x 128/8 x up to 1024 59.4 and 127; 3 parts, 8 x 96/4 x up to
+//     4096 30.7 and 34.9; 4 parts, 4 x 32/8 x 5 tokens behind up to 512 14.4 and 20.5, 4 x 256/8 x up to 4096 36.9 and 34.8
+//   16-bit rows of 64, 2 parts: 2 x 16/1 x up to 65,536 26.6 and 43.0, 64 x 128/8 x up to 1024 49.2 and 69.6; 4 parts, 4 x 256/8 x up to 4096 28.7 and 24.6
+//   16-bit rows of 128, 2 parts: 2 x 16/1 x up to 65,536 38.9 and 47.1; but 16 x 128/8 x up to 2048 43.0 and 38.9, and with 4 x 32/8 x 4 tokens
+//     45.1 and 36.9: there the rows bound it, and only few KV heads leave SMs for the parts
+int narrow_parts(const forge_kv_cache& c, int G, int T) {
+    if (G * T <= kNarrowRows) return 1;
+    const int most = eight_bit(c.format) ? 4 : c.D <= 64 || (long long)c.B * c.Hkv <= 32 ? 2 : 1;
+    for (int parts = 2; parts <= most; ++parts)
+        if (G % parts == 0 && G / parts * T <= kNarrowRows) return parts;
+    return 1;
+}
+
 // Floats of what a CTA leaves of an item: O, m and l of the rows that its kernel works on.
 size_t part_floats(long long rows, int D) { return (size_t)(rows <= kNarrowRows ? 8 : 128) * ((D <= 64 ? 64 : 128) + 4); }
 
@@ -84,6 +99,14 @@ int attn_kv(const forge_kv_cache* cache, const forge_kv_pages* pages, const int3
     if (tiles < ctas) ctas = (int)tiles;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (!pages) return run_format<false>(*cache, a, ctas, s);
+    a.page_heads = cache->Hkv;
+    if (const int parts = narrow_parts(*cache, G, T); parts > 1 && tiles * parts < (1LL << 31)) {
+        a.Hkv *= parts;
+        a.G /= parts;
+        a.rows /= parts;
+        a.part_mul = (unsigned)(((1ULL << 32) + parts - 1) / parts);
+        if (tiles * parts > ctas) ctas = tiles * parts < sms ? (int)(tiles * parts) : sms < kKvMaxCtas ? sms : kKvMaxCtas;
+    }
     a.table = table;
     a.num_pages = pages->num_pages;
     a.max_pages = cache->Smax / pages->page_size;

@@ -49,6 +49,9 @@ struct KvAttnArgs {
     // a cache in pages: the rows of a sequence are those of the pages that its row of the table names, in that order
     const int32_t* table;            // [B, max_pages]
     int max_pages, num_pages, page_shift;
+    // The heads of a KV head may be worked on as those of several KV heads with the same rows: Hkv, G and rows count these parts then.
+    int page_heads;                  // KV heads that a page has
+    unsigned part_mul;               // 2^32 / parts of a KV head, rounded up; 0: one part
 };
 
 namespace {
@@ -59,7 +62,8 @@ __device__ __forceinline__ int page_entry(const KvAttnArgs& a, int b, int page) 
     return page < a.max_pages ? __ldcg(a.table + (int64_t)b * a.max_pages + page) : -1;  // L2's: the kernel before this one may have had old ones in L1
 }
 __device__ __forceinline__ int page_box(const KvAttnArgs& a, int entry, int kvh) {
-    return (unsigned)entry < (unsigned)a.num_pages ? entry * a.Hkv + kvh : -1;
+    if (a.part_mul) kvh = (int)__umulhi((unsigned)kvh, a.part_mul);
+    return (unsigned)entry < (unsigned)a.num_pages ? entry * a.page_heads + kvh : -1;
 }
 
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {

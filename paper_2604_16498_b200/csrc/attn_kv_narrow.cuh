@@ -214,7 +214,8 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
     // ---- the warp's copies run ahead of its products, across the ends of sequences
     NarrowWalk ahead = cur;
     int issued = 0;
-    const uint64_t policy = ptx::l2_policy_evict_first();
+    // rows that several parts of a KV head's query heads read stay in L2 for the next one
+    const uint64_t policy = PAGED && a.part_mul ? ptx::l2_policy_evict_normal() : ptx::l2_policy_evict_first();
     // PAGED: 32 entries of the table, one in each lane, those of the item's pages from entries0 on; and the ones that come after them in the run, asked
     // for when the first of these is used: behind the copies in flight they are long in coming.
     int entries = -1, entries0 = 0, entries_then = -1;
