@@ -509,15 +509,19 @@ int forge_attn_tree_pages(const forge_kv_pages* cache, const int32_t* table, int
  * any order is right.  x, y, out: rows of x_stride, y_stride, out_stride elements (0: dense), multiples of 8; out may be y
  * itself with the same stride, but may not overlap it otherwise, nor x.  K, N, rank: multiples of 8, rank up to 128.
  * Sums are kept in fp32, x A_i^T times the scale to within 2^-15 of itself (bf16) or 2^-21 (fp16), and out is rounded once.  The same inputs give
- * the same bits.
+ * the same bits.  n * N and n * rank are below 2^31.
+ * workspace: at least forge_linear_adapters_workspace_bytes(T, rank) bytes, 16-byte aligned, of any contents (none below 512 tokens: NULL).  Two
+ * calls that may overlap on the GPU must not share it.
  */
 typedef struct forge_adapters {
     const void *a, *b;
     const float* scales;
     int n, rank, K, N, dtype;
 } forge_adapters;
+size_t forge_linear_adapters_workspace_bytes(int T, int rank);
 int forge_linear_adapters(const forge_adapters* set, const void* x, const void* y, void* out, int T, int64_t x_stride, int64_t y_stride,
-                          int64_t out_stride, const int32_t* requests, const int32_t* adapters, int R, void* stream);
+                          int64_t out_stride, const int32_t* requests, const int32_t* adapters, int R, void* workspace, size_t workspace_bytes,
+                          void* stream);
 
 /*
  * Buffer planning for a fixed sequence of operators (Section 4.5, "Liveness Analysis" and "Linear-Scan

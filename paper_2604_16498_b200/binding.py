@@ -160,7 +160,8 @@ SIGNATURES.update({
     "forge_attn_decode_pages": (_i, [ctypes.POINTER(KVPagesDesc), _vp, _i, _i, _vp, _vp, _i, _i, _vp, _f, _vp, _sz, _vp]),
     "forge_attn_tree_pages": (_i, [ctypes.POINTER(KVPagesDesc), _vp, _i, _i, _vp, _vp, _i, _i, _i, _vp, _vp, _vp, _vp, _i, _f, _vp, _sz,
                                    _vp]),
-    "forge_linear_adapters": (_i, [ctypes.POINTER(AdaptersDesc), _vp, _vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _i, _vp]),
+    "forge_linear_adapters": (_i, [ctypes.POINTER(AdaptersDesc), _vp, _vp, _vp, _i, _i64, _i64, _i64, _vp, _vp, _i, _vp, _sz, _vp]),
+    "forge_linear_adapters_workspace_bytes": (_sz, [_i, _i]),
 })
 
 _lib = None
@@ -173,7 +174,7 @@ _HOST_CALLS_ENTRIES = ("forge_attn_fused", "forge_attn_fused_f16", "forge_attn_f
 _HOST_CALLS_KV_ENTRIES = ("forge_rotary_apply", "forge_kv_append", "forge_kv_read", "forge_attn_decode_kv", "forge_attn_tree")
 
 _HOST_CALLS_PAGES_ENTRIES = ("forge_kv_assign_pages", "forge_kv_append_pages", "forge_kv_read_pages", "forge_attn_decode_pages",
-                             "forge_attn_tree_pages", "forge_linear_adapters")
+                             "forge_attn_tree_pages", "forge_linear_adapters", "forge_linear_adapters_workspace_bytes")
 
 
 class ForgeError(RuntimeError):
@@ -990,12 +991,17 @@ def _rows(t: torch.Tensor, dtype, name: str, shape):
     return t.data_ptr(), t.stride(0) if shape[0] > 1 else 0
 
 
-def linear_adapters(x, y, a, b, adapters, requests=None, scales=None, out=None):
+def linear_adapters_workspace_bytes(T, rank) -> int:
+    return int(load().forge_linear_adapters_workspace_bytes(T, rank))
+
+
+def linear_adapters(x, y, a, b, adapters, requests=None, scales=None, out=None, workspace=None):
     """forge_linear_adapters: y + scales[i] * (x A_i^T) B_i^T with i = adapters[requests[t]] (requests None: adapters[t]); x [T,K] and
     y, out [T,N] views with contiguous rows, a [n,rank,K], b [n,N,rank], all bf16 or fp16; adapters int32 [R], requests int32 [T], scales
-    fp32 [n] or None.  Tokens without an adapter (-1) keep y.  out may be y itself."""
+    fp32 [n] or None.  Tokens without an adapter (-1) keep y.  out may be y itself.  workspace: uint8, of any contents; without one,
+    a fresh one is allocated where the call needs it."""
     if _host_calls is not None:
-        st = _host_calls.adapters(x, y, a, b, adapters, requests, scales, out)
+        st = _host_calls.adapters(x, y, a, b, adapters, requests, scales, out, workspace)
         if st >= 0:
             _check("forge_linear_adapters", st)
             return out
@@ -1017,8 +1023,12 @@ def linear_adapters(x, y, a, b, adapters, requests=None, scales=None, out=None):
     d = AdaptersDesc(a=_dev(a, t, "a"), b=_dev(b, t, "b"), scales=_dev_or_none(scales, torch.float32, "scales", (n,)), n=n, rank=rank, K=K, N=N,
                      dtype=_DTYPES[t])
     rp, ap = _dev_or_none(requests, torch.int32, "requests", (T,)), _dev(adapters, torch.int32, "adapters")
-    _on_current(x, y, out, a, b, scales, requests, adapters)
-    _check("forge_linear_adapters", load().forge_linear_adapters(d, xp, yp, op, T, xs, ys, os_, rp, ap, R, _stream()))
+    _on_current(x, y, out, a, b, scales, requests, adapters, workspace)
+    if workspace is None:
+        need = linear_adapters_workspace_bytes(T, rank)
+        workspace = torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+    wp, wn = (None, 0) if workspace is None else (_dev(workspace, torch.uint8, "workspace"), workspace.numel())
+    _check("forge_linear_adapters", load().forge_linear_adapters(d, xp, yp, op, T, xs, ys, os_, rp, ap, R, wp, wn, _stream()))
     return out
 
 

@@ -6,7 +6,7 @@
 //     u^T(16 ranks x 8 tokens) += A(16 x 16 of K) x^T,     out^T(16 columns x 8 tokens) += B(16 x 16 ranks) u^T,
 // so a token alone costs no rows that do not exist, and A and B go from memory to the instructions' registers in 16- and 8-byte loads: the order of a
 // contraction's elements is free, and so are the output columns that a tile's rows stand for (8 side by side for a lane, 16 bytes of out).
-// Tokens of a tile with one adapter side by side form groups of up to 8.
+// A tile's tokens of one adapter form groups of up to 8.
 //   few tokens (tiles up to 8): the warps share the CTA's part of K, and add up through shared memory
 //   many: the warps share the groups, and each goes through the CTA's part of K
 // u goes into the second product as two 16-bit numbers, the rounded one and what that left, so that out is off by its own rounding alone.
@@ -25,7 +25,7 @@ namespace {
 constexpr int kAdCtas = 8;                 // of a cluster
 constexpr int kAdWarps = 8, kAdThreads = kAdWarps * 32;
 constexpr int kAdMost = 128;               // tokens of a tile
-constexpr int kTileTokens = 512;           // from how many tokens on the tensor cores' tiles of 128 are the faster ones (ranks up to 64)
+constexpr int kTileTokens = 512;           // from how many tokens on the tensor cores' tiles of 128 are the faster ones
 
 struct AdapterArgs {
     const void *x, *y, *a, *b;
@@ -62,8 +62,8 @@ __device__ __forceinline__ float2 unpack16(uint32_t w) {
 __device__ __forceinline__ uint4 load16(const void* p, bool there) { return there ? *static_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0); }
 __device__ __forceinline__ uint2 load8(const void* p, bool there) { return there ? *static_cast<const uint2*>(p) : make_uint2(0, 0); }
 
-// Tokens first .. first + n - 1 of the tile (n <= 8), which have the same adapter; -1: none.
-struct AdGroup { int16_t first, n; int adapter; };
+// n tokens of the tile (up to 8) which have the same adapter (-1: none).
+struct AdGroup { uint8_t token[8]; int n, adapter; };
 
 __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int t) {
     int i = t;
@@ -72,64 +72,131 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int t) {
     return (unsigned)i < (unsigned)a.n ? i : -1;
 }
 
-// One warp: the groups of the tile's tokens.  Returns how many.
-__device__ __forceinline__ int make_groups(const int* which, int tokens, AdGroup* groups, int lane) {
-    int count = 0, run = 0;  // run: where the current one begins
-    for (int s = 0; s < tokens; s += 32) {
-        const int t = s + lane, w = t < tokens ? which[t] : -2;
-        const bool begins = t < tokens && (t == 0 || which[t - 1] != w);
-        const unsigned starts = __ballot_sync(0xffffffffu, begins);
-        const unsigned before = starts & (0xffffffffu >> (31 - lane));
-        const int from = before ? s + 31 - __clz(before) : run;          // of this token's run
-        const bool opens = t < tokens && ((t - from) & 7) == 0;
-        const unsigned open = __ballot_sync(0xffffffffu, opens);
-        if (opens) {
-            int end = t + 1;
-            while (end < tokens && end < t + 8 && which[end] == w) ++end;
-            groups[count + __popc(open & ((1u << lane) - 1u))] = {(int16_t)t, (int16_t)(end - t), w};
+// The CTA's first 128 threads: the groups of the tile's tokens (up to 128), those of one adapter side by side, adapters in the order of their first tokens;
+// the same in every CTA.  `base`: room for 128.  Needs a barrier behind it.
+__device__ __forceinline__ void make_groups(const int* which, int tokens, AdGroup* groups, int* n_groups, int* base) {
+    if (threadIdx.x >= (tokens <= 32 ? 32 : 128)) return;
+    const int t = threadIdx.x, lane = t & 31, mine = t < tokens ? which[t] : -2;
+    if (tokens <= 32) {  // one warp
+        const unsigned same = __match_any_sync(0xffffffffu, mine);
+        const int total = __popc(same), before = __popc(same & ((1u << lane) - 1u)), first = __ffs(same) - 1;
+        const int n = t < tokens && first == t ? (total + 7) / 8 : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(0xffffffffu, sum, o);
+            if (lane >= o) sum += v;
         }
-        count += __popc(open);
-        if (starts) run = s + 31 - __clz(starts);
+        const int at = __shfl_sync(0xffffffffu, sum - n, first);
+        if (lane == 31) *n_groups = sum;
+        if (t < tokens) {
+            AdGroup& g = groups[at + before / 8];
+            g.token[before & 7] = (uint8_t)t;
+            if ((before & 7) == 0) {
+                g.n = min(8, total - before);
+                g.adapter = mine;
+            }
+        }
+        return;
     }
-    return count;
+    int total = 0, before = 0, first = t;  // tokens of this one's adapter; those before it; the first of them
+    for (int s = tokens - 1; s >= 0; --s) {
+        if (which[s] != mine) continue;
+        ++total;
+        before += s < t;
+        first = s;
+    }
+    // where each adapter's groups begin: a sum over its first token and those before
+    int n = t < tokens && first == t ? (total + 7) / 8 : 0, sum = n;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int v = __shfl_up_sync(0xffffffffu, sum, o);
+        if (lane >= o) sum += v;
+    }
+    base[t] = sum;
+    asm volatile("bar.sync 3, 128;" ::: "memory");
+    int at = sum - n, all = 0;
+    for (int w = 0; w < 4; ++w) {
+        const int part = base[w * 32 + 31];
+        if (w < (t >> 5)) at += part;
+        all += part;
+    }
+    asm volatile("bar.sync 3, 128;" ::: "memory");
+    base[t] = at;
+    if (t == 0) *n_groups = all;
+    asm volatile("bar.sync 3, 128;" ::: "memory");
+    if (t < tokens) {
+        AdGroup& g = groups[base[first] + before / 8];
+        g.token[before & 7] = (uint8_t)t;
+        if ((before & 7) == 0) {
+            g.n = min(8, total - before);
+            g.adapter = mine;
+        }
+    }
 }
 
-// u^T = A x^T over this CTA's part of K, in blocks of 64, into `mine` ([warp][token][rank] for SMALL, [token][rank]).
-template <bool F16, int RT, bool SMALL>
+// A group's 64 elements of K: its tokens' x and its adapter's A, as the instructions take them (32 at a time: lane c has elements 8 c .. 8 c + 7 of
+// them, four for each of two instructions).
+template <int RT>
+struct AdBlock {
+    uint4 x[2], lo[RT][2], hi[RT][2];
+    __device__ __forceinline__ void load(const AdapterArgs& a, const AdGroup& gr, const uint16_t* xp, int blk, int lane) {
+        const int g = lane >> 2, c = lane & 3;
+        const uint16_t* const ap = static_cast<const uint16_t*>(a.a) + (int64_t)max(gr.adapter, 0) * a.rank * a.K;
+        const uint16_t* const xrow = xp + gr.token[min(g, gr.n - 1)] * a.xs;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int k = blk * 64 + h * 32 + 8 * c;
+            const bool in = k < a.K && gr.adapter >= 0;
+            x[h] = load16(xrow + k, in && g < gr.n);
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const int row = i * 16 + g;
+                lo[i][h] = load16(ap + (int64_t)row * a.K + k, in && row < a.rank);
+                hi[i][h] = load16(ap + (int64_t)(row + 8) * a.K + k, in && row + 8 < a.rank);
+            }
+        }
+    }
+};
+
+// u^T = A x^T over this CTA's part of K, in blocks of 64, into `mine` ([warp][token][rank] for SMALL, [token][rank]).  Up to 32 ranks the next
+// block, which may be the next group's, is on its way while one is worked on.
+template <bool F16, int RT, bool SMALL, int CTAS>
 __device__ __forceinline__ void shrink_groups(const AdapterArgs& a, const AdGroup* groups, int n_groups, float* mine, int t0, int cta, int warp, int lane) {
     constexpr int kRanks = AdapterShape<RT>::kRanks;
+    constexpr bool kAhead = RT <= 2;
     const int g = lane >> 2, c = lane & 3;
     const int blocks = (a.K + 63) / 64;
     const uint16_t* const xp = static_cast<const uint16_t*>(a.x) + (int64_t)t0 * a.xs;
-    for (int gi = SMALL ? 0 : warp; gi < n_groups; gi += SMALL ? 1 : kAdWarps) {
-        const AdGroup gr = groups[gi];
+    const int first = SMALL ? cta * kAdWarps + warp : cta, step = SMALL ? CTAS * kAdWarps : CTAS;
+    const int g0 = SMALL ? 0 : warp, g_step = SMALL ? 1 : kAdWarps;
+    AdBlock<RT> now, then;
+    if (kAhead && g0 < n_groups && first < blocks) then.load(a, groups[g0], xp, first, lane);
+    for (int gi = g0; gi < n_groups; gi += g_step) {
+        const AdGroup& gr = groups[gi];
         float u[RT][4];
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) u[i][k] = 0.f;
-        if (gr.adapter >= 0) {
-            const uint16_t* const ap = static_cast<const uint16_t*>(a.a) + (int64_t)gr.adapter * a.rank * a.K;
-            const uint16_t* const xrow = xp + (gr.first + min(g, gr.n - 1)) * a.xs;
-            const int first = SMALL ? cta * kAdWarps + warp : cta, step = SMALL ? kAdCtas * kAdWarps : kAdCtas;
 #pragma unroll 1
-            for (int blk = first; blk < blocks; blk += step) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {  // 32 of K: lane c has elements 8 c .. 8 c + 7 of them, four for each of two instructions
-                    const int k = blk * 64 + h * 32 + 8 * c;
-                    const bool in = k < a.K;
-                    const uint4 xv = load16(xrow + k, in && g < gr.n);
-#pragma unroll
-                    for (int i = 0; i < RT; ++i) {
-                        const int row = i * 16 + g;
-                        const uint4 lo = load16(ap + (int64_t)row * a.K + k, in && row < a.rank);
-                        const uint4 hi = load16(ap + (int64_t)(row + 8) * a.K + k, in && row + 8 < a.rank);
-                        const uint32_t f0[4] = {lo.x, hi.x, lo.y, hi.y}, f1[4] = {lo.z, hi.z, lo.w, hi.w};
-                        mma_16816<F16>(u[i], f0, xv.x, xv.y);
-                        mma_16816<F16>(u[i], f1, xv.z, xv.w);
-                    }
-                }
+        for (int blk = first; blk < blocks; blk += step) {
+            if constexpr (kAhead) {
+                now = then;
+                if (blk + step < blocks) then.load(a, gr, xp, blk + step, lane);
+                else if (gi + g_step < n_groups) then.load(a, groups[gi + g_step], xp, first, lane);
+            } else {
+                now.load(a, gr, xp, blk, lane);
             }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const uint32_t f0[4] = {now.lo[i][h].x, now.hi[i][h].x, now.lo[i][h].y, now.hi[i][h].y};
+                    const uint32_t f1[4] = {now.lo[i][h].z, now.hi[i][h].z, now.lo[i][h].w, now.hi[i][h].w};
+                    mma_16816<F16>(u[i], f0, now.x[h].x, now.x[h].y);
+                    mma_16816<F16>(u[i], f1, now.x[h].z, now.x[h].w);
+                }
         }
         // rows g, g + 8 are ranks, columns 2c, 2c + 1 tokens
 #pragma unroll
@@ -137,14 +204,14 @@ __device__ __forceinline__ void shrink_groups(const AdapterArgs& a, const AdGrou
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int t = 2 * c + (k & 1), r = i * 16 + g + 8 * (k >> 1);
-                if (t < gr.n) mine[((SMALL ? warp * a.tile : 0) + gr.first + t) * kRanks + r] = u[i][k];
+                if (t < gr.n) mine[((SMALL ? warp * a.tile : 0) + gr.token[t]) * kRanks + r] = u[i][k];
             }
     }
 }
 
-// Each CTA's part of u to where it is summed: to the CTA that has the token's eighth of the tile (`per` tokens).
+// Each CTA's part of u to where it is summed: to the CTA that has the token's share of the tile (`per` tokens).
 template <int RT>
-__device__ __forceinline__ void send_eighths(const float* mine, uint32_t inbox_addr, int tokens, int per, int cta) {
+__device__ __forceinline__ void send_parts(const float* mine, uint32_t inbox_addr, int tokens, int per, int cta) {
     constexpr int kRanks = AdapterShape<RT>::kRanks;
     for (int e = threadIdx.x; e < tokens * kRanks; e += kAdThreads) {
         const int t = e / kRanks, p = t / per;
@@ -154,7 +221,7 @@ __device__ __forceinline__ void send_eighths(const float* mine, uint32_t inbox_a
 
 // Tokens sum0 .. sum1 - 1 of the tile: the CTAs' parts ([from][per][rank] in `inbox`) summed, scaled and cut into two; a warp for each token, two ranks to a
 // lane.  put(t, r, hi, lo): ranks r, r + 1 as two pairs; put_unit(t, unit): out += unit * u B^T (lane 0).
-template <bool F16, int RT, typename Put, typename PutUnit>
+template <bool F16, int RT, int CTAS, typename Put, typename PutUnit>
 __device__ __forceinline__ void sum_parts(const AdapterArgs& a, const int* which, const float* inbox, int per, int sum0, int sum1, int warp, int lane,
                                           Put put, PutUnit put_unit) {
     constexpr int kRanks = AdapterShape<RT>::kRanks, kEach = (kRanks + 63) / 64;
@@ -169,7 +236,7 @@ __device__ __forceinline__ void sum_parts(const AdapterArgs& a, const int* which
             v[j] = make_float2(0.f, 0.f);
             if (r < a.rank && i >= 0) {  // (a multiple of 8)
 #pragma unroll
-                for (int p = 0; p < kAdCtas; ++p) {
+                for (int p = 0; p < CTAS; ++p) {
                     const float2 w = *reinterpret_cast<const float2*>(inbox + (p * per + t - sum0) * kRanks + r);
                     v[j].x += w.x;
                     v[j].y += w.y;
@@ -201,43 +268,92 @@ __device__ __forceinline__ void sum_parts(const AdapterArgs& a, const int* which
     }
 }
 
-// out^T = y^T + unit B u^T, 64 columns at a time: lane (g, c) has columns 8 g .. 8 g + 7 of tokens 2c, 2c + 1.  Row g (+ 8) of tile i of
-// the instructions' 16 is column 8 g + 2 i (+ 1).
-template <bool F16, int RT>
-__device__ __forceinline__ void expand_groups(const AdapterArgs& a, const AdGroup* groups, int n_groups, const uint16_t* u_hi, const uint16_t* u_lo,
-                                              const float* unit, int t0, int cta, int warp, int lane) {
+// A group's part of the output's 64 columns from `col0` on: B's rows as the instructions take them, and y.  Lane (g, c) has columns 8 g .. 8 g + 7 of the
+// group's tokens 2c, 2c + 1; row g (+ 8) of tile i of the instructions' 16 is column 8 g + 2 i (+ 1).
+template <int RT>
+using AdRows = uint2[RT][4][2];
+template <int RT>
+__device__ __forceinline__ void load_b(AdRows<RT>& b, const AdapterArgs& a, int adapter, int col0, int lane) {
+    const int c = lane & 3, col = col0 + 8 * (lane >> 2);
+    const uint16_t* const bp = static_cast<const uint16_t*>(a.b) + ((int64_t)max(adapter, 0) * a.N + col) * a.rank;
+#pragma unroll
+    for (int s = 0; s < RT; ++s)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b[s][i][h] = load8(bp + (2 * i + h) * a.rank + 16 * s + 4 * c, adapter >= 0 && col < a.N && 16 * s + 4 * c < a.rank);
+}
+template <int RT>
+struct AdColumns {
+    AdRows<RT> b;
+    uint4 ya, yb;
+    __device__ __forceinline__ void load_y(const AdapterArgs& a, const AdGroup& gr, bool there, int t0, int col0, int lane) {
+        const int c = lane & 3, col = col0 + 8 * (lane >> 2);
+        const uint16_t* const yp = static_cast<const uint16_t*>(a.y) + (int64_t)t0 * a.ys + col;
+        there = there && col < a.N;
+        ya = load16(yp + gr.token[2 * c] * a.ys, there && 2 * c < gr.n);
+        yb = load16(yp + gr.token[2 * c + 1] * a.ys, there && 2 * c + 1 < gr.n);
+    }
+};
+
+// Which pieces of 64 columns and which groups a warp has: pieces `first` .. end - 1 are shared by kAdWarps * `of` warps, of which this is number `warp`; with
+// fewer pieces than warps several have the same one, each some of the groups.
+struct AdShare {
+    int piece, step, g0, g1;
+    __device__ __forceinline__ AdShare(int first, int end, int n_groups, int warp, int of) {
+        const int warps = kAdWarps * of, parts = max(warps / max(end - first, 1), 1), part = warp % parts;
+        piece = first + warp / parts;
+        step = warps / parts;
+        g0 = n_groups * part / parts;
+        g1 = n_groups * (part + 1) / parts;
+    }
+};
+
+// out^T = y^T + unit B u^T.  `next`: the first piece's first group, if EARLY.  The next group's y, and up to 32 ranks its B, are on their way while one is
+// worked on.
+template <bool F16, int RT, bool EARLY>
+__device__ __forceinline__ void expand_groups(const AdapterArgs& a, const AdGroup* groups, const uint16_t* u_hi, const uint16_t* u_lo, const float* unit,
+                                              int t0, const AdShare& share, int end, AdColumns<RT>& next, int lane) {
     constexpr int kRow = AdapterShape<RT>::kHalfRow;
+    constexpr bool kAhead = RT <= 2;
     const int g = lane >> 2, c = lane & 3;
-    const int units = (a.N + 63) / 64;
-    for (int un = cta * kAdWarps + warp; un < units; un += kAdCtas * kAdWarps) {
+    uint16_t* const op = static_cast<uint16_t*>(a.out) + (int64_t)t0 * a.os;
+    if (share.g0 >= share.g1) return;
+    bool ready = EARLY;
+    for (int un = share.piece; un < end; un += share.step) {
         const int col = un * 64 + 8 * g;
         const bool in = col < a.N;
-        uint2 bf[RT][4][2];
-        int have = -1;
-        for (int gi = 0; gi < n_groups; ++gi) {
-            const AdGroup gr = groups[gi];
-            const int ta = gr.first + 2 * c, tb = ta + 1;
+        if (!ready) {
+            next.load_y(a, groups[share.g0], true, t0, un * 64, lane);
+            if (kAhead) load_b<RT>(next.b, a, groups[share.g0].adapter, un * 64, lane);
+        }
+        ready = false;
+        AdRows<RT> bf;
+        auto take_b = [&]() {
+#pragma unroll
+            for (int s = 0; s < RT; ++s)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { bf[s][i][0] = next.b[s][i][0]; bf[s][i][1] = next.b[s][i][1]; }
+        };
+        if (kAhead) take_b();
+        else load_b<RT>(bf, a, groups[share.g0].adapter, un * 64, lane);
+        for (int gi = share.g0; gi < share.g1; ++gi) {
+            const AdGroup& gr = groups[gi];
+            const AdGroup& then = groups[min(gi + 1, share.g1 - 1)];
+            const int ta = gr.token[2 * c], tb = gr.token[2 * c + 1];
             const bool has_a = in && 2 * c < gr.n, has_b = in && 2 * c + 1 < gr.n;
-            const uint4 ya = load16(static_cast<const uint16_t*>(a.y) + (int64_t)(t0 + ta) * a.ys + col, has_a);
-            const uint4 yb = load16(static_cast<const uint16_t*>(a.y) + (int64_t)(t0 + tb) * a.ys + col, has_b);
+            const uint4 ya = next.ya, yb = next.yb;
+            next.load_y(a, then, gi + 1 < share.g1, t0, un * 64, lane);
+            const bool change = then.adapter != gr.adapter;
+            if (kAhead && change) load_b<RT>(next.b, a, then.adapter, un * 64, lane);
             uint4 oa = ya, ob = yb;
             if (gr.adapter >= 0) {
-                if (gr.adapter != have) {
-                    have = gr.adapter;
-                    const uint16_t* const bp = static_cast<const uint16_t*>(a.b) + ((int64_t)have * a.N + col) * a.rank;
-#pragma unroll
-                    for (int s = 0; s < RT; ++s)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) bf[s][i][h] = load8(bp + (2 * i + h) * a.rank + 16 * s + 4 * c, in && 16 * s + 4 * c < a.rank);
-                }
                 float acc[4][4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
 #pragma unroll
                     for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
-                const int row = (gr.first + min(g, gr.n - 1)) * kRow + 4 * c;
+                const int row = gr.token[min(g, gr.n - 1)] * kRow + 4 * c;
 #pragma unroll
                 for (int s = 0; s < RT; ++s) {
                     const uint2 hi = *reinterpret_cast<const uint2*>(u_hi + row + 16 * s), lo = *reinterpret_cast<const uint2*>(u_lo + row + 16 * s);
@@ -260,19 +376,24 @@ __device__ __forceinline__ void expand_groups(const AdapterArgs& a, const AdGrou
                 oa = make_uint4(ra[0], ra[1], ra[2], ra[3]);
                 ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
             }
-            if (has_a) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + (int64_t)(t0 + ta) * a.os + col) = oa;
-            if (has_b) *reinterpret_cast<uint4*>(static_cast<uint16_t*>(a.out) + (int64_t)(t0 + tb) * a.os + col) = ob;
+            if (has_a) *reinterpret_cast<uint4*>(op + ta * a.os + col) = oa;
+            if (has_b) *reinterpret_cast<uint4*>(op + tb * a.os + col) = ob;
+            if (change) {
+                if (kAhead) take_b();
+                else load_b<RT>(bf, a, then.adapter, un * 64, lane);
+            }
         }
     }
 }
 
+// SMALL: up to 8 tokens to a tile; else 16.
 template <bool F16, int RT, bool SMALL>
-__global__ void __launch_bounds__(kAdThreads) adapters_kernel(const AdapterArgs a) {
+__global__ void __launch_bounds__(kAdThreads, RT <= 4 ? 2 : 1) adapters_kernel(const AdapterArgs a) {
     using S = AdapterShape<RT>;
     constexpr int kRanks = S::kRanks, kRow = S::kHalfRow;
     extern __shared__ __align__(16) uint8_t smem[];
     __shared__ AdGroup groups[kAdMost];
-    __shared__ int which[kAdMost];
+    __shared__ int which[kAdMost], base[kAdMost];
     __shared__ float unit[kAdMost];  // out += unit * (u in shared memory) B^T
     __shared__ int n_groups;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -289,12 +410,18 @@ __global__ void __launch_bounds__(kAdThreads) adapters_kernel(const AdapterArgs 
     pdl_wait();
     for (int t = threadIdx.x; t < tokens; t += kAdThreads) which[t] = adapter_of(a, t0 + t);
     __syncthreads();
-    if (warp == 0) {
-        const int n = make_groups(which, tokens, groups, lane);
-        if (lane == 0) n_groups = n;
-    }
+    make_groups(which, tokens, groups, &n_groups, base);
     __syncthreads();
-    shrink_groups<F16, RT, SMALL>(a, groups, n_groups, mine, t0, cta, warp, lane);
+    // of the output's first columns, B and y are asked for now: they need not wait for u
+    constexpr bool kEarly = RT <= 2;
+    const int pieces = (a.N + 63) / 64;
+    const AdShare share(0, pieces, n_groups, warp * kAdCtas + cta, kAdCtas);
+    AdColumns<RT> columns;
+    if (kEarly && share.piece < pieces && share.g0 < share.g1) {
+        load_b<RT>(columns.b, a, groups[share.g0].adapter, share.piece * 64, lane);
+        columns.load_y(a, groups[share.g0], true, t0, share.piece * 64, lane);
+    }
+    shrink_groups<F16, RT, SMALL, kAdCtas>(a, groups, n_groups, mine, t0, cta, warp, lane);
     __syncthreads();
     ad_wait();  // all CTAs of the cluster run
 
@@ -309,7 +436,7 @@ __global__ void __launch_bounds__(kAdThreads) adapters_kernel(const AdapterArgs 
         }
         ad_arrive();
         ad_wait();
-        sum_parts<F16, RT>(a, which, inbox, a.tile, 0, tokens, warp, lane,
+        sum_parts<F16, RT, kAdCtas>(a, which, inbox, a.tile, 0, tokens, warp, lane,
                            [&](int t, int r, uint32_t hi, uint32_t lo) {
                                *reinterpret_cast<uint32_t*>(u_hi + t * kRow + r) = hi;
                                *reinterpret_cast<uint32_t*>(u_lo + t * kRow + r) = lo;
@@ -318,10 +445,10 @@ __global__ void __launch_bounds__(kAdThreads) adapters_kernel(const AdapterArgs 
         __syncthreads();
     } else {  // each its eighth of the tokens
         const int per = a.tile / kAdCtas;
-        send_eighths<RT>(mine, inbox_addr, tokens, per, cta);
+        send_parts<RT>(mine, inbox_addr, tokens, per, cta);
         ad_arrive();
         ad_wait();
-        sum_parts<F16, RT>(a, which, inbox, per, cta * per, min(cta * per + per, tokens), warp, lane,
+        sum_parts<F16, RT, kAdCtas>(a, which, inbox, per, cta * per, min(cta * per + per, tokens), warp, lane,
                            [&](int t, int r, uint32_t hi, uint32_t lo) {
 #pragma unroll
                                for (int p = 0; p < kAdCtas; ++p) {
@@ -336,125 +463,158 @@ __global__ void __launch_bounds__(kAdThreads) adapters_kernel(const AdapterArgs 
         ad_arrive();
         ad_wait();
     }
-    expand_groups<F16, RT>(a, groups, n_groups, u_hi, u_lo, unit, t0, cta, warp, lane);
+    expand_groups<F16, RT, kEarly>(a, groups, u_hi, u_lo, unit, t0, share, pieces, columns, lane);
 }
 
-// ------------------------------------------------------------------------------------------------- tiles of up to 128 tokens on the tensor cores
-// Many tokens: a tile's tokens are the 128 rows of a tcgen05 tile.  Contraction: u[128 x ranks] = x A_i^T for each adapter i that the tile has, x and
-// A through a ring filled by TMA; a row takes its own adapter's u.  Output: D[128 x 128 columns] = [u, what rounding left] [B_i, B_i]^T, and the row
-// of y, which lies in shared memory, gets its own adapter's D added there and leaves by TMA.  A tile of more than kTileAdapters adapters, each of
-// which takes a pass over the tile, goes by groups of 8 tokens like small ones.
-constexpr int kTileAdapters = 4;
-constexpr int kTileCols = 128;
+// ------------------------------------------------------------------------------------------------- tiles of 128 tokens on the tensor cores
+// Many tokens: 128 of them are the rows of a tcgen05 tile, and each product is a kernel of its own with u in the workspace between them, so that the second
+// one, which moves most of the bytes, shares them out evenly over all SMs.
+//   u[128 x ranks] = x A_i^T for each adapter i that the tile has, a cluster of eight CTAs to a tile; a row takes its own adapter's
+//   D[128 x 128 columns] = [u, what rounding left] [B_i, B_i]^T; the rows of y, which lie in shared memory, get their own adapter's D added there and
+//     leave by TMA
+// A tile of more than kTileAdapters adapters, each of which takes a pass over the tile, goes by groups of 8 tokens like small ones.
+constexpr int kTileRows = 128, kTileCols = 128, kTileAdapters = 4;
+constexpr int kListInts = 8;  // of a tile: how many adapters it has (kTileAdapters + 1: more than that), and which
 
-template <int RT>
-struct TileShape {
-    static constexpr int kRanks = RT * 16;
-    static constexpr int kOp = (2 * kRanks + 63) / 64 * 16384;   // u and its rest: [128 rows x 64] chunks
-    static constexpr int kStage = 16384 + kRanks * 128;          // x's and A's 64 of K
-    static constexpr int kY = 3, kB = 3;                         // buffers of y (and out), of B
-    static constexpr int kYBytes = 2 * 16384, kBBytes = kTileCols * 128;
-    static constexpr int kRing = kY * kYBytes + kB * kBBytes;    // the contraction's stages before that
-    static constexpr int kStages = kRing / kStage < 8 ? kRing / kStage : 8;
-    static constexpr int kInboxOff = kOp, kRingOff = kInboxOff + 128 * kRanks * 4;
-    static constexpr int kSmem = 1024 + kRingOff + kRing;
-    // by groups: what the CTA has of u, then u, in the ring's place
-    static_assert(128 * kRanks * 4 + 128 * AdapterShape<RT>::kHalfRow * 4 <= kRing && kRingOff % 1024 == 0 && kStage % 1024 == 0, "shared memory");
-    static_assert(kSmem <= 232448 - 6144, "shared memory");
+inline int padded_ranks(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
+// The workspace: adapters and units of the tokens, the tiles' lists, u.
+struct TileWorkspace {
+    size_t unit, list, u, bytes;
+    TileWorkspace(long long T, int ranks) {
+        auto up = [](long long n) { return ((size_t)n + 255) / 256 * 256; };
+        unit = up(T * 4);
+        list = unit + up(T * 4);
+        u = list + up((T + kTileRows - 1) / kTileRows * kListInts * 4);
+        bytes = u + (size_t)T * ranks * 4;
+    }
+};
+struct TileArgs {
+    AdapterArgs a;
+    int *which, *list;
+    float* unit;
+    uint32_t* u;  // [token][ranks], then what rounding left of them, in pairs
 };
 
-template <bool F16, int RT>
-__global__ void __launch_bounds__(kAdThreads, 1)
-adapters_tile_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_a, const __grid_constant__ CUtensorMap tmap_y,
-                     const __grid_constant__ CUtensorMap tmap_b, const __grid_constant__ CUtensorMap tmap_out, const AdapterArgs a) {
-    using S = TileShape<RT>;
+template <int RT>
+struct ContractShape {
+    static constexpr int kRanks = RT * 16;
+    static constexpr int kStage = 16384 + kRanks * 128;          // x's and A's 64 of K
+    static constexpr int kStages = RT == 8 ? 4 : RT == 4 ? 3 : 4;  // (with these two CTAs to an SM, but for RT = 8)
+    static constexpr int kInboxOff = kStages * kStage;
+    static constexpr int kSmem = 1024 + kInboxOff + kTileRows * kRanks * 4;
+    static constexpr int kTmemCols = kTileAdapters * kRanks;
+    static_assert(kTileRows * kRanks * 4 <= kInboxOff && kStage % 1024 == 0, "by groups: what the CTA has of u, in the ring's place");
+    static_assert(kSmem <= 232448 - 4096 && (RT == 8 || 2 * (kSmem + 4096) <= 232448), "shared memory");
+};
+
+// CTAS: of a cluster, which share K.
+template <bool F16, int RT, int CTAS>
+__global__ void __launch_bounds__(kAdThreads, RT == 8 ? 1 : 2)
+adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_a, const TileArgs ta) {
+    using S = ContractShape<RT>;
     using namespace ptx;
-    constexpr int kRanks = S::kRanks, kRow = AdapterShape<RT>::kHalfRow;
+    constexpr int kRanks = S::kRanks, kPer = kTileRows / CTAS;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ AdGroup groups[kAdMost];
-    __shared__ int which[kAdMost], several[kTileAdapters];
-    __shared__ float unit[kAdMost];
+    __shared__ AdGroup groups[kTileRows];
+    __shared__ int which[kTileRows], base[kTileRows], several[kTileAdapters];
     __shared__ int n_groups, n_several;
-    __shared__ uint64_t x_full[S::kStages], x_free[S::kStages], u_done, y_full[S::kY], y_free[S::kY], b_full[S::kB], b_free[S::kB], d_full[2], d_free[2];
+    __shared__ uint64_t x_full[S::kStages], x_free[S::kStages], u_done;
     __shared__ uint32_t tmem_slot;
+    const AdapterArgs& a = ta.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int cta = blockIdx.x % kAdCtas;
-    const int t0 = (int)(blockIdx.x / kAdCtas) * a.tile, tokens = min(a.tile, a.T - t0), per = a.tile / kAdCtas;
-    uint8_t* smem = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));
-    uint8_t* ring = smem + S::kRingOff;
-    float* inbox = reinterpret_cast<float*>(smem + S::kInboxOff);
+    const int cta = blockIdx.x % CTAS, tile = blockIdx.x / CTAS;
+    const int t0 = tile * kTileRows, tokens = min(kTileRows, a.T - t0);
+    uint8_t* ring = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));
+    float* inbox = reinterpret_cast<float*>(ring + S::kInboxOff);
     ad_arrive();  // waited for before the first store into another CTA's shared memory
     if (threadIdx.x == 0) {
-        for (int i = 0; i < S::kStages; ++i) { mbar_init(&x_full[i], 1); mbar_init(&x_free[i], 1); }
+        for (int i = 0; i < S::kStages; ++i) { mbar_init(&x_full[i], 2); mbar_init(&x_free[i], 1); }  // full: x, and A
         mbar_init(&u_done, 1);
-        for (int i = 0; i < S::kY; ++i) { mbar_init(&y_full[i], 1); mbar_init(&y_free[i], 1); }
-        for (int i = 0; i < S::kB; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_free[i], 1); }
-        for (int i = 0; i < 2; ++i) { mbar_init(&d_full[i], 1); mbar_init(&d_free[i], 4); }
         fence_mbar_init();
         prefetch_tmap(&tmap_x);
         prefetch_tmap(&tmap_a);
-        prefetch_tmap(&tmap_y);
-        prefetch_tmap(&tmap_b);
-        prefetch_tmap(&tmap_out);
-        n_several = 0;
     }
     if (warp == 2) {
-        tmem_alloc(&tmem_slot, 256);
+        tmem_alloc(&tmem_slot, S::kTmemCols);
         tmem_relinquish();
     }
     pdl_launch_dependents();
     pdl_wait();
-    for (int t = threadIdx.x; t < tokens; t += kAdThreads) which[t] = adapter_of(a, t0 + t);
+    const int blocks = (a.K + 63) / 64, my_blocks = cta < blocks ? (blocks - cta + CTAS - 1) / CTAS : 0;
+    const int early = min(my_blocks, S::kStages);
+    __syncthreads();
+    if (warp == 3 && elect_one()) {  // the first of x, whatever adapters it will meet
+        for (int i = 0; i < early; ++i) {
+            mbar_expect_tx(&x_full[i], 16384);
+            tma_load_2d(ring + i * S::kStage, &tmap_x, &x_full[i], (cta + i * CTAS) * 64, t0);
+        }
+    }
+    __syncwarp();
+    // ---- the adapters that the tile has, in the order of their first tokens
+    if (warp == 0) {
+        int mine[kTileRows / 32], n = 0;
+#pragma unroll
+        for (int k = 0; k < kTileRows / 32; ++k) {
+            const int t = k * 32 + lane;
+            mine[k] = t < tokens ? adapter_of(a, t0 + t) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kTileRows / 32; ++k)
+            if (k * 32 + lane < tokens) which[k * 32 + lane] = mine[k];
+#pragma unroll
+        for (int k = 0; k < kTileRows / 32; ++k) {
+            for (unsigned left; n <= kTileAdapters && (left = __ballot_sync(0xffffffffu, mine[k] >= 0)) != 0;) {
+                const int x = __shfl_sync(0xffffffffu, mine[k], __ffs(left) - 1);
+                if (lane == 0 && n < kTileAdapters) several[n] = x;
+                ++n;
+#pragma unroll
+                for (int l = 0; l < kTileRows / 32; ++l)
+                    if (mine[l] == x) mine[l] = -1;
+            }
+        }
+        __syncwarp();
+        if (lane == 0) n_several = n;
+        if (cta == 0) {
+            if (lane == 0) ta.list[tile * kListInts] = n;
+            if (lane < min(n, kTileAdapters)) ta.list[tile * kListInts + 1 + lane] = several[lane];
+        }
+    }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
-    // ---- the adapters that the tile has, in the order of their first tokens
-    if (warp == 0) {
-        int n = 0;
-        for (int s = 0; s < tokens; s += 32) {
-            const int t = s + lane, w = t < tokens ? which[t] : -1;
-            unsigned starts = __ballot_sync(0xffffffffu, w >= 0 && (t == 0 || which[t - 1] != w));
-            for (; starts && n <= kTileAdapters; starts &= starts - 1) {
-                const int x = __shfl_sync(0xffffffffu, w, __ffs(starts) - 1);
-                bool had = false;
-                for (int i = 0; i < n && i < kTileAdapters; ++i) had |= several[i] == x;
-                if (had) continue;
-                if (lane == 0 && n < kTileAdapters) several[n] = x;
-                ++n;
-                __syncwarp();
-            }
-        }
-        if (lane == 0) n_several = n;
-    } else if (warp == 1) {
-        const int n = make_groups(which, tokens, groups, lane);
-        if (lane == 0) n_groups = n;
-    }
-    __syncthreads();
     const int adapters = n_several;
-    const bool tiled = adapters > 0 && adapters <= kTileAdapters;
+    const bool tiled = adapters <= kTileAdapters;
     bool failed = false;
-    const uint32_t inbox_addr = smem_u32(inbox), op_addr = smem_u32(smem), unit_addr = smem_u32(unit);
-    float* mine = reinterpret_cast<float*>(ring);                                              // (by groups)
-    uint16_t* u_hi = reinterpret_cast<uint16_t*>(ring + 128 * kRanks * 4);
-    uint16_t* u_lo = u_hi + 128 * kRow;
-
-    // ---- the contraction
-    const int blocks = (a.K + 63) / 64, my_blocks = cta < blocks ? (blocks - cta + kAdCtas - 1) / kAdCtas : 0;
+    const uint32_t inbox_addr = smem_u32(inbox);
+    if (!tiled || adapters == 0) {  // what has come of x is not wanted
+        if (threadIdx.x == 0)
+            for (int i = 0; i < early && !failed; ++i) {
+                mbar_arrive(&x_full[i]);
+                if (!mbar_wait(&x_full[i], 0)) failed = true;
+            }
+        __syncthreads();
+    }
     if (!tiled) {
-        shrink_groups<F16, RT, false>(a, groups, n_groups, mine, t0, cta, warp, lane);
+        make_groups(which, tokens, groups, &n_groups, base);
+        __syncthreads();
+        float* mine = reinterpret_cast<float*>(ring);
+        shrink_groups<F16, RT, false, CTAS>(a, groups, n_groups, mine, t0, cta, warp, lane);
         __syncthreads();
         ad_wait();
-        send_eighths<RT>(mine, inbox_addr, tokens, per, cta);
+        send_parts<RT>(mine, inbox_addr, tokens, kPer, cta);
     } else {
         if (warp == 0 && elect_one()) {
             int n = 0;
             for (int j = 0; j < adapters && !failed; ++j)
                 for (int i = 0; i < my_blocks; ++i, ++n) {
-                    const int st = n % S::kStages, k = (cta + i * kAdCtas) * 64;
+                    const int st = n % S::kStages, k = (cta + i * CTAS) * 64;
                     if (n >= S::kStages && !mbar_wait(&x_free[st], (n / S::kStages - 1) & 1)) { failed = true; break; }
-                    mbar_expect_tx(&x_full[st], a.tile * 128 + kRanks * 128);
-                    tma_load_2d(ring + st * S::kStage, &tmap_x, &x_full[st], k, t0);
+                    if (n >= early) {
+                        mbar_expect_tx(&x_full[st], 16384);
+                        tma_load_2d(ring + st * S::kStage, &tmap_x, &x_full[st], k, t0);
+                    }
+                    mbar_expect_tx(&x_full[st], kRanks * 128);
                     tma_load_2d(ring + st * S::kStage + 16384, &tmap_a, &x_full[st], k, several[j] * a.rank);
                 }
         } else if (warp == 1 && elect_one()) {
@@ -470,7 +630,7 @@ adapters_tile_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
                     for (int k = 0; k < 4; ++k) mma_ss(tmem + j * kRanks, xd + (k * 32 >> 4), ad + (k * 32 >> 4), idesc, i > 0 || k > 0);
                     mma_commit(&x_free[st]);
                 }
-            if (my_blocks == 0) mbar_arrive(&u_done);
+            if (n == 0) mbar_arrive(&u_done);
             else if (!failed) mma_commit(&u_done);
         }
         __syncwarp();
@@ -480,8 +640,8 @@ adapters_tile_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
             const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
             if (!warp_wait(&u_done, 0)) failed = true;
             tc_fence_after_sync();
-            const int p = row / per;
-            const uint32_t to = own >= 0 ? peer_smem(inbox_addr + (cta * per + row - p * per) * kRanks * 4, p) : 0;
+            const int p = row / kPer;
+            const uint32_t to = peer_smem(inbox_addr + (cta * kPer + row - p * kPer) * kRanks * 4, p);
             for (int j = 0; j < adapters && !failed; ++j) {
                 const bool hit = own == several[j];
                 if (!__any_sync(0xffffffffu, hit)) continue;
@@ -502,191 +662,281 @@ adapters_tile_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_co
     }
     ad_arrive();
     ad_wait();
-    tc_fence_after_sync();
 
-    // ---- u, to all CTAs
-    sum_parts<F16, RT>(a, which, inbox, per, cta * per, min(cta * per + per, tokens), warp, lane,
+    sum_parts<F16, RT, CTAS>(a, which, inbox, kPer, cta * kPer, min(cta * kPer + kPer, tokens), warp, lane,
                        [&](int t, int r, uint32_t hi, uint32_t lo) {
-                           uint32_t to_hi, to_lo;
-                           if (tiled) {  // elements r and kRanks + r of row t, in chunks of 64 with 128-byte swizzle
-                               auto at = [&](int e) { return op_addr + (e >> 6) * 16384 + t * 128 + ((((e & 63) >> 3) ^ (t & 7)) << 4) + (e & 7) * 2; };
-                               to_hi = at(r);
-                               to_lo = at(kRanks + r);
-                           } else {
-                               to_hi = smem_u32(u_hi + t * kRow + r);
-                               to_lo = smem_u32(u_lo + t * kRow + r);
-                           }
-#pragma unroll
-                           for (int p = 0; p < kAdCtas; ++p) {
-                               store_peer(peer_smem(to_hi, p), hi);
-                               store_peer(peer_smem(to_lo, p), lo);
-                           }
+                           uint32_t* to = ta.u + (int64_t)(t0 + t) * kRanks + r / 2;
+                           to[0] = hi;
+                           to[kRanks / 2] = lo;
                        },
                        [&](int t, float x) {
-#pragma unroll
-                           for (int p = 0; p < kAdCtas; ++p) store_peer(peer_smem(unit_addr + t * 4, p), x);
+                           ta.unit[t0 + t] = x;
+                           ta.which[t0 + t] = which[t];
                        });
-    asm volatile("fence.proxy.async;" ::: "memory");  // the tensor cores read what plain stores wrote
-    __syncwarp();
-    ad_arrive();
-    ad_wait();
-    asm volatile("fence.proxy.async;" ::: "memory");
+    if (failed) {
+        atomicExch(a.status, 1);
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // let copies and products in flight end before their memory goes away
+    }
+    __syncthreads();
+    if (warp == 2) tmem_dealloc(tmem, S::kTmemCols);
+}
 
-    // ---- the output
-    if (!tiled) {
-        expand_groups<F16, RT>(a, groups, n_groups, u_hi, u_lo, unit, t0, cta, warp, lane);
-    } else {
-        const int chunks = (a.N + kTileCols - 1) / kTileCols;
-        uint8_t* b_ring = ring + S::kY * S::kYBytes;
-        if (warp == 0 && elect_one()) {
-            int n = 0, m = 0;  // chunks; chunks and adapters
-            for (int q = cta; q < chunks && !failed; q += kAdCtas, ++n) {
-                const int yb = n % S::kY;
-                if (n >= S::kY && !mbar_wait(&y_free[yb], (n / S::kY - 1) & 1)) { failed = true; break; }
-                mbar_expect_tx(&y_full[yb], 2 * a.tile * 128);
-                tma_load_2d(ring + yb * S::kYBytes, &tmap_y, &y_full[yb], q * kTileCols, t0);
-                tma_load_2d(ring + yb * S::kYBytes + 16384, &tmap_y, &y_full[yb], q * kTileCols + 64, t0);
-                for (int j = 0; j < adapters; ++j, ++m) {
-                    const int bb = m % S::kB;
-                    if (m >= S::kB && !mbar_wait(&b_free[bb], (m / S::kB - 1) & 1)) { failed = true; break; }
-                    mbar_expect_tx(&b_full[bb], S::kBBytes);
-                    tma_load_2d(b_ring + bb * S::kBBytes, &tmap_b, &b_full[bb], 0, several[j] * a.N + q * kTileCols);
+template <int RT>
+struct OutputShape {
+    static constexpr int kRanks = RT * 16;
+    static constexpr int kOp = (2 * kRanks + 63) / 64 * 16384;   // u and its rest: [128 rows x 64] chunks
+    static constexpr int kY = RT == 8 ? 2 : 4, kB = RT == 8 ? 2 : 3;  // buffers of y (and out), of B
+    static constexpr int kYBytes = 2 * 16384, kBBytes = (kRanks + 63) / 64 * kTileCols * 128;
+    static constexpr int kYOff = kOp, kBOff = kYOff + kY * kYBytes;
+    static constexpr int kSmem = 1024 + kBOff + kB * kBBytes;
+    static constexpr int kThreads = 10 * 32;  // warps 0-7: out, two groups of 128 threads, each half of the columns; 8: TMA; 9: tcgen05.mma
+    static_assert(2 * kTileRows * AdapterShape<RT>::kHalfRow * 2 <= kBOff, "by groups: u, in the tile's and y's place");
+    static_assert(kSmem <= 232448 - 4096, "shared memory");
+};
+
+template <bool F16, int RT>
+__global__ void __launch_bounds__(OutputShape<RT>::kThreads, 1)
+adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_constant__ CUtensorMap tmap_y, const __grid_constant__ CUtensorMap tmap_b,
+                       const __grid_constant__ CUtensorMap tmap_out, const TileArgs ta) {
+    using S = OutputShape<RT>;
+    using namespace ptx;
+    constexpr int kRanks = S::kRanks, kRow = AdapterShape<RT>::kHalfRow;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ AdGroup groups[kTileRows];
+    __shared__ int which[kTileRows], base[kTileRows];
+    __shared__ float unit[kTileRows];
+    __shared__ int n_groups;
+    __shared__ uint64_t u_full, y_full[S::kY], y_free[S::kY], b_full[S::kB], b_free[S::kB], d_full[2], d_free[2];
+    __shared__ uint32_t tmem_slot;
+    const AdapterArgs& a = ta.a;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t* smem = smem_raw + (((smem_u32(smem_raw) + 1023u) & ~1023u) - smem_u32(smem_raw));
+    uint8_t *y_ring = smem + S::kYOff, *b_ring = smem + S::kBOff;
+    if (threadIdx.x == 0) {
+        mbar_init(&u_full, 1);
+        for (int i = 0; i < S::kY; ++i) { mbar_init(&y_full[i], 1); mbar_init(&y_free[i], 2); }
+        for (int i = 0; i < S::kB; ++i) { mbar_init(&b_full[i], 1); mbar_init(&b_free[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&d_full[i], 1); mbar_init(&d_free[i], 8); }
+        fence_mbar_init();
+        prefetch_tmap(&tmap_u);
+        prefetch_tmap(&tmap_y);
+        prefetch_tmap(&tmap_b);
+        prefetch_tmap(&tmap_out);
+    }
+    if (warp == 9) {
+        tmem_alloc(&tmem_slot, 2 * kTileCols);
+        tmem_relinquish();
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = tmem_slot;
+    pdl_launch_dependents();
+    pdl_wait();
+
+    // this CTA's chunks of 128 columns, of all tiles'
+    const int chunks = (a.N + kTileCols - 1) / kTileCols;
+    const long long all = (long long)((a.T + kTileRows - 1) / kTileRows) * chunks;
+    const long long from = all * blockIdx.x / gridDim.x, to = all * (blockIdx.x + 1) / gridDim.x;
+    bool failed = false;
+    int n = 0, m = 0, seg = 0;  // chunks; chunks and adapters; tiles that went through the tensor cores, of this CTA so far
+    for (long long at = from; at < to;) {
+        const int tile = (int)(at / chunks), q0 = (int)(at - (long long)tile * chunks), q1 = (int)min((long long)chunks, q0 + to - at);
+        at += q1 - q0;
+        const int t0 = tile * kTileRows, tokens = min(kTileRows, a.T - t0);
+        const int* list = ta.list + tile * kListInts;
+        const int adapters = __ldcg(list);
+        if (adapters == 0 && a.y == a.out) continue;
+        if (adapters > kTileAdapters) {
+            // ---- by groups of tokens; no copies are in flight, as behind each tile
+            uint16_t *u_hi = reinterpret_cast<uint16_t*>(smem), *u_lo = u_hi + kTileRows * kRow;
+            for (int t = threadIdx.x; t < tokens; t += S::kThreads) {
+                which[t] = __ldcg(ta.which + t0 + t);
+                unit[t] = __ldcg(ta.unit + t0 + t);
+            }
+            for (int e = threadIdx.x; e < tokens * kRanks; e += S::kThreads) {  // pairs
+                const int t = e / kRanks, r = e % kRanks * 2;
+                const uint32_t w = __ldcg(ta.u + (int64_t)t0 * kRanks + e);
+                *reinterpret_cast<uint32_t*>((r < kRanks ? u_hi + r : u_lo + r - kRanks) + t * kRow) = w;
+            }
+            __syncthreads();
+            make_groups(which, tokens, groups, &n_groups, base);
+            __syncthreads();
+            if (warp < kAdWarps) {
+                const int end = min(2 * q1, (a.N + 63) / 64);
+                AdColumns<RT> columns;
+                expand_groups<F16, RT, false>(a, groups, u_hi, u_lo, unit, t0, AdShare(2 * q0, end, n_groups, warp, 1), end, columns, lane);
+            }
+            fence_proxy_async_smem();  // the ring is the copy engine's again
+            __syncthreads();
+            continue;
+        }
+        if (warp == 8) {
+            if (elect_one() && !failed) {
+                mbar_expect_tx(&u_full, S::kOp);
+#pragma unroll
+                for (int c = 0; c < S::kOp / 16384; ++c) tma_load_2d(smem + c * 16384, &tmap_u, &u_full, c * 64, t0);
+                int several[kTileAdapters];
+#pragma unroll
+                for (int j = 0; j < kTileAdapters; ++j) several[j] = j < adapters ? __ldcg(list + 1 + j) : 0;
+                int nn = n, mm = m;
+                for (int q = q0; q < q1 && !failed; ++q, ++nn) {
+                    const int yb = nn % S::kY;
+                    if (nn >= S::kY && !mbar_wait(&y_free[yb], (nn / S::kY - 1) & 1)) { failed = true; break; }
+                    mbar_expect_tx(&y_full[yb], S::kYBytes);
+                    tma_load_2d(y_ring + yb * S::kYBytes, &tmap_y, &y_full[yb], q * kTileCols, t0);
+                    tma_load_2d(y_ring + yb * S::kYBytes + 16384, &tmap_y, &y_full[yb], q * kTileCols + 64, t0);
+#pragma unroll
+                    for (int j = 0; j < kTileAdapters; ++j) {
+                        if (j >= adapters) break;
+                        const int bb = mm % S::kB;
+                        if (mm >= S::kB && !mbar_wait(&b_free[bb], (mm / S::kB - 1) & 1)) { failed = true; break; }
+                        mbar_expect_tx(&b_full[bb], S::kBBytes);
+#pragma unroll
+                        for (int c = 0; c < (kRanks + 63) / 64; ++c)
+                            tma_load_2d(b_ring + bb * S::kBBytes + c * (kTileCols * 128), &tmap_b, &b_full[bb], c * 64, several[j] * a.N + q * kTileCols);
+                        ++mm;
+                    }
                 }
             }
-        } else if (warp == 1 && elect_one()) {
-            constexpr uint32_t idesc = F16 ? make_idesc_f16(128, kTileCols, false, false) : make_idesc_bf16(128, kTileCols, false, false);
-            const uint64_t ud = make_smem_desc(op_addr, 16, 1024);
-            int m = 0;
-            for (int q = cta; q < chunks && !failed; q += kAdCtas)
-                for (int j = 0; j < adapters; ++j, ++m) {
-                    const int bb = m % S::kB, db = m & 1;
-                    if (!mbar_wait(&b_full[bb], (m / S::kB) & 1)) { failed = true; break; }
-                    if (m >= 2 && !mbar_wait(&d_free[db], (m / 2 - 1) & 1)) { failed = true; break; }
-                    tc_fence_after_sync();
-                    const uint64_t bd = make_smem_desc(smem_u32(b_ring + bb * S::kBBytes), 16, 1024);
+            __syncwarp();
+        } else if (warp == 9) {
+            if (elect_one() && !failed) {
+                constexpr uint32_t idesc = F16 ? make_idesc_f16(128, kTileCols, false, false) : make_idesc_bf16(128, kTileCols, false, false);
+                const uint64_t ud = make_smem_desc(smem_u32(smem), 16, 1024);
+                if (!mbar_wait(&u_full, seg & 1)) failed = true;
+                int mm = m;
+                for (int q = q0; q < q1 && !failed; ++q)
+                    for (int j = 0; j < adapters; ++j, ++mm) {
+                        const int bb = mm % S::kB, db = mm & 1;
+                        if (!mbar_wait(&b_full[bb], (mm / S::kB) & 1)) { failed = true; break; }
+                        if (mm >= 2 && !mbar_wait(&d_free[db], (mm / 2 - 1) & 1)) { failed = true; break; }
+                        tc_fence_after_sync();
+                        const uint64_t bd = make_smem_desc(smem_u32(b_ring + bb * S::kBBytes), 16, 1024);
 #pragma unroll
-                    for (int e = 0; e < 2 * kRanks; e += 16)  // u's ranks, then what rounding left of them, with the same columns of B
-                        mma_ss(tmem + db * kTileCols, ud + (((e >> 6) * 16384 + (e & 63) * 2) >> 4), bd + ((e % kRanks) * 2 >> 4), idesc, e > 0);
-                    mma_commit(&b_free[bb]);
-                    mma_commit(&d_full[db]);
-                }
-        } else if (warp >= 4) {
-            const int row = threadIdx.x & 127, own = row < tokens ? which[row] : -1;
-            const float mul = own >= 0 ? unit[row] : 0.f;
-            const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16);
-            int n = 0, m = 0;
-            for (int q = cta; q < chunks; q += kAdCtas, ++n) {
-                const int yb = n % S::kY;
-                uint8_t* y = ring + yb * S::kYBytes + row * 128;
-                if (!failed && !warp_wait(&y_full[yb], (n / S::kY) & 1)) failed = true;
-                for (int j = 0; j < adapters; ++j, ++m) {
-                    const int db = m & 1;
-                    if (!failed && !warp_wait(&d_full[db], (m / 2) & 1)) failed = true;
+                        for (int e = 0; e < 2 * kRanks; e += 16) {  // u's ranks, then what rounding left of them, with the same columns of B
+                            const int r = e % kRanks;
+                            mma_ss(tmem + db * kTileCols, ud + (((e >> 6) * 16384 + (e & 63) * 2) >> 4),
+                                   bd + (((r >> 6) * (kTileCols * 128) + (r & 63) * 2) >> 4), idesc, e > 0);
+                        }
+                        mma_commit(&b_free[bb]);
+                        mma_commit(&d_full[db]);
+                    }
+            }
+            __syncwarp();
+        } else {
+            const int row = threadIdx.x & 127, half = warp >> 2;
+            const int own = row < tokens ? __ldcg(ta.which + t0 + row) : -1;
+            const float mul = row < tokens ? __ldcg(ta.unit + t0 + row) : 0.f;
+            const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64;
+            int several[kTileAdapters];
+#pragma unroll
+            for (int j = 0; j < kTileAdapters; ++j) several[j] = j < adapters ? __ldcg(list + 1 + j) : -2;
+            int nn = n, mm = m;
+            for (int q = q0; q < q1; ++q, ++nn) {
+                const int yb = nn % S::kY;
+                uint8_t* half_ring = y_ring + yb * S::kYBytes + half * 16384;
+                uint8_t* y = half_ring + row * 128;
+                if (!failed && !warp_wait(&y_full[yb], (nn / S::kY) & 1)) failed = true;
+#pragma unroll
+                for (int j = 0; j < kTileAdapters; ++j) {
+                    if (j >= adapters) break;
+                    const int db = mm & 1;
+                    if (!failed && !warp_wait(&d_full[db], (mm / 2) & 1)) failed = true;
                     const bool hit = own == several[j];
                     if (!failed && __any_sync(0xffffffffu, hit)) {
                         tc_fence_after_sync();
+                        uint32_t d[2][32];
+                        __syncwarp();
+                        tmem_ld_x32(lanes + db * kTileCols, d[0]);
+                        tmem_ld_x32(lanes + db * kTileCols + 32, d[1]);
+                        tmem_ld_wait();
+                        if (hit) {
 #pragma unroll
-                        for (int h = 0; h < kTileCols / 32; ++h) {
-                            uint32_t d[32];
-                            __syncwarp();
-                            tmem_ld_x32(lanes + db * kTileCols + h * 32, d);
-                            tmem_ld_wait();
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                if (!hit) break;
-                                uint4* at = reinterpret_cast<uint4*>(y + (h >> 1) * 16384 + ((((h & 1) * 4 + i) ^ (row & 7)) << 4));
-                                const uint4 w = *at;
+                            for (int i = 0; i < 8; ++i) {
+                                uint4* at16 = reinterpret_cast<uint4*>(y + ((i ^ (row & 7)) << 4));
+                                const uint4 w = *at16;
                                 const uint32_t in[4] = {w.x, w.y, w.z, w.w};
                                 uint32_t out[4];
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) {
                                     const float2 f = unpack16<F16>(in[k]);
-                                    out[k] = pack16<F16>(fmaf(__uint_as_float(d[i * 8 + 2 * k]), mul, f.x), fmaf(__uint_as_float(d[i * 8 + 2 * k + 1]), mul, f.y));
+                                    out[k] = pack16<F16>(fmaf(__uint_as_float(d[i >> 2][(i & 3) * 8 + 2 * k]), mul, f.x),
+                                                         fmaf(__uint_as_float(d[i >> 2][(i & 3) * 8 + 2 * k + 1]), mul, f.y));
                                 }
-                                *at = make_uint4(out[0], out[1], out[2], out[3]);
+                                *at16 = make_uint4(out[0], out[1], out[2], out[3]);
                             }
                         }
                         tc_fence_before_sync();
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&d_free[db]);
+                    ++mm;
                 }
                 fence_proxy_async_smem();
-                asm volatile("bar.sync 1, 128;" ::: "memory");
-                if (threadIdx.x == 128 && !failed) {
-                    tma_store_2d(&tmap_out, ring + yb * S::kYBytes, q * kTileCols, t0);
-                    if (q * kTileCols + 64 < a.N) tma_store_2d(&tmap_out, ring + yb * S::kYBytes + 16384, q * kTileCols + 64, t0);
+                if (half == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
+                else asm volatile("bar.sync 2, 128;" ::: "memory");
+                if ((threadIdx.x & 127) == 0 && !failed) {
+                    if (q * kTileCols + half * 64 < a.N) tma_store_2d(&tmap_out, half_ring, q * kTileCols + half * 64, t0);
                     tma_store_commit();
-                    if (n > 0) {
+                    if (q > q0) {
                         tma_store_wait_read<1>();  // all but this one
-                        mbar_arrive(&y_free[(n - 1) % S::kY]);
+                        mbar_arrive(&y_free[(nn - 1) % S::kY]);
+                    }
+                    if (q == q1 - 1) {
+                        tma_store_wait_read<0>();
+                        mbar_arrive(&y_free[yb]);
                     }
                 }
+                __syncwarp();
             }
-            if (threadIdx.x == 128) tma_store_wait_all<0>();
         }
-        __syncwarp();
+        ++seg;
+        n += q1 - q0;
+        m += (q1 - q0) * adapters;
+        tc_fence_before_sync();
+        __syncthreads();  // all has been read: the next tile's copies may come
+        tc_fence_after_sync();
     }
+    if ((threadIdx.x & 127) == 0 && warp < 8) tma_store_wait_all<0>();
     if (failed) {
         atomicExch(a.status, 1);
         for (int i = 0; i < 2000; ++i) __nanosleep(1000);  // let copies and products in flight end before their memory goes away
     }
-    tc_fence_before_sync();
     __syncthreads();
-    if (warp == 2) tmem_dealloc(tmem, 256);
-}
-
-// How many clusters of the tile kernel the GPU holds at a time (once per device).
-template <typename Kernel>
-int resident_clusters(Kernel kernel, int smem) {
-    static int known[64] = {};
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 0;
-    if (known[dev] == 0) {
-        cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(kAdCtas * 32);
-        cfg.blockDim = dim3(kAdThreads);
-        cfg.dynamicSmemBytes = smem;
-        cudaLaunchAttribute attr[1];
-        attr[0].id = cudaLaunchAttributeClusterDimension;
-        attr[0].val.clusterDim.x = kAdCtas;
-        attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-        cfg.attrs = attr;
-        cfg.numAttrs = 1;
-        int n = 0;
-        if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-            cudaGetLastError();
-            n = 0;
-        }
-        known[dev] = n > 0 ? n : sm_count() / kAdCtas;
-    }
-    return known[dev];
+    if (warp == 9) tmem_dealloc(tmem, 2 * kTileCols);
 }
 
 template <bool F16, int RT>
-int launch_adapters_tiles(AdapterArgs a, cudaStream_t s) {
-    using S = TileShape<RT>;
-    auto kernel = adapters_tile_kernel<F16, RT>;
-    FORGE_SET_SMEM_ONCE(kernel, S::kSmem);
-    const int clusters = resident_clusters(kernel, S::kSmem);
-    if (clusters <= 0) return FORGE_ERR_CUDA;
-    // as many turns of all the clusters that run at a time as tiles of 128 take, in even tiles
-    const long long turns = (a.T + 128LL * clusters - 1) / (128LL * clusters);
-    const long long want = (a.T + turns * clusters - 1) / (turns * clusters);
-    a.tile = (int)((want + 7) / 8 * 8);
-    CUtensorMap tx, ta, ty, tb, to;
+int launch_adapters_tiles(const AdapterArgs& a, void* workspace, cudaStream_t s) {
+    using C = ContractShape<RT>;
+    using O = OutputShape<RT>;
+    const long long tiles = ((long long)a.T + kTileRows - 1) / kTileRows, chunks = tiles * ((a.N + kTileCols - 1) / kTileCols);
+    const int sms = sm_count();
+    // clusters of four where those of eight would not all run at a time (two CTAs to an SM, and SMs that no cluster fits on)
+    const bool wide = tiles * kAdCtas * (RT == 8 ? 2 : 1) <= sms * 3 / 2;
+    auto contract = wide ? adapters_contract_kernel<F16, RT, kAdCtas> : adapters_contract_kernel<F16, RT, kAdCtas / 2>;
+    auto output = adapters_output_kernel<F16, RT>;
+    FORGE_SET_SMEM_ONCE((adapters_contract_kernel<F16, RT, kAdCtas>), C::kSmem);
+    FORGE_SET_SMEM_ONCE((adapters_contract_kernel<F16, RT, kAdCtas / 2>), C::kSmem);
+    FORGE_SET_SMEM_ONCE(output, O::kSmem);
+    const TileWorkspace w(a.T, C::kRanks);
+    char* base = static_cast<char*>(workspace);
+    TileArgs t = {a, reinterpret_cast<int*>(base), reinterpret_cast<int*>(base + w.list), reinterpret_cast<float*>(base + w.unit), reinterpret_cast<uint32_t*>(base + w.u)};
+    CUtensorMap tx, ta, tu, ty, tb, to;
     auto rows = [&](CUtensorMap* m, const void* p, int64_t width, int64_t n, int64_t stride, int box_rows) {
         const uint64_t dims[2] = {(uint64_t)width, (uint64_t)n}, strides[1] = {(uint64_t)stride * 2};
         const uint32_t box[2] = {64, (uint32_t)box_rows};
         return encode_tmap_bf16_sw128(m, p, 2, dims, strides, box);
     };
-    if (!rows(&tx, a.x, a.K, a.T, a.xs, a.tile) || !rows(&ta, a.a, a.K, (int64_t)a.n * a.rank, a.K, S::kRanks) ||
-        !rows(&ty, a.y, a.N, a.T, a.ys, a.tile) || !rows(&tb, a.b, a.rank, (int64_t)a.n * a.N, a.rank, kTileCols) ||
-        !rows(&to, a.out, a.N, a.T, a.os, a.tile))
+    if (!rows(&tx, a.x, a.K, a.T, a.xs, kTileRows) || !rows(&ta, a.a, a.K, (int64_t)a.n * a.rank, a.K, C::kRanks) ||
+        !rows(&tu, t.u, 2 * C::kRanks, a.T, 2 * C::kRanks, kTileRows) || !rows(&ty, a.y, a.N, a.T, a.ys, kTileRows) ||
+        !rows(&tb, a.b, a.rank, (int64_t)a.n * a.N, a.rank, kTileCols) || !rows(&to, a.out, a.N, a.T, a.os, kTileRows))
         return FORGE_ERR_CUDA;
-    const long long tiles = ((long long)a.T + a.tile - 1) / a.tile;
-    FORGE_CUDA_TRY(launch_pdl_cluster(kernel, dim3((unsigned)(tiles * kAdCtas)), dim3(kAdThreads), S::kSmem, kAdCtas, s, tx, ta, ty, tb, to, a));
-    return finish_launch(1);
+    const int ctas = wide ? kAdCtas : kAdCtas / 2;
+    FORGE_CUDA_TRY(launch_pdl_cluster(contract, dim3((unsigned)(tiles * ctas)), dim3(kAdThreads), C::kSmem, ctas, s, tx, ta, t));
+    FORGE_CUDA_TRY(launch_pdl(output, dim3((unsigned)(chunks < sms ? chunks : sms)), dim3(O::kThreads), O::kSmem, s, tu, ty, tb, to, t));
+    return finish_launch(2);
 }
 
 template <bool F16, int RT, bool SMALL>
@@ -701,29 +951,34 @@ int launch_adapters(const AdapterArgs& a, cudaStream_t s) {
     return finish_launch(1);
 }
 template <bool F16, int RT>
-int launch_adapters(const AdapterArgs& a, cudaStream_t s) {
-    if constexpr (RT <= 4)
-        if (a.T >= kTileTokens && (long long)a.n * a.N < (1LL << 31)) return launch_adapters_tiles<F16, RT>(a, s);
+int launch_adapters(const AdapterArgs& a, void* workspace, cudaStream_t s) {
+    if (a.T >= kTileTokens) return launch_adapters_tiles<F16, RT>(a, workspace, s);
     return a.tile <= 8 ? launch_adapters<F16, RT, true>(a, s) : launch_adapters<F16, RT, false>(a, s);
 }
 template <bool F16>
-int launch_adapters(const AdapterArgs& a, cudaStream_t s) {
-    return a.rank <= 16   ? launch_adapters<F16, 1>(a, s)
-           : a.rank <= 32 ? launch_adapters<F16, 2>(a, s)
-           : a.rank <= 64 ? launch_adapters<F16, 4>(a, s)
-                          : launch_adapters<F16, 8>(a, s);
+int launch_adapters(const AdapterArgs& a, void* workspace, cudaStream_t s) {
+    return a.rank <= 16   ? launch_adapters<F16, 1>(a, workspace, s)
+           : a.rank <= 32 ? launch_adapters<F16, 2>(a, workspace, s)
+           : a.rank <= 64 ? launch_adapters<F16, 4>(a, workspace, s)
+                          : launch_adapters<F16, 8>(a, workspace, s);
 }
 
 }  // namespace
 }  // namespace forge
 
+extern "C" size_t forge_linear_adapters_workspace_bytes(int T, int rank) {
+    using namespace forge;
+    if (T < kTileTokens || rank <= 0 || rank > 128) return 0;
+    return TileWorkspace(T, padded_ranks(rank)).bytes;
+}
+
 extern "C" int forge_linear_adapters(const forge_adapters* set, const void* x, const void* y, void* out, int T, int64_t x_stride,
                                      int64_t y_stride, int64_t out_stride, const int32_t* requests, const int32_t* adapters, int R,
-                                     void* stream) {
+                                     void* workspace, size_t workspace_bytes, void* stream) {
     using namespace forge;
     if (!set || !set->a || !set->b || !x || !y || !out || !adapters || T <= 0 || R <= 0) return FORGE_ERR_INVALID_ARG;
     if (set->n <= 0 || set->rank <= 0 || set->K <= 0 || set->N <= 0 || x_stride < 0 || y_stride < 0 || out_stride < 0) return FORGE_ERR_INVALID_ARG;
-    if (!aligned16(set->a) || !aligned16(set->b) || !aligned16(x) || !aligned16(y) || !aligned16(out)) return FORGE_ERR_INVALID_ARG;
+    if (!aligned16(set->a) || !aligned16(set->b) || !aligned16(x) || !aligned16(y) || !aligned16(out) || !aligned16(workspace)) return FORGE_ERR_INVALID_ARG;
     auto odd4 = [](const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; };
     if (odd4(set->scales) || odd4(requests) || odd4(adapters) || (!requests && R != T)) return FORGE_ERR_INVALID_ARG;
     if (set->dtype != FORGE_DTYPE_BF16 && set->dtype != FORGE_DTYPE_F16) return set->dtype == FORGE_DTYPE_F32 ? FORGE_ERR_UNSUPPORTED : FORGE_ERR_INVALID_ARG;
@@ -735,6 +990,10 @@ extern "C" int forge_linear_adapters(const forge_adapters* set, const void* x, c
     if (y == out && a.ys != a.os) return FORGE_ERR_INVALID_ARG;
     if (set->K % 8 != 0 || set->N % 8 != 0 || set->rank % 8 != 0 || set->rank > 128) return FORGE_ERR_UNSUPPORTED;
     if (a.xs % 8 != 0 || a.ys % 8 != 0 || a.os % 8 != 0) return FORGE_ERR_UNSUPPORTED;
+    if ((long long)set->n * set->N >= (1LL << 31) || (long long)set->n * set->rank >= (1LL << 31)) return FORGE_ERR_UNSUPPORTED;  // counted in 32 bits
+    const size_t need = forge_linear_adapters_workspace_bytes(T, set->rank);
+    if (need > 0 && !workspace) return FORGE_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return FORGE_ERR_WORKSPACE;
     a.x = x; a.y = y; a.out = out;
     a.a = set->a; a.b = set->b;
     a.scales = set->scales;
@@ -747,9 +1006,7 @@ extern "C" int forge_linear_adapters(const forge_adapters* set, const void* x, c
     a.status = device_status_word();
     if (sms <= 0 || !a.status) return FORGE_ERR_CUDA;
     const int want = (T + sms / 4 - 1) / (sms / 4);
-    a.tile = want <= 8 ? want : want <= 16 ? 16 : want <= 32 ? 32 : want <= 64 ? 64 : 128;
-    if (a.rank > 64 && a.tile > 64) a.tile = 64;
-    if ((long long)T / a.tile >= (1LL << 28)) return FORGE_ERR_UNSUPPORTED;
+    a.tile = want <= 8 ? want : 16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    return set->dtype == FORGE_DTYPE_F16 ? launch_adapters<true>(a, s) : launch_adapters<false>(a, s);
+    return set->dtype == FORGE_DTYPE_F16 ? launch_adapters<true>(a, workspace, s) : launch_adapters<false>(a, workspace, s);
 }

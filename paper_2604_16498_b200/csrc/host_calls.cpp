@@ -384,6 +384,7 @@ struct PagesEntries {
     decltype(&forge_attn_decode_pages) decode;
     decltype(&forge_attn_tree_pages) tree;
     decltype(&forge_linear_adapters) adapters;
+    decltype(&forge_linear_adapters_workspace_bytes) adapters_workspace;
 } pages;
 bool pages_bound = false;
 bool pages_ready(Py_ssize_t n, Py_ssize_t want) { return pages_bound && ready(n, want); }
@@ -520,23 +521,25 @@ PyObject* py_tree_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// adapters(x, y, a, b, adapters, requests or None, scales or None, out)
+// adapters(x, y, a, b, adapters, requests or None, scales or None, out, workspace or None); a call that needs a workspace and has none goes the general way
 PyObject* py_adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded([&]() -> PyObject* {
         at::ScalarType ty;
         forge_adapters d = {};
         int T, R;
-        bool no_r, no_s;
+        bool no_r, no_s, no_w;
         int64_t xs[1], ys[1], os[1];
-        if (!pages_ready(n, 8) || !is_16_bit(a[0], &ty)) return not_plain();
+        if (!pages_ready(n, 9) || !is_16_bit(a[0], &ty)) return not_plain();
         const at::Tensor *x = plain_view(a[0], ty, xs, 2), *y = plain_view(a[1], ty, ys, 2), *out = plain_view(a[7], ty, os, 2);
         const at::Tensor *wa = plain(a[2], ty, 3), *wb = plain(a[3], ty, 3), *ad = plain(a[4], at::kInt, 1);
         const at::Tensor *r = plain_or_none(a[5], at::kInt, 1, &no_r), *sc = plain_or_none(a[6], at::kFloat, 1, &no_s);
-        if (!x || !y || !out || !wa || !wb || !ad || (!r && !no_r) || (!sc && !no_s)) return not_plain();
+        const at::Tensor* ws = plain_or_none(a[8], at::kByte, 1, &no_w);
+        if (!x || !y || !out || !wa || !wb || !ad || (!r && !no_r) || (!sc && !no_s) || (!ws && !no_w)) return not_plain();
         const auto as = wa->sizes(), bs = wb->sizes();
         if (!small(x->size(0), &T) || !small(x->size(1), &d.K) || !small(y->size(1), &d.N) || !small(as[0], &d.n) || !small(as[1], &d.rank) ||
             !small(ad->size(0), &R) || !sized(y, T) || !sized(out, T, d.N) || as[2] != d.K || bs[0] != d.n || bs[1] != d.N || bs[2] != d.rank ||
-            !sized(r, T) || !sized(sc, d.n) || (!r && R != T) || !here({x, y, out, wa, wb, ad, r, sc}))
+            !sized(r, T) || !sized(sc, d.n) || (!r && R != T) || !here({x, y, out, wa, wb, ad, r, sc, ws}) ||
+            (!ws && pages.adapters_workspace(T, d.rank) > 0))
             return not_plain();
         const int64_t sx = T > 1 ? xs[0] : 0, sy = T > 1 ? ys[0] : 0, so = T > 1 ? os[0] : 0;
         d.a = address(wa);
@@ -545,15 +548,17 @@ PyObject* py_adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
         d.dtype = dtype_of(ty);
         void *px = address(x), *py = address(y), *po = address(out), *s = stream();
         const int32_t *pr = ints(r), *pa = ints(ad);
-        return run([&] { return pages.adapters(&d, px, py, po, T, sx, sy, so, pr, pa, R, s); });
+        void* pw = address(ws);
+        const size_t bytes = ws ? (size_t)ws->numel() : 0;
+        return run([&] { return pages.adapters(&d, px, py, po, T, sx, sy, so, pr, pa, R, pw, bytes, s); });
     });
 }
 
-// bind_pages(addresses of the six entry points, in the order of PagesEntries); after bind()
+// bind_pages(addresses of the seven entry points, in the order of PagesEntries); after bind()
 PyObject* py_bind_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    void* p[6];
-    if (n != 6) { PyErr_SetString(PyExc_TypeError, "six addresses expected"); return nullptr; }
-    for (int i = 0; i < 6; ++i) {
+    void* p[7];
+    if (n != 7) { PyErr_SetString(PyExc_TypeError, "seven addresses expected"); return nullptr; }
+    for (int i = 0; i < 7; ++i) {
         p[i] = PyLong_AsVoidPtr(a[i]);
         if (!p[i]) {
             if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "address expected");
@@ -566,6 +571,7 @@ PyObject* py_bind_pages(PyObject*, PyObject* const* a, Py_ssize_t n) {
     pages.decode = reinterpret_cast<decltype(pages.decode)>(p[3]);
     pages.tree = reinterpret_cast<decltype(pages.tree)>(p[4]);
     pages.adapters = reinterpret_cast<decltype(pages.adapters)>(p[5]);
+    pages.adapters_workspace = reinterpret_cast<decltype(pages.adapters_workspace)>(p[6]);
     pages_bound = true;
     Py_RETURN_NONE;
 }

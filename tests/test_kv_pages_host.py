@@ -133,19 +133,25 @@ def test_attention_refusals(lib):
 
 
 def test_adapters_refusals(lib):
-    def call(s="given", x=P, y=P + 4096, out=P + 8192, T=3, xs=0, ys=0, os=0, requests=P, adapters=P, R=2, **kw):
+    def call(s="given", x=P, y=P + 4096, out=P + 8192, T=3, xs=0, ys=0, os=0, requests=P, adapters=P, R=2, ws=None, nws=0, **kw):
         a = dict(a=P, b=P, scales=P, n=2, rank=16, K=64, N=64, dtype=0)
         a.update(kw)
         d = binding.AdaptersDesc(**a)
-        return lib.forge_linear_adapters(None if s is None else ctypes.byref(d), x, y, out, T, xs, ys, os, requests, adapters, R, None)
+        return lib.forge_linear_adapters(None if s is None else ctypes.byref(d), x, y, out, T, xs, ys, os, requests, adapters, R, ws, nws, None)
 
     for kw in (dict(s=None), dict(a=None), dict(b=None), dict(a=P + 8), dict(b=P + 2), dict(scales=P + 2), dict(n=0), dict(rank=0), dict(K=0), dict(N=-8),
                dict(dtype=3), dict(dtype=-1), dict(x=None), dict(y=None), dict(out=None), dict(x=P + 8), dict(y=P + 8), dict(out=P + 4), dict(T=0),
                dict(R=0), dict(adapters=None), dict(adapters=P + 2), dict(requests=P + 2), dict(requests=None), dict(xs=56), dict(ys=32), dict(os=63),
                dict(xs=-64), dict(y=P, out=P, ys=128, os=64)):
         assert call(**kw) == BAD, kw
-    for kw in (dict(dtype=2), dict(rank=12), dict(rank=136), dict(K=60), dict(N=68), dict(xs=68), dict(ys=70), dict(os=66)):
+    for kw in (dict(dtype=2), dict(rank=12), dict(rank=136), dict(K=60), dict(N=68), dict(xs=68), dict(ys=70), dict(os=66),
+               dict(n=1 << 26), dict(n=1 << 28, N=8)):
         assert call(**kw) == UNS, kw
+    # many tokens need a workspace
+    need = lib.forge_linear_adapters_workspace_bytes(600, 16)
+    assert need >= 600 * (16 * 4 + 8) and lib.forge_linear_adapters_workspace_bytes(511, 16) == 0
+    assert lib.forge_linear_adapters_workspace_bytes(600, 130) == 0 and lib.forge_linear_adapters_workspace_bytes(-5, 16) == 0
+    assert call(T=600) == BAD and call(T=600, ws=P + 8, nws=need) == BAD and call(T=600, ws=P, nws=need - 1) == WS
 
 
 def test_the_binding_checks_shapes_and_places():
@@ -174,7 +180,7 @@ def test_what_is_not_plain_goes_the_general_way():
     binding.load()
     c = binding._host_calls
     assert c is not None
-    for bad in ((), (1,) * 5, (1,) * 7, (0,) * 6, ("x",) * 6):
+    for bad in ((), (1,) * 6, (1,) * 8, (0,) * 7, ("x",) * 7):
         with pytest.raises((TypeError, ValueError)):
             c.bind_pages(*bad)
     x, i, t = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32), torch.zeros(4, 3, dtype=torch.int32)
@@ -187,7 +193,7 @@ def test_what_is_not_plain_goes_the_general_way():
             assert c.read_pages(at, dev, t, x[None], x[None], None, None) == -1
             assert c.decode_pages(at, dev, x, t, i, None, x, ws) == -1
             assert c.tree_pages(at, dev, x[None], t, i, None, None, x[None], ws) == -1
-    assert c.adapters(x[:, 0], x[:, 0], x, x, i, None, None, x[:, 0]) == -1
+    assert c.adapters(x[:, 0], x[:, 0], x, x, i, None, None, x[:, 0], None) == -1
     for fn in (c.assign_pages, c.append_pages, c.read_pages, c.decode_pages, c.tree_pages, c.adapters):
         for bad in ((), (None,), (None,) * 7, (None,) * 8, (None,) * 9, (None,) * 10, (x,) * 8, (0,) * 10):
             assert fn(*bad) == -1

@@ -64,16 +64,18 @@ def test_ranks_and_tokens(dtype, rank, T, runs):
 
 @TYPES
 @pytest.mark.parametrize("K,N", [(8, 8), (64, 64), (72, 4096), (4096, 72), (768, 2304), (1000, 520), (14336, 136), (2048, 8192)])
-@pytest.mark.parametrize("T,runs", [(5, 2), (400, 30)])
+@pytest.mark.parametrize("T,runs", [(5, 2), (400, 30), (700, 130)])
 def test_widths(dtype, K, N, T, runs):
     check(2, dtype, T, 3, 16, K, N, runs=runs)
 
 
 @TYPES
-@pytest.mark.parametrize("T", [2000, 2369, 4737, 9000])
+@pytest.mark.parametrize("T", [512, 640, 2000, 2369, 4737, 9000])
 def test_large_tiles(dtype, T):
     """Runs that begin and end anywhere in a tile, one of all its tokens, and tokens in turns."""
     check(3, dtype, T, 5, 64, 512, 256, runs=157)
+    check(6, dtype, T, 40, 72, 192, 392, which=(torch.arange(T, device="cuda") // 900 * 7 + torch.arange(T, device="cuda") % 900 // 850 * torch.arange(T, device="cuda")) % 41 - 1)
+    check(7, dtype, T, 6, 24, 64, 136, which=torch.where(torch.arange(T, device="cuda") < 512, -1, 3))
     check(4, dtype, T, 2, 8, 128, 64, which=torch.arange(T, device="cuda") % 3 - 1)
     check(5, dtype, T, 1, 128, 128, 128, which=torch.zeros(T, device="cuda"), with_scales=False)
 
@@ -91,7 +93,7 @@ def test_requests_say_whose_a_token_is():
 
 
 @TYPES
-@pytest.mark.parametrize("T", [9, 500])
+@pytest.mark.parametrize("T", [9, 500, 645])
 def test_views_and_in_place(dtype, T):
     """The columns of a fused projection, in place; what lies beside them stays."""
     g, x, _, a, b, scales = make(7, dtype, T, 3, 32, 128, 64)
@@ -110,7 +112,7 @@ def test_views_and_in_place(dtype, T):
 
 
 @TYPES
-@pytest.mark.parametrize("T", [6, 300])
+@pytest.mark.parametrize("T", [6, 300, 650])
 def test_what_is_no_number_stays_with_its_token_and_adapter(dtype, T):
     g, x, y, a, b, scales = make(8, dtype, T, 4, 16, 192, 128)
     which = (torch.arange(T, device="cuda") // 2 % 3).int()      # adapter 3 is nobody's
