@@ -498,12 +498,12 @@ struct TileArgs {
 template <int RT>
 struct ContractShape {
     static constexpr int kRanks = RT * 16;
-    static constexpr int kStage = 16384 + kRanks * 128;          // x's and A's 64 of K
-    static constexpr int kStages = RT == 8 ? 4 : RT == 4 ? 3 : 4;  // (with these two CTAs to an SM, but for RT = 8)
-    static constexpr int kInboxOff = kStages * kStage;
+    static constexpr int kABytes = kRanks * 128;                 // an adapter's 64 of K
+    static constexpr int kX = RT == 4 ? 3 : 4, kA = RT == 4 ? 3 : 4;  // buffers of x's 64 of K and of A's (with these two CTAs to an SM, but for RT = 8)
+    static constexpr int kAOff = kX * 16384, kInboxOff = kAOff + kA * kABytes;
     static constexpr int kSmem = 1024 + kInboxOff + kTileRows * kRanks * 4;
     static constexpr int kTmemCols = kTileAdapters * kRanks;
-    static_assert(kTileRows * kRanks * 4 <= kInboxOff && kStage % 1024 == 0, "by groups: what the CTA has of u, in the ring's place");
+    static_assert(kTileRows * kRanks * 4 <= kInboxOff && kInboxOff % 1024 == 0, "by groups: what the CTA has of u, in the rings' place");
     static_assert(kSmem <= 232448 - 4096 && (RT == 8 || 2 * (kSmem + 4096) <= 232448), "shared memory");
 };
 
@@ -518,7 +518,7 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
     __shared__ AdGroup groups[kTileRows];
     __shared__ int which[kTileRows], base[kTileRows], several[kTileAdapters];
     __shared__ int n_groups, n_several;
-    __shared__ uint64_t x_full[S::kStages], x_free[S::kStages], u_done;
+    __shared__ uint64_t x_full[S::kX], x_free[S::kX], a_full[S::kA], a_free[S::kA], u_done;
     __shared__ uint32_t tmem_slot;
     const AdapterArgs& a = ta.a;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -528,7 +528,8 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
     float* inbox = reinterpret_cast<float*>(ring + S::kInboxOff);
     ad_arrive();  // waited for before the first store into another CTA's shared memory
     if (threadIdx.x == 0) {
-        for (int i = 0; i < S::kStages; ++i) { mbar_init(&x_full[i], 2); mbar_init(&x_free[i], 1); }  // full: x, and A
+        for (int i = 0; i < S::kX; ++i) { mbar_init(&x_full[i], 1); mbar_init(&x_free[i], 1); }
+        for (int i = 0; i < S::kA; ++i) { mbar_init(&a_full[i], 1); mbar_init(&a_free[i], 1); }
         mbar_init(&u_done, 1);
         fence_mbar_init();
         prefetch_tmap(&tmap_x);
@@ -541,12 +542,12 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
     pdl_launch_dependents();
     pdl_wait();
     const int blocks = (a.K + 63) / 64, my_blocks = cta < blocks ? (blocks - cta + CTAS - 1) / CTAS : 0;
-    const int early = min(my_blocks, S::kStages);
+    const int early = min(my_blocks, S::kX);
     __syncthreads();
     if (warp == 3 && elect_one()) {  // the first of x, whatever adapters it will meet
         for (int i = 0; i < early; ++i) {
             mbar_expect_tx(&x_full[i], 16384);
-            tma_load_2d(ring + i * S::kStage, &tmap_x, &x_full[i], (cta + i * CTAS) * 64, t0);
+            tma_load_2d(ring + i * 16384, &tmap_x, &x_full[i], (cta + i * CTAS) * 64, t0);
         }
     }
     __syncwarp();
@@ -589,10 +590,7 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
     const uint32_t inbox_addr = smem_u32(inbox);
     if (!tiled || adapters == 0) {  // what has come of x is not wanted
         if (threadIdx.x == 0)
-            for (int i = 0; i < early && !failed; ++i) {
-                mbar_arrive(&x_full[i]);
-                if (!mbar_wait(&x_full[i], 0)) failed = true;
-            }
+            for (int i = 0; i < early && !failed; ++i) failed = !mbar_wait(&x_full[i], 0);
         __syncthreads();
     }
     if (!tiled) {
@@ -605,31 +603,39 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
         send_parts<RT>(mine, inbox_addr, tokens, kPer, cta);
     } else {
         if (warp == 0 && elect_one()) {
-            int n = 0;
-            for (int j = 0; j < adapters && !failed; ++j)
-                for (int i = 0; i < my_blocks; ++i, ++n) {
-                    const int st = n % S::kStages, k = (cta + i * CTAS) * 64;
-                    if (n >= S::kStages && !mbar_wait(&x_free[st], (n / S::kStages - 1) & 1)) { failed = true; break; }
-                    if (n >= early) {
-                        mbar_expect_tx(&x_full[st], 16384);
-                        tma_load_2d(ring + st * S::kStage, &tmap_x, &x_full[st], k, t0);
-                    }
-                    mbar_expect_tx(&x_full[st], kRanks * 128);
-                    tma_load_2d(ring + st * S::kStage + 16384, &tmap_a, &x_full[st], k, several[j] * a.rank);
+            int n = 0;  // A's
+            for (int i = 0; i < (adapters > 0 ? my_blocks : 0) && !failed; ++i) {
+                const int xb = i % S::kX, k = (cta + i * CTAS) * 64;
+                if (i >= early) {
+                    if (!mbar_wait(&x_free[xb], (i / S::kX - 1) & 1)) { failed = true; break; }
+                    mbar_expect_tx(&x_full[xb], 16384);
+                    tma_load_2d(ring + xb * 16384, &tmap_x, &x_full[xb], k, t0);
                 }
+                for (int j = 0; j < adapters; ++j, ++n) {
+                    const int ab = n % S::kA;
+                    if (n >= S::kA && !mbar_wait(&a_free[ab], (n / S::kA - 1) & 1)) { failed = true; break; }
+                    mbar_expect_tx(&a_full[ab], S::kABytes);
+                    tma_load_2d(ring + S::kAOff + ab * S::kABytes, &tmap_a, &a_full[ab], k, several[j] * a.rank);
+                }
+            }
         } else if (warp == 1 && elect_one()) {
             constexpr uint32_t idesc = F16 ? make_idesc_f16(128, kRanks, false, false) : make_idesc_bf16(128, kRanks, false, false);
             int n = 0;
-            for (int j = 0; j < adapters && !failed; ++j)
-                for (int i = 0; i < my_blocks; ++i, ++n) {
-                    const int st = n % S::kStages;
-                    if (!mbar_wait(&x_full[st], (n / S::kStages) & 1)) { failed = true; break; }
+            for (int i = 0; i < (adapters > 0 ? my_blocks : 0) && !failed; ++i) {
+                const int xb = i % S::kX;
+                if (!mbar_wait(&x_full[xb], (i / S::kX) & 1)) { failed = true; break; }
+                const uint64_t xd = make_smem_desc(smem_u32(ring + xb * 16384), 16, 1024);
+                for (int j = 0; j < adapters; ++j, ++n) {
+                    const int ab = n % S::kA;
+                    if (!mbar_wait(&a_full[ab], (n / S::kA) & 1)) { failed = true; break; }
                     tc_fence_after_sync();
-                    const uint64_t xd = make_smem_desc(smem_u32(ring + st * S::kStage), 16, 1024), ad = make_smem_desc(smem_u32(ring + st * S::kStage + 16384), 16, 1024);
+                    const uint64_t ad = make_smem_desc(smem_u32(ring + S::kAOff + ab * S::kABytes), 16, 1024);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) mma_ss(tmem + j * kRanks, xd + (k * 32 >> 4), ad + (k * 32 >> 4), idesc, i > 0 || k > 0);
-                    mma_commit(&x_free[st]);
+                    mma_commit(&a_free[ab]);
                 }
+                mma_commit(&x_free[xb]);
+            }
             if (n == 0) mbar_arrive(&u_done);
             else if (!failed) mma_commit(&u_done);
         }
@@ -681,6 +687,10 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
     if (warp == 2) tmem_dealloc(tmem, S::kTmemCols);
 }
 
+// What a chunk of a tile's columns takes, in quarters of one with one adapter: each further adapter costs a product, its B and a pass of the warps whose rows
+// have it; by groups a chunk takes about five times as long.
+__device__ __forceinline__ int chunk_cost(int adapters) { return adapters > kTileAdapters ? 20 : 3 + max(adapters, 1); }
+
 template <int RT>
 struct OutputShape {
     static constexpr int kRanks = RT * 16;
@@ -706,6 +716,7 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
     __shared__ int which[kTileRows], base[kTileRows];
     __shared__ float unit[kTileRows];
     __shared__ int n_groups;
+    __shared__ long long share[2];
     __shared__ uint64_t u_full, y_full[S::kY], y_free[S::kY], b_full[S::kB], b_free[S::kB], d_full[2], d_free[2];
     __shared__ uint32_t tmem_slot;
     const AdapterArgs& a = ta.a;
@@ -734,10 +745,37 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
     pdl_launch_dependents();
     pdl_wait();
 
-    // this CTA's chunks of 128 columns, of all tiles'
-    const int chunks = (a.N + kTileCols - 1) / kTileCols;
-    const long long all = (long long)((a.T + kTileRows - 1) / kTileRows) * chunks;
-    const long long from = all * blockIdx.x / gridDim.x, to = all * (blockIdx.x + 1) / gridDim.x;
+    // This CTA's chunks of 128 columns: an even share of what all tiles' chunks take, in quarters of one with one adapter.
+    const int chunks = (a.N + kTileCols - 1) / kTileCols, tiles = (a.T + kTileRows - 1) / kTileRows;
+    if (warp == 0) {
+        auto cost = [&](int t) { return t < tiles ? chunk_cost(__ldcg(ta.list + t * kListInts)) : 0; };
+        long long all = 0;
+        for (int t = lane; t < tiles; t += 32) all += cost(t);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
+        all *= chunks;
+        const long long lo = all * blockIdx.x / gridDim.x, hi = all * (blockIdx.x + 1) / gridDim.x;
+        long long before = 0;
+        for (int t1 = 0; t1 < tiles; t1 += 32) {
+            const long long mine = (long long)cost(t1 + lane) * chunks;
+            long long incl = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const long long v = __shfl_up_sync(0xffffffffu, incl, o);
+                if (lane >= o) incl += v;
+            }
+            const long long start = before + incl - mine;
+            auto mark = [&](long long u, int e) {
+                if (mine > 0 && u >= start && u < start + mine) share[e] = (long long)(t1 + lane) * chunks + (u - start) / (mine / chunks);
+            };
+            mark(lo, 0);
+            mark(hi, 1);
+            before += __shfl_sync(0xffffffffu, incl, 31);
+        }
+        if (lane == 0 && hi == all) share[1] = (long long)tiles * chunks;
+    }
+    __syncthreads();
+    const long long from = share[0], to = share[1];
     bool failed = false;
     int n = 0, m = 0, seg = 0;  // chunks; chunks and adapters; tiles that went through the tensor cores, of this CTA so far
     for (long long at = from; at < to;) {
