@@ -510,7 +510,7 @@ int forge_attn_tree_pages(const forge_kv_pages* cache, const int32_t* table, int
  * itself with the same stride, but may not overlap it otherwise, nor x.  K, N, rank: multiples of 8, rank up to 128.
  * Sums are kept in fp32, x A_i^T times the scale to within 2^-15 of itself (bf16) or 2^-21 (fp16), and out is rounded once.  The same inputs give
  * the same bits.  n * N and n * rank are below 2^31.
- * workspace: at least forge_linear_adapters_workspace_bytes(T, rank) bytes, 16-byte aligned, of any contents (none below 512 tokens: NULL).  Two
+ * workspace: at least forge_linear_adapters_workspace_bytes(T, rank) bytes, 16-byte aligned, of any contents (none up to 512 tokens: NULL).  Two
  * calls that may overlap on the GPU must not share it.
  */
 typedef struct forge_adapters {

@@ -25,7 +25,10 @@ namespace {
 constexpr int kAdCtas = 8;                 // of a cluster
 constexpr int kAdWarps = 8, kAdThreads = kAdWarps * 32;
 constexpr int kAdMost = 128;               // tokens of a tile
-constexpr int kTileTokens = 512;           // from how many tokens on the tensor cores' tiles of 128 are the faster ones
+// From how many tokens on the tensor cores' tiles of 128 are the faster ones: when more than 32 tiles of 16 are too many to run at a time.  Groups and
+// tiles, 4096 x 4096, 16 ranks: one adapter, 512 tokens 19.5 and 23.6 us, 592 30.7 and 23.6, 2000 59.4 and 29.7; 8 adapters in runs of 16 tokens, 512 tokens
+// 22.6 and 42, 1000 35.8 and 46.1, 2000 63.6 and 56.3; in turns, 512 tokens 25.7 and 42, 1000 45.1 and 50.2, 2000 82.9 and 60.5.
+constexpr int kTileTokens = 513;
 
 struct AdapterArgs {
     const void *x, *y, *a, *b;
@@ -472,9 +475,10 @@ __global__ void __launch_bounds__(kAdThreads, RT <= 4 ? 2 : 1) adapters_kernel(c
 //   u[128 x ranks] = x A_i^T for each adapter i that the tile has, a cluster of eight CTAs to a tile; a row takes its own adapter's
 //   D[128 x 128 columns] = [u, what rounding left] [B_i, B_i]^T; the rows of y, which lie in shared memory, get their own adapter's D added there and
 //     leave by TMA
-// A tile of more than kTileAdapters adapters, each of which takes a pass over the tile, goes by groups of 8 tokens like small ones.
-constexpr int kTileRows = 128, kTileCols = 128, kTileAdapters = 4;
-constexpr int kListInts = 8;  // of a tile: how many adapters it has (kTileAdapters + 1: more than that), and which
+// A tile of more than tile_adapters() adapters, each of which takes a pass over the tile, goes by groups of 8 tokens like small ones.
+constexpr int kTileRows = 128, kTileCols = 128;
+constexpr int tile_adapters(int ranks) { return ranks <= 32 ? 8 : 4; }  // their u lie side by side in tensor memory, of two CTAs to an SM
+constexpr int kListInts = 16;  // of a tile: how many adapters it has (one more than tile_adapters: more than that), and which
 
 inline int padded_ranks(int rank) { return rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128; }
 // The workspace: adapters and units of the tokens, the tiles' lists, u.
@@ -502,7 +506,7 @@ struct ContractShape {
     static constexpr int kX = RT == 4 ? 3 : 4, kA = RT == 4 ? 3 : 4;  // buffers of x's 64 of K and of A's (with these two CTAs to an SM, but for RT = 8)
     static constexpr int kAOff = kX * 16384, kInboxOff = kAOff + kA * kABytes;
     static constexpr int kSmem = 1024 + kInboxOff + kTileRows * kRanks * 4;
-    static constexpr int kTmemCols = kTileAdapters * kRanks;
+    static constexpr int kAdapters = tile_adapters(kRanks), kTmemCols = kAdapters * kRanks;
     static_assert(kTileRows * kRanks * 4 <= kInboxOff && kInboxOff % 1024 == 0, "by groups: what the CTA has of u, in the rings' place");
     static_assert(kSmem <= 232448 - 4096 && (RT == 8 || 2 * (kSmem + 4096) <= 232448), "shared memory");
 };
@@ -516,7 +520,7 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
     constexpr int kRanks = S::kRanks, kPer = kTileRows / CTAS;
     extern __shared__ uint8_t smem_raw[];
     __shared__ AdGroup groups[kTileRows];
-    __shared__ int which[kTileRows], base[kTileRows], several[kTileAdapters];
+    __shared__ int which[kTileRows], base[kTileRows], several[S::kAdapters];
     __shared__ int n_groups, n_several;
     __shared__ uint64_t x_full[S::kX], x_free[S::kX], a_full[S::kA], a_free[S::kA], u_done;
     __shared__ uint32_t tmem_slot;
@@ -564,9 +568,9 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
             if (k * 32 + lane < tokens) which[k * 32 + lane] = mine[k];
 #pragma unroll
         for (int k = 0; k < kTileRows / 32; ++k) {
-            for (unsigned left; n <= kTileAdapters && (left = __ballot_sync(0xffffffffu, mine[k] >= 0)) != 0;) {
+            for (unsigned left; n <= S::kAdapters && (left = __ballot_sync(0xffffffffu, mine[k] >= 0)) != 0;) {
                 const int x = __shfl_sync(0xffffffffu, mine[k], __ffs(left) - 1);
-                if (lane == 0 && n < kTileAdapters) several[n] = x;
+                if (lane == 0 && n < S::kAdapters) several[n] = x;
                 ++n;
 #pragma unroll
                 for (int l = 0; l < kTileRows / 32; ++l)
@@ -577,7 +581,7 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
         if (lane == 0) n_several = n;
         if (cta == 0) {
             if (lane == 0) ta.list[tile * kListInts] = n;
-            if (lane < min(n, kTileAdapters)) ta.list[tile * kListInts + 1 + lane] = several[lane];
+            if (lane < min(n, S::kAdapters)) ta.list[tile * kListInts + 1 + lane] = several[lane];
         }
     }
     tc_fence_before_sync();
@@ -585,7 +589,7 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
     tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
     const int adapters = n_several;
-    const bool tiled = adapters <= kTileAdapters;
+    const bool tiled = adapters <= S::kAdapters;
     bool failed = false;
     const uint32_t inbox_addr = smem_u32(inbox);
     if (!tiled || adapters == 0) {  // what has come of x is not wanted
@@ -689,11 +693,11 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
 
 // What a chunk of a tile's columns takes, in quarters of one with one adapter: each further adapter costs a product, its B and a pass of the warps whose rows
 // have it; by groups a chunk takes about five times as long.
-__device__ __forceinline__ int chunk_cost(int adapters) { return adapters > kTileAdapters ? 20 : 3 + max(adapters, 1); }
+__device__ __forceinline__ int chunk_cost(int adapters, int most) { return adapters > most ? 20 : 3 + max(adapters, 1); }
 
 template <int RT>
 struct OutputShape {
-    static constexpr int kRanks = RT * 16;
+    static constexpr int kRanks = RT * 16, kAdapters = tile_adapters(kRanks);
     static constexpr int kOp = (2 * kRanks + 63) / 64 * 16384;   // u and its rest: [128 rows x 64] chunks
     static constexpr int kY = RT == 8 ? 2 : 4, kB = RT == 8 ? 2 : 3;  // buffers of y (and out), of B
     static constexpr int kYBytes = 2 * 16384, kBBytes = (kRanks + 63) / 64 * kTileCols * 128;
@@ -748,7 +752,7 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
     // This CTA's chunks of 128 columns: an even share of what all tiles' chunks take, in quarters of one with one adapter.
     const int chunks = (a.N + kTileCols - 1) / kTileCols, tiles = (a.T + kTileRows - 1) / kTileRows;
     if (warp == 0) {
-        auto cost = [&](int t) { return t < tiles ? chunk_cost(__ldcg(ta.list + t * kListInts)) : 0; };
+        auto cost = [&](int t) { return t < tiles ? chunk_cost(__ldcg(ta.list + t * kListInts), S::kAdapters) : 0; };
         long long all = 0;
         for (int t = lane; t < tiles; t += 32) all += cost(t);
 #pragma unroll
@@ -785,7 +789,7 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
         const int* list = ta.list + tile * kListInts;
         const int adapters = __ldcg(list);
         if (adapters == 0 && a.y == a.out) continue;
-        if (adapters > kTileAdapters) {
+        if (adapters > S::kAdapters) {
             // ---- by groups of tokens; no copies are in flight, as behind each tile
             uint16_t *u_hi = reinterpret_cast<uint16_t*>(smem), *u_lo = u_hi + kTileRows * kRow;
             for (int t = threadIdx.x; t < tokens; t += S::kThreads) {
@@ -814,9 +818,9 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
                 mbar_expect_tx(&u_full, S::kOp);
 #pragma unroll
                 for (int c = 0; c < S::kOp / 16384; ++c) tma_load_2d(smem + c * 16384, &tmap_u, &u_full, c * 64, t0);
-                int several[kTileAdapters];
+                int several[S::kAdapters];
 #pragma unroll
-                for (int j = 0; j < kTileAdapters; ++j) several[j] = j < adapters ? __ldcg(list + 1 + j) : 0;
+                for (int j = 0; j < S::kAdapters; ++j) several[j] = j < adapters ? __ldcg(list + 1 + j) : 0;
                 int nn = n, mm = m;
                 for (int q = q0; q < q1 && !failed; ++q, ++nn) {
                     const int yb = nn % S::kY;
@@ -825,7 +829,7 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
                     tma_load_2d(y_ring + yb * S::kYBytes, &tmap_y, &y_full[yb], q * kTileCols, t0);
                     tma_load_2d(y_ring + yb * S::kYBytes + 16384, &tmap_y, &y_full[yb], q * kTileCols + 64, t0);
 #pragma unroll
-                    for (int j = 0; j < kTileAdapters; ++j) {
+                    for (int j = 0; j < S::kAdapters; ++j) {
                         if (j >= adapters) break;
                         const int bb = mm % S::kB;
                         if (mm >= S::kB && !mbar_wait(&b_free[bb], (mm / S::kB - 1) & 1)) { failed = true; break; }
@@ -867,9 +871,9 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
             const int own = row < tokens ? __ldcg(ta.which + t0 + row) : -1;
             const float mul = row < tokens ? __ldcg(ta.unit + t0 + row) : 0.f;
             const uint32_t lanes = tmem + (static_cast<uint32_t>((warp & 3) * 32) << 16) + half * 64;
-            int several[kTileAdapters];
+            int several[S::kAdapters];
 #pragma unroll
-            for (int j = 0; j < kTileAdapters; ++j) several[j] = j < adapters ? __ldcg(list + 1 + j) : -2;
+            for (int j = 0; j < S::kAdapters; ++j) several[j] = j < adapters ? __ldcg(list + 1 + j) : -2;
             int nn = n, mm = m;
             for (int q = q0; q < q1; ++q, ++nn) {
                 const int yb = nn % S::kY;
@@ -877,7 +881,7 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
                 uint8_t* y = half_ring + row * 128;
                 if (!failed && !warp_wait(&y_full[yb], (nn / S::kY) & 1)) failed = true;
 #pragma unroll
-                for (int j = 0; j < kTileAdapters; ++j) {
+                for (int j = 0; j < S::kAdapters; ++j) {
                     if (j >= adapters) break;
                     const int db = mm & 1;
                     if (!failed && !warp_wait(&d_full[db], (mm / 2) & 1)) failed = true;

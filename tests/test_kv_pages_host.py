@@ -149,7 +149,7 @@ def test_adapters_refusals(lib):
         assert call(**kw) == UNS, kw
     # many tokens need a workspace
     need = lib.forge_linear_adapters_workspace_bytes(600, 16)
-    assert need >= 600 * (16 * 4 + 8) and lib.forge_linear_adapters_workspace_bytes(511, 16) == 0
+    assert need >= 600 * (16 * 4 + 8) and lib.forge_linear_adapters_workspace_bytes(512, 16) == 0
     assert lib.forge_linear_adapters_workspace_bytes(600, 130) == 0 and lib.forge_linear_adapters_workspace_bytes(-5, 16) == 0
     assert call(T=600) == BAD and call(T=600, ws=P + 8, nws=need) == BAD and call(T=600, ws=P, nws=need - 1) == WS
 

@@ -70,7 +70,7 @@ def test_widths(dtype, K, N, T, runs):
 
 
 @TYPES
-@pytest.mark.parametrize("T", [512, 640, 2000, 2369, 4737, 9000])
+@pytest.mark.parametrize("T", [512, 513, 640, 2000, 2369, 4737, 9000])
 def test_large_tiles(dtype, T):
     """Runs that begin and end anywhere in a tile, one of all its tokens, and tokens in turns."""
     check(3, dtype, T, 5, 64, 512, 256, runs=157)
