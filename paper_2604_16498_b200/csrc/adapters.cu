@@ -24,7 +24,7 @@ namespace {
 
 constexpr int kAdCtas = 8;                 // of a cluster
 constexpr int kAdWarps = 8, kAdThreads = kAdWarps * 32;
-constexpr int kAdMost = 128;               // tokens of a tile
+constexpr int kAdMost = 16;                // tokens of a tile of the kernel for few of them
 // From how many tokens on the tensor cores' tiles of 128 are the faster ones: when more than 32 tiles of 16 are too many to run at a time.  Groups and
 // tiles, 4096 x 4096, 16 ranks: one adapter, 512 tokens 19.5 and 23.6 us, 592 30.7 and 23.6, 2000 59.4 and 29.7; 8 adapters in runs of 16 tokens, 512 tokens
 // 22.6 and 42, 1000 35.8 and 46.1, 2000 63.6 and 56.3; in turns, 512 tokens 25.7 and 42, 1000 45.1 and 50.2, 2000 82.9 and 60.5.

@@ -706,22 +706,22 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
         cur.step<KEYS>(a, sched, blocks);
     }
 
-    // kMine registers of a fragment of O^T from kMine warp on in this lane, summed over several fragments; a few at a time, whose loads leave
-    // together.  of(i): the i-th.
+    // kMine registers of a fragment of O^T from kMine warp on in this lane, summed over several fragments; a few at a time, and the loads of three
+    // times as many leave together (1 x 32/8 heads x 32,000 bf16 rows, 19 parts to an item: 28.5 and 26.8 us).  of(i): the i-th.
     constexpr int kMine = KS * 4 / kNarrowWarps;
     float sum[kMine], M[2], L[2];
     auto sum_over = [&](int n_of, auto of) {
-        constexpr int kAtOnce = 4;
+        constexpr int kAtOnce = 4, kLoads = 3 * kAtOnce;
         M[0] = M[1] = -INFINITY;
         L[0] = L[1] = 0.f;
 #pragma unroll
         for (int k = 0; k < kMine; ++k) sum[k] = 0.f;
 #pragma unroll 1
-        for (int i0 = 0; i0 < n_of; i0 += kAtOnce) {
-            float2 m[kAtOnce], l[kAtOnce];
-            float x[kAtOnce][kMine];
+        for (int i0 = 0; i0 < n_of; i0 += kLoads) {
+            float2 m[kLoads], l[kLoads];
+            float x[kLoads][kMine];
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
+            for (int i = 0; i < kLoads; ++i) {
                 const float* f = of(min(i0 + i, n_of - 1));
                 m[i] = make_float2(-INFINITY, -INFINITY);
                 l[i] = make_float2(0.f, 0.f);
@@ -734,22 +734,26 @@ attn_kv_narrow_kernel(const __grid_constant__ CUtensorMap tmap_k, const __grid_c
                     for (int k = 0; k < kMine; ++k) x[i][k] = f[(warp * kMine + k) * 32 + lane];
                 }
             }
-            float old[2] = {M[0], M[1]};
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) { M[0] = fmaxf(M[0], m[i].x); M[1] = fmaxf(M[1], m[i].y); }
-            const float ref0 = M[0] == -INFINITY ? 0.f : M[0], ref1 = M[1] == -INFINITY ? 0.f : M[1];
-            const float a0 = ex2(old[0] - ref0), a1 = ex2(old[1] - ref1);
-            L[0] *= a0;
-            L[1] *= a1;
+            for (int j = 0; j < kLoads; j += kAtOnce) {
+                if (i0 + j >= n_of) break;
+                float old[2] = {M[0], M[1]};
 #pragma unroll
-            for (int k = 0; k < kMine; ++k) sum[k] *= k & 1 ? a1 : a0;
+                for (int i = j; i < j + kAtOnce; ++i) { M[0] = fmaxf(M[0], m[i].x); M[1] = fmaxf(M[1], m[i].y); }
+                const float ref0 = M[0] == -INFINITY ? 0.f : M[0], ref1 = M[1] == -INFINITY ? 0.f : M[1];
+                const float a0 = ex2(old[0] - ref0), a1 = ex2(old[1] - ref1);
+                L[0] *= a0;
+                L[1] *= a1;
 #pragma unroll
-            for (int i = 0; i < kAtOnce; ++i) {
-                const float w0 = ex2(m[i].x - ref0), w1 = ex2(m[i].y - ref1);
-                L[0] = fmaf(w0, l[i].x, L[0]);
-                L[1] = fmaf(w1, l[i].y, L[1]);
+                for (int k = 0; k < kMine; ++k) sum[k] *= k & 1 ? a1 : a0;
 #pragma unroll
-                for (int k = 0; k < kMine; ++k) sum[k] = fmaf(k & 1 ? w1 : w0, x[i][k], sum[k]);
+                for (int i = j; i < j + kAtOnce; ++i) {
+                    const float w0 = ex2(m[i].x - ref0), w1 = ex2(m[i].y - ref1);
+                    L[0] = fmaf(w0, l[i].x, L[0]);
+                    L[1] = fmaf(w1, l[i].y, L[1]);
+#pragma unroll
+                    for (int k = 0; k < kMine; ++k) sum[k] = fmaf(k & 1 ? w1 : w0, x[i][k], sum[k]);
+                }
             }
         }
     };

@@ -476,3 +476,77 @@ def test_calls_on_two_streams():
             outs.append(binding.attn_decode_pages(q, pages, table, n))
     torch.cuda.synchronize()
     assert all(same_bits(o, want) for o in outs)
+
+
+def test_native_and_general_marshalling_do_the_same(monkeypatch):
+    """Each call by the native way and by Python's, with and without its optional arguments."""
+    g = ref.seeded(43)
+    B, Hq, Hkv, D, P, T = 3, 6, 2, 64, 16, 9
+    cache = ref.make_cache(g, B, Hkv, 96, D, I8, binding)
+    q, n = ref.normal(g, (B, Hq, D), HF), i32([90, 4, 40])
+    qt = ref.normal(g, (B, T, Hq, D), HF).transpose(1, 2)
+    bits = ref.tree_bits(ref.random_tree(g, B, T))
+    k, v, qa = ref.normal(g, (T, Hkv, D), HF), ref.normal(g, (T, Hkv, D), HF), ref.normal(g, (T, Hq, D), HF)
+    rotary = binding.Rotary(binding.rotary_frequencies(D)[0].cuda())
+    x, y = ref.normal(g, (T, 128), HF), ref.normal(g, (T, 64), HF)
+    a, b = ref.normal(g, (4, 8, 128), HF), ref.normal(g, (4, 64, 8), HF)
+    which = i32([0, 1, -1, 3, 3, 2, 0, 1, 1])
+    scales = torch.rand(4, generator=g, device="cuda")
+
+    def everything():
+        out = []
+        pages, table = paged(ref.seeded(44), cache, P)
+        tables = binding.PageTables(table.clone(), torch.arange(pages.num_pages, dtype=torch.int32, device="cuda"), i32([5]), P)
+        step, left = binding.PageSlots.empty(B, T), i32([0])
+        out.append(binding.assign_pages(tables, n, step, counts=i32([3, 4, 2]), free_left=left).slots.clone())
+        out += [step.lens.clone(), step.starts.clone(), step.positions.clone(), step.requests.clone(), tables.table.clone(), left]
+        binding.assign_pages(tables, n, step)
+        out += [step.slots.clone(), tables.free_count.clone()]
+        slots = torch.arange(T, dtype=torch.int32, device="cuda") * 5
+        out.append(binding.kv_append_pages(pages, k, v, slots, positions=slots, rotary=rotary, q=qa, q_out=torch.zeros_like(qa)))
+        assert binding.kv_append_pages(pages, v, k, slots + 1) is None
+        out += [pages.k.clone(), pages.v_scale.clone().nan_to_num()]
+        ko, vo = (torch.zeros((B, Hkv, 20, D), dtype=HF, device="cuda") for _ in range(2))
+        out += list(binding.kv_read_pages(pages, table, ko, vo, first=i32([3, 0, 30]), counts=i32([20, 4, 9])))
+        ws = torch.zeros(1 << 25, dtype=torch.uint8, device="cuda")
+        out.append(binding.attn_decode_pages(q, pages, table, n, out=torch.empty_like(q), workspace=ws))
+        out.append(binding.attn_tree_pages(qt, pages, table, n - 2, bits, scale=0.3, out=torch.empty_like(qt), workspace=ws))
+        out.append(binding.attn_tree_pages(qt, pages, table, n - 2, out=torch.empty_like(qt), workspace=ws))
+        out.append(binding.linear_adapters(x, y, a, b, which, scales=scales, out=torch.empty_like(y)))
+        out.append(binding.linear_adapters(x, y, a, b, which[:4].contiguous(), requests=which, out=torch.empty_like(y)))
+        binding.check_status()
+        return out
+
+    native = everything()
+    monkeypatch.setattr(binding, "_host_calls", None)
+    for i, (one, other) in enumerate(zip(native, everything())):
+        assert torch.equal(one.float(), other.float()), i
+
+
+def test_nothing_beside_the_outputs_is_written():
+    """Slots, tables and rows lie between guards."""
+    P, num, Hkv, D = 16, 8, 2, 64
+    guard = 64
+    for T, more in ((40, [3, 20]), (3000, [3, 90])):
+        buf = {n: torch.full((m + 2 * guard,), 77, dtype=torch.int32, device="cuda")
+               for n, m in (("lens", 2), ("starts", 3), ("slots", T), ("positions", T), ("requests", T), ("left", 1), ("table", 2 * 6))}
+        mid = {n: x[guard:-guard] for n, x in buf.items()}
+        mid["table"].fill_(-1)
+        tables = binding.PageTables(mid["table"].view(2, 6), torch.arange(num, dtype=torch.int32, device="cuda"), i32([num]), P)
+        binding.assign_pages(tables, i32([0, 0]), binding.PageSlots(*(mid[n] for n in ("lens", "starts", "slots", "positions", "requests"))),
+                             counts=i32(more), free_left=mid["left"])
+        assert mid["lens"].tolist() == more and mid["left"].tolist() == [num - sum(-(-m // P) for m in more)]
+        for x in buf.values():
+            assert (x[:guard] == 77).all() and (x[-guard:] == 77).all()
+    big = torch.full((num + 2, Hkv, P, D), 9.0, dtype=BF, device="cuda")
+    other = big.clone()
+    pages = binding.KVPages(big[1:-1], other[1:-1])
+    k = torch.ones((4, Hkv, D), dtype=BF, device="cuda")
+    binding.kv_append_pages(pages, k, k, i32([0, num * P - 1, num * P, -1]))
+    for x in (big, other):
+        assert (x[0] == 9).all() and (x[-1] == 9).all() and (x == 1).sum() == 2 * Hkv * D
+        assert (x[1, :, 0] == 1).all() and (x[-2, :, -1] == 1).all()
+    q = torch.ones((3, 4, D), dtype=BF, device="cuda")
+    out = torch.full((5, 4, D), 9.0, dtype=BF, device="cuda")
+    binding.attn_decode_pages(q, pages, i32([[0, 1]] * 3), i32([32, 0, 7]), out=out[1:4])
+    assert (out[0] == 9).all() and (out[4] == 9).all() and (out[2] == 0).all()
