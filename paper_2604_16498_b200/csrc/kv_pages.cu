@@ -12,8 +12,9 @@
 namespace forge {
 namespace {
 
-constexpr int kPagesThreads = 1024, kPagesWarps = kPagesThreads / 32;
-constexpr int kManyTokens = 2048, kManyCtas = 8;  // from how many tokens on a cluster does it
+constexpr int kPagesThreads = 1024, kFewThreads = 128;  // of a CTA; that of a small step
+constexpr int kFewTokens = 512;                         // ... which has no more requests than threads, and tokens than this
+constexpr int kManyTokens = 2048, kManyCtas = 8;        // from how many tokens on a cluster does it
 
 struct PagesArgs {
     const int32_t *lens, *counts, *done;
@@ -23,8 +24,8 @@ struct PagesArgs {
     int B, max_pages, page_shift, num_pages, T;
 };
 
-// The sum of v over the threads up to this one; *all: over all threads.  `warps`: room for kPagesWarps.
-template <typename V>
+// The sum of v over the threads up to this one; *all: over all threads.  `warps`: room for one of each warp.
+template <int THREADS, typename V>
 __device__ __forceinline__ V block_scan(V v, V* warps, V* all) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 #pragma unroll
@@ -35,8 +36,8 @@ __device__ __forceinline__ V block_scan(V v, V* warps, V* all) {
     __syncthreads();  // `warps` of the sum before has been read
     if (lane == 31) warps[warp] = v;
     __syncthreads();
-    V w = warps[lane];
-    static_assert(kPagesWarps == 32, "a lane for each warp");
+    static_assert(THREADS <= 1024, "a lane for each warp");
+    V w = lane < THREADS / 32 ? warps[lane] : V(0);
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
         const V t = __shfl_up_sync(0xffffffffu, w, o);
@@ -46,11 +47,12 @@ __device__ __forceinline__ V block_scan(V v, V* warps, V* all) {
     const V before = __shfl_sync(0xffffffffu, w, max(warp - 1, 0));
     return warp > 0 ? v + before : v;
 }
-// The first of kPagesThreads ascending sums that is above x; the last one if none is.
+// The first of THREADS ascending sums that is above x; the last one if none is.
+template <int THREADS>
 __device__ __forceinline__ int first_above(const int* sums, int x) {
     int at = 0;
 #pragma unroll
-    for (int step = kPagesThreads / 2; step > 0; step >>= 1)
+    for (int step = THREADS / 2; step > 0; step >>= 1)
         if (sums[at + step - 1] <= x) at += step;
     return at;
 }
@@ -60,12 +62,12 @@ __device__ __forceinline__ int clamped_len(const PagesArgs& a, int b) { return m
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
 __device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 
-template <int CTAS>
-__global__ void __launch_bounds__(kPagesThreads) assign_pages_kernel(const PagesArgs a) {
-    __shared__ int64_t warp_tokens[kPagesWarps];
-    __shared__ int warp_pages[kPagesWarps];
+template <int CTAS, int THREADS>
+__global__ void __launch_bounds__(THREADS) assign_pages_kernel(const PagesArgs a) {
+    __shared__ int64_t warp_tokens[THREADS / 32];
+    __shared__ int warp_pages[THREADS / 32];
     // of the requests of this turn: where their tokens and new pages end, how many rows they have (-1 - rows: refused)
-    __shared__ int token_end[kPagesThreads], page_end[kPagesThreads], rows_of[kPagesThreads];
+    __shared__ int token_end[THREADS], page_end[THREADS], rows_of[THREADS];
     __shared__ int taken;
     pdl_launch_dependents();
     pdl_wait();
@@ -74,19 +76,19 @@ __global__ void __launch_bounds__(kPagesThreads) assign_pages_kernel(const Pages
     if (tid == 0) taken = 0;
     int64_t tokens = 0;  // of the requests before this turn's
     int pages = 0;       // and new pages that they want (no more than T / P + B, those that T has no room for left out)
-    for (int b0 = 0; b0 < a.B; b0 += kPagesThreads) {
+    for (int b0 = 0; b0 < a.B; b0 += THREADS) {
         const int b = b0 + tid;
         const int len = b < a.B ? clamped_len(a, b) : 0;
         const int64_t count = b >= a.B ? 0 : a.counts ? max(__ldcg(a.counts + b), 0) : 1;
         if (CTAS > 1) cluster_arrive();  // all have read lens, which new_lens may be
         int64_t all_tokens;
         int all_pages;
-        const int64_t end = tokens + block_scan(count, warp_tokens, &all_tokens);
+        const int64_t end = tokens + block_scan<THREADS>(count, warp_tokens, &all_tokens);
         const int have = (len + P1) >> a.page_shift;
         const int64_t need = (len + count + P1) >> a.page_shift;
         bool fits = need <= a.max_pages && end <= a.T;
         const int want = fits ? (int)need - have : 0;
-        const int wanted = pages + block_scan(want, warp_pages, &all_pages);
+        const int wanted = pages + block_scan<THREADS>(want, warp_pages, &all_pages);
         fits = fits && (want == 0 || wanted <= room);
         token_end[tid] = (int)min(end, (int64_t)a.T);
         page_end[tid] = wanted;
@@ -102,13 +104,13 @@ __global__ void __launch_bounds__(kPagesThreads) assign_pages_kernel(const Pages
         }
         __syncthreads();
         const int page_to = min(pages + all_pages, taken);
-        for (int i = pages + rank * kPagesThreads + tid; i < page_to; i += CTAS * kPagesThreads) {  // new pages into the table
-            const int at = first_above(page_end, i), first = at > 0 ? page_end[at - 1] : pages;  // up to `taken` none is refused
+        for (int i = pages + rank * THREADS + tid; i < page_to; i += CTAS * THREADS) {  // new pages into the table
+            const int at = first_above<THREADS>(page_end, i), first = at > 0 ? page_end[at - 1] : pages;  // up to `taken` none is refused
             a.table[(int64_t)(b0 + at) * a.max_pages + ((rows_of[at] + P1) >> a.page_shift) + i - first] = __ldcg(a.free_pages + room - 1 - i);
         }
         const int token0 = (int)min(tokens, (int64_t)a.T), token1 = (int)min(tokens + all_tokens, (int64_t)a.T);
-        for (int t = token0 + rank * kPagesThreads + tid; t < token1; t += CTAS * kPagesThreads) {
-            const int at = first_above(token_end, t), has = rows_of[at], rows = has >= 0 ? has : -1 - has;
+        for (int t = token0 + rank * THREADS + tid; t < token1; t += CTAS * THREADS) {
+            const int at = first_above<THREADS>(token_end, t), has = rows_of[at], rows = has >= 0 ? has : -1 - has;
             const int pos = rows + t - (at > 0 ? token_end[at - 1] : token0);
             int slot = -1;
             if (has >= 0) {
@@ -125,7 +127,7 @@ __global__ void __launch_bounds__(kPagesThreads) assign_pages_kernel(const Pages
         pages += all_pages;
         __syncthreads();  // this turn's sums have been read
     }
-    for (int64_t t = min(tokens, (int64_t)a.T) + rank * kPagesThreads + tid; t < a.T; t += CTAS * kPagesThreads) {  // behind the last token
+    for (int64_t t = min(tokens, (int64_t)a.T) + rank * THREADS + tid; t < a.T; t += CTAS * THREADS) {  // behind the last token
         a.slots[t] = -1;
         if (a.positions) a.positions[t] = 0;
         if (a.requests) a.requests[t] = -1;
@@ -134,9 +136,9 @@ __global__ void __launch_bounds__(kPagesThreads) assign_pages_kernel(const Pages
 }
 
 __global__ void __launch_bounds__(kPagesThreads) release_pages_kernel(const PagesArgs a) {
-    __shared__ int64_t warp_pages[kPagesWarps];
+    __shared__ int64_t warp_pages[kPagesThreads / 32];
     __shared__ int64_t page_end[kPagesThreads];
-    __shared__ int warp_good[kPagesWarps];
+    __shared__ int warp_good[kPagesThreads / 32];
     pdl_launch_dependents();
     pdl_wait();
     const int tid = threadIdx.x, P1 = (1 << a.page_shift) - 1;
@@ -145,7 +147,7 @@ __global__ void __launch_bounds__(kPagesThreads) release_pages_kernel(const Page
         const int b = b0 + tid;
         const int64_t n = b < a.B && __ldcg(a.done + b) != 0 ? (clamped_len(a, b) + P1) >> a.page_shift : 0;
         int64_t all;
-        page_end[tid] = block_scan(n, warp_pages, &all);
+        page_end[tid] = block_scan<kPagesThreads>(n, warp_pages, &all);
         __syncthreads();
         for (int64_t i0 = 0; i0 < all; i0 += kPagesThreads) {
             const int64_t i = i0 + tid;
@@ -159,7 +161,7 @@ __global__ void __launch_bounds__(kPagesThreads) release_pages_kernel(const Page
             }
             const bool good = (unsigned)entry < (unsigned)a.num_pages;
             int all_good;
-            const int to = free + block_scan((int)good, warp_good, &all_good) - 1;
+            const int to = free + block_scan<kPagesThreads>((int)good, warp_good, &all_good) - 1;
             if (good && to < a.num_pages) a.free_pages[to] = entry;
             free = min(free + all_good, a.num_pages);
         }
@@ -212,10 +214,12 @@ extern "C" int forge_kv_assign_pages(const forge_kv_page_tables* tables, const i
     a.requests = out->requests;
     a.T = out->T;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (a.T < kManyTokens)
-        FORGE_CUDA_TRY(launch_pdl(assign_pages_kernel<1>, dim3(1), dim3(kPagesThreads), 0, s, a));
+    if (a.B <= kFewThreads && a.T <= kFewTokens)
+        FORGE_CUDA_TRY(launch_pdl(assign_pages_kernel<1, kFewThreads>, dim3(1), dim3(kFewThreads), 0, s, a));
+    else if (a.T < kManyTokens)
+        FORGE_CUDA_TRY(launch_pdl(assign_pages_kernel<1, kPagesThreads>, dim3(1), dim3(kPagesThreads), 0, s, a));
     else
-        FORGE_CUDA_TRY(launch_pdl_cluster(assign_pages_kernel<kManyCtas>, dim3(kManyCtas), dim3(kPagesThreads), 0, kManyCtas, s, a));
+        FORGE_CUDA_TRY(launch_pdl_cluster(assign_pages_kernel<kManyCtas, kPagesThreads>, dim3(kManyCtas), dim3(kPagesThreads), 0, kManyCtas, s, a));
     return finish_launch(1);
 }
 
