@@ -163,45 +163,34 @@ struct AdBlock {
 };
 
 // u^T = A x^T over this CTA's part of K, in blocks of 64, into `mine` ([warp][token][rank] for SMALL, [token][rank]).  Up to 32 ranks the next
-// block, which may be the next group's, is on its way while one is worked on.
+// block, which may be the next group's, is on its way while one is worked on, in two sets of registers in turns.
 template <bool F16, int RT, bool SMALL, int CTAS>
 __device__ __forceinline__ void shrink_groups(const AdapterArgs& a, const AdGroup* groups, int n_groups, float* mine, int t0, int cta, int warp, int lane) {
     constexpr int kRanks = AdapterShape<RT>::kRanks;
-    constexpr bool kAhead = RT <= 2;
     const int g = lane >> 2, c = lane & 3;
     const int blocks = (a.K + 63) / 64;
     const uint16_t* const xp = static_cast<const uint16_t*>(a.x) + (int64_t)t0 * a.xs;
     const int first = SMALL ? cta * kAdWarps + warp : cta, step = SMALL ? CTAS * kAdWarps : CTAS;
-    const int g0 = SMALL ? 0 : warp, g_step = SMALL ? 1 : kAdWarps;
-    AdBlock<RT> now, then;
-    if (kAhead && g0 < n_groups && first < blocks) then.load(a, groups[g0], xp, first, lane);
-    for (int gi = g0; gi < n_groups; gi += g_step) {
-        const AdGroup& gr = groups[gi];
-        float u[RT][4];
+    const int g_step = SMALL ? 1 : kAdWarps;
+    float u[RT][4];
+    auto clear = [&]() {
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
             for (int k = 0; k < 4; ++k) u[i][k] = 0.f;
-#pragma unroll 1
-        for (int blk = first; blk < blocks; blk += step) {
-            if constexpr (kAhead) {
-                now = then;
-                if (blk + step < blocks) then.load(a, gr, xp, blk + step, lane);
-                else if (gi + g_step < n_groups) then.load(a, groups[gi + g_step], xp, first, lane);
-            } else {
-                now.load(a, gr, xp, blk, lane);
+    };
+    auto add = [&](const AdBlock<RT>& b) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const uint32_t f0[4] = {b.lo[i][h].x, b.hi[i][h].x, b.lo[i][h].y, b.hi[i][h].y};
+                const uint32_t f1[4] = {b.lo[i][h].z, b.hi[i][h].z, b.lo[i][h].w, b.hi[i][h].w};
+                mma_16816<F16>(u[i], f0, b.x[h].x, b.x[h].y);
+                mma_16816<F16>(u[i], f1, b.x[h].z, b.x[h].w);
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    const uint32_t f0[4] = {now.lo[i][h].x, now.hi[i][h].x, now.lo[i][h].y, now.hi[i][h].y};
-                    const uint32_t f1[4] = {now.lo[i][h].z, now.hi[i][h].z, now.lo[i][h].w, now.hi[i][h].w};
-                    mma_16816<F16>(u[i], f0, now.x[h].x, now.x[h].y);
-                    mma_16816<F16>(u[i], f1, now.x[h].z, now.x[h].w);
-                }
-        }
-        // rows g, g + 8 are ranks, columns 2c, 2c + 1 tokens
+    };
+    auto put = [&](const AdGroup& gr) {  // rows g, g + 8 are ranks, columns 2c, 2c + 1 tokens
 #pragma unroll
         for (int i = 0; i < RT; ++i)
 #pragma unroll
@@ -209,6 +198,52 @@ __device__ __forceinline__ void shrink_groups(const AdapterArgs& a, const AdGrou
                 const int t = 2 * c + (k & 1), r = i * 16 + g + 8 * (k >> 1);
                 if (t < gr.n) mine[((SMALL ? warp * a.tile : 0) + gr.token[t]) * kRanks + r] = u[i][k];
             }
+    };
+    clear();
+    if (first >= blocks) {  // no part of K
+        for (int gi = SMALL ? 0 : warp; gi < n_groups; gi += g_step) put(groups[gi]);
+        return;
+    }
+    struct At { int gi, blk; } at = {SMALL ? 0 : warp, first}, next = at;
+    auto step_on = [&](At& x) {
+        x.blk += step;
+        if (x.blk >= blocks) {
+            x.blk = first;
+            x.gi += g_step;
+        }
+    };
+    if constexpr (RT <= 2) {
+        AdBlock<RT> even, odd;
+        auto load = [&](AdBlock<RT>& b) {
+            if (next.gi < n_groups) b.load(a, groups[next.gi], xp, next.blk, lane);
+            step_on(next);
+        };
+        auto use = [&](const AdBlock<RT>& b) {
+            add(b);
+            if (at.blk + step >= blocks) {
+                put(groups[at.gi]);
+                clear();
+            }
+            step_on(at);
+        };
+        load(even);
+        while (at.gi < n_groups) {
+            load(odd);
+            use(even);
+            if (at.gi >= n_groups) break;
+            load(even);
+            use(odd);
+        }
+    } else {
+        for (; at.gi < n_groups; step_on(at)) {
+            AdBlock<RT> b;
+            b.load(a, groups[at.gi], xp, at.blk, lane);
+            add(b);
+            if (at.blk + step >= blocks) {
+                put(groups[at.gi]);
+                clear();
+            }
+        }
     }
 }
 
@@ -312,79 +347,87 @@ struct AdShare {
     }
 };
 
-// out^T = y^T + unit B u^T.  `next`: the first piece's first group, if EARLY.  The next group's y, and up to 32 ranks its B, are on their way while one is
-// worked on.
+// out^T = y^T + unit B u^T.  `even`: the first piece's first group, if EARLY.  Up to 32 ranks the next group's y and B are on their way while one is worked
+// on, in two sets of registers in turns; more ranks have one set, and B is kept while the adapter stays.
 template <bool F16, int RT, bool EARLY>
 __device__ __forceinline__ void expand_groups(const AdapterArgs& a, const AdGroup* groups, const uint16_t* u_hi, const uint16_t* u_lo, const float* unit,
-                                              int t0, const AdShare& share, int end, AdColumns<RT>& next, int lane) {
+                                              int t0, const AdShare& share, int end, AdColumns<RT>& even, int lane) {
     constexpr int kRow = AdapterShape<RT>::kHalfRow;
-    constexpr bool kAhead = RT <= 2;
     const int g = lane >> 2, c = lane & 3;
     uint16_t* const op = static_cast<uint16_t*>(a.out) + (int64_t)t0 * a.os;
     if (share.g0 >= share.g1) return;
-    bool ready = EARLY;
-    for (int un = share.piece; un < end; un += share.step) {
-        const int col = un * 64 + 8 * g;
-        const bool in = col < a.N;
-        if (!ready) {
-            next.load_y(a, groups[share.g0], true, t0, un * 64, lane);
-            if (kAhead) load_b<RT>(next.b, a, groups[share.g0].adapter, un * 64, lane);
+    auto use = [&](const AdColumns<RT>& at, const AdGroup& gr, int col0) {
+        const int col = col0 + 8 * g, ta = gr.token[2 * c], tb = gr.token[2 * c + 1];
+        const bool has_a = col < a.N && 2 * c < gr.n, has_b = col < a.N && 2 * c + 1 < gr.n;
+        uint4 oa = at.ya, ob = at.yb;
+        if (gr.adapter >= 0) {
+            float acc[4][4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
+            const int row = gr.token[min(g, gr.n - 1)] * kRow + 4 * c;
+#pragma unroll
+            for (int s = 0; s < RT; ++s) {
+                const uint2 hi = *reinterpret_cast<const uint2*>(u_hi + row + 16 * s), lo = *reinterpret_cast<const uint2*>(u_lo + row + 16 * s);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t f[4] = {at.b[s][i][0].x, at.b[s][i][1].x, at.b[s][i][0].y, at.b[s][i][1].y};
+                    mma_16816<F16>(acc[i], f, hi.x, hi.y);
+                    mma_16816<F16>(acc[i], f, lo.x, lo.y);
+                }
+            }
+            const float ua = has_a ? unit[ta] : 0.f, ub = has_b ? unit[tb] : 0.f;
+            const uint32_t wa[4] = {oa.x, oa.y, oa.z, oa.w}, wb[4] = {ob.x, ob.y, ob.z, ob.w};
+            uint32_t ra[4], rb[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {  // columns 2 i, 2 i + 1 of the lane's 8
+                const float2 fa = unpack16<F16>(wa[i]), fb = unpack16<F16>(wb[i]);
+                ra[i] = pack16<F16>(fmaf(acc[i][0], ua, fa.x), fmaf(acc[i][2], ua, fa.y));
+                rb[i] = pack16<F16>(fmaf(acc[i][1], ub, fb.x), fmaf(acc[i][3], ub, fb.y));
+            }
+            oa = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+            ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
         }
-        ready = false;
-        AdRows<RT> bf;
-        auto take_b = [&]() {
-#pragma unroll
-            for (int s = 0; s < RT; ++s)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { bf[s][i][0] = next.b[s][i][0]; bf[s][i][1] = next.b[s][i][1]; }
+        if (has_a) *reinterpret_cast<uint4*>(op + ta * a.os + col) = oa;
+        if (has_b) *reinterpret_cast<uint4*>(op + tb * a.os + col) = ob;
+    };
+    struct At { int un, gi; } at = {share.piece, share.g0}, next = at;
+    auto step_on = [&](At& x) {
+        if (++x.gi >= share.g1) {
+            x.gi = share.g0;
+            x.un += share.step;
+        }
+    };
+    if constexpr (RT <= 2) {
+        AdColumns<RT> odd;
+        auto load = [&](AdColumns<RT>& to) {
+            if (next.un < end) {
+                load_b<RT>(to.b, a, groups[next.gi].adapter, next.un * 64, lane);
+                to.load_y(a, groups[next.gi], true, t0, next.un * 64, lane);
+            }
+            step_on(next);
         };
-        if (kAhead) take_b();
-        else load_b<RT>(bf, a, groups[share.g0].adapter, un * 64, lane);
-        for (int gi = share.g0; gi < share.g1; ++gi) {
-            const AdGroup& gr = groups[gi];
-            const AdGroup& then = groups[min(gi + 1, share.g1 - 1)];
-            const int ta = gr.token[2 * c], tb = gr.token[2 * c + 1];
-            const bool has_a = in && 2 * c < gr.n, has_b = in && 2 * c + 1 < gr.n;
-            const uint4 ya = next.ya, yb = next.yb;
-            next.load_y(a, then, gi + 1 < share.g1, t0, un * 64, lane);
-            const bool change = then.adapter != gr.adapter;
-            if (kAhead && change) load_b<RT>(next.b, a, then.adapter, un * 64, lane);
-            uint4 oa = ya, ob = yb;
-            if (gr.adapter >= 0) {
-                float acc[4][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
-                const int row = gr.token[min(g, gr.n - 1)] * kRow + 4 * c;
-#pragma unroll
-                for (int s = 0; s < RT; ++s) {
-                    const uint2 hi = *reinterpret_cast<const uint2*>(u_hi + row + 16 * s), lo = *reinterpret_cast<const uint2*>(u_lo + row + 16 * s);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t f[4] = {bf[s][i][0].x, bf[s][i][1].x, bf[s][i][0].y, bf[s][i][1].y};
-                        mma_16816<F16>(acc[i], f, hi.x, hi.y);
-                        mma_16816<F16>(acc[i], f, lo.x, lo.y);
-                    }
-                }
-                const float ua = has_a ? unit[ta] : 0.f, ub = has_b ? unit[tb] : 0.f;
-                const uint32_t wa[4] = {ya.x, ya.y, ya.z, ya.w}, wb[4] = {yb.x, yb.y, yb.z, yb.w};
-                uint32_t ra[4], rb[4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {  // columns 2 i, 2 i + 1 of the lane's 8
-                    const float2 fa = unpack16<F16>(wa[i]), fb = unpack16<F16>(wb[i]);
-                    ra[i] = pack16<F16>(fmaf(acc[i][0], ua, fa.x), fmaf(acc[i][2], ua, fa.y));
-                    rb[i] = pack16<F16>(fmaf(acc[i][1], ub, fb.x), fmaf(acc[i][3], ub, fb.y));
-                }
-                oa = make_uint4(ra[0], ra[1], ra[2], ra[3]);
-                ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
-            }
-            if (has_a) *reinterpret_cast<uint4*>(op + ta * a.os + col) = oa;
-            if (has_b) *reinterpret_cast<uint4*>(op + tb * a.os + col) = ob;
-            if (change) {
-                if (kAhead) take_b();
-                else load_b<RT>(bf, a, then.adapter, un * 64, lane);
-            }
+        if (EARLY) step_on(next);
+        else load(even);
+        while (at.un < end) {
+            load(odd);
+            use(even, groups[at.gi], at.un * 64);
+            step_on(at);
+            if (at.un >= end) break;
+            load(even);
+            use(odd, groups[at.gi], at.un * 64);
+            step_on(at);
+        }
+    } else {
+        int have_un = -1, have = -1;
+        for (; at.un < end; step_on(at)) {
+            const AdGroup& gr = groups[at.gi];
+            even.load_y(a, gr, true, t0, at.un * 64, lane);
+            if (at.un != have_un || gr.adapter != have) load_b<RT>(even.b, a, gr.adapter, at.un * 64, lane);
+            have_un = at.un;
+            have = gr.adapter;
+            use(even, gr, at.un * 64);
         }
     }
 }
@@ -753,15 +796,16 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
     const int chunks = (a.N + kTileCols - 1) / kTileCols, tiles = (a.T + kTileRows - 1) / kTileRows;
     if (warp == 0) {
         auto cost = [&](int t) { return t < tiles ? chunk_cost(__ldcg(ta.list + t * kListInts), S::kAdapters) : 0; };
-        long long all = 0;
-        for (int t = lane; t < tiles; t += 32) all += cost(t);
+        const int cost0 = cost(lane);
+        long long all = cost0;
+        for (int t = 32 + lane; t < tiles; t += 32) all += cost(t);
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) all += __shfl_xor_sync(0xffffffffu, all, o);
         all *= chunks;
         const long long lo = all * blockIdx.x / gridDim.x, hi = all * (blockIdx.x + 1) / gridDim.x;
         long long before = 0;
         for (int t1 = 0; t1 < tiles; t1 += 32) {
-            const long long mine = (long long)cost(t1 + lane) * chunks;
+            const long long mine = (long long)(t1 == 0 ? cost0 : cost(t1 + lane)) * chunks;
             long long incl = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -1043,11 +1087,12 @@ extern "C" int forge_linear_adapters(const forge_adapters* set, const void* x, c
     a.adapters = adapters;
     a.T = T; a.R = R;
     a.n = set->n; a.rank = set->rank; a.K = set->K; a.N = set->N;
-    // A tile's tokens: so many that the clusters fill the GPU about twice over; from 16 on the warps share the tokens, by eights.
+    // A tile's tokens: so many that all clusters run at a time, two CTAs to an SM (one for more than 64 ranks) but for the SMs that no whole cluster
+    // fits on (200 tokens of 200 requests of 40 adapters, 4096 x 4096, 16 ranks: 24.6 us in 34 clusters, 21.6 in 29); from 9 on 16, which the warps share.
     const int sms = sm_count();
     a.status = device_status_word();
     if (sms <= 0 || !a.status) return FORGE_ERR_CUDA;
-    const int want = (T + sms / 4 - 1) / (sms / 4);
+    const int clusters = (a.rank <= 64 ? 2 : 1) * sms / 9, want = (T + clusters - 1) / clusters;
     a.tile = want <= 8 ? want : 16;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     return set->dtype == FORGE_DTYPE_F16 ? launch_adapters<true>(a, workspace, s) : launch_adapters<false>(a, workspace, s);
