@@ -10,7 +10,8 @@
  *     one dispatch, the linear output never materialised (Section 4.3 "Pass 5:
  *     Operator Fusion", Listing 6 and Eq. 11);
  *   - what stands around the decode step when a model is served: rotary positions, KV caches
- *     of 16-bit or 8-bit rows, attention of single tokens and of drafted trees over them.
+ *     of 16-bit or 8-bit rows, attention of single tokens and of drafted trees over them;
+ *   - a step of many requests: a KV cache in pages with its tables, and low-rank adapters.
  *
  * Conventions shared by every entry point
  *   - Unless a parameter says HOST, pointers are DEVICE pointers owned by the

@@ -3,6 +3,8 @@
 // Reading back is bound by moving bytes (16 x 8 heads x 4096 e4m3 rows of 128, 254 MB, in 46 us: 5.5 TB/s), rotation and append of many tokens by
 // those and the instructions on each element (rotating 3 x 32 heads x 1777 fp16 rows, 87 MB, 18.7 us: 4.7 TB/s; append of 4 x 2048 tokens of 32/8
 // heads to e4m3, 185 MB, 39 us: 4.7 TB/s), and all three at a token per sequence by the launch (2.1, 2.7 and 2.5 us in a chain of launches).
+// A cache in pages: append finds a token's row by its slot, one more dependent read; reading back one entry of the table for each 16 bytes (5625 tokens of
+// 28/4 heads to int8 rows, 98 MB, 23 us, and back, 17 MB, 6 us).
 //
 // Rotation.  A warp works on the heads of one token (or on a share of them), a lane on the same 16 elements of every head, which hold whole
 // pairs: so the cosines and sines are made once for all heads (per head they would take longer than the copies), and no
