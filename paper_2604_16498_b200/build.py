@@ -92,12 +92,10 @@ def _try_host_calls() -> None:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     lib, host = force or _stale(), force or _host_calls_stale()
-    with ThreadPoolExecutor(max_workers=1) as pool:
-        done = pool.submit(_try_host_calls) if host else None
-        if lib:
-            _build_lib(verbose)
-        if done:
-            done.result()
+    if host:  # before the library, not beside it: whoever stands in for subprocess.run sees one command after the other
+        _try_host_calls()
+    if lib:
+        _build_lib(verbose)
     return LIB
 
 
