@@ -524,7 +524,7 @@ __global__ void __launch_bounds__(kAdThreads, RT <= 4 ? 2 : 1) adapters_kernel(c
 //   D[128 x 128 columns] = [u, what rounding left] [B_i, B_i]^T; the rows of y, which lie in shared memory, get their own adapter's D added there and
 //     leave by TMA
 // What bounds them: the second kernel HBM (4000 tokens, 4096 x 14336, 64 ranks, 229 MB of y and out: 41.4 us, 5.5 TB/s, with one adapter), the first one its fixed
-// steps and the copies (33 MB of x: 17 us); the same with 9 requests of 5 adapters 75 to 78 us for both.
+// steps and the copies (33 MB of x: 17 us); the same with 9 requests of 5 adapters 73 to 75 us for both.
 // A tile of more than tile_adapters() adapters, each of which takes a pass over the tile, goes by groups of 8 tokens like small ones.
 constexpr int kTileRows = 128, kTileCols = 128;
 constexpr int tile_adapters(int ranks) { return ranks <= 32 ? 8 : 4; }  // their u lie side by side in tensor memory, of two CTAs to an SM
@@ -549,23 +549,24 @@ struct TileArgs {
     uint32_t* u;  // [token][ranks], then what rounding left of them, in pairs
 };
 
-template <int RT>
+// DEEP: one CTA to an SM.
+template <int RT, bool DEEP>
 struct ContractShape {
     static constexpr int kRanks = RT * 16;
     static constexpr int kABytes = kRanks * 128;                 // an adapter's 64 of K
-    static constexpr int kX = RT == 4 ? 3 : 4, kA = RT == 4 ? 3 : 4;  // buffers of x's 64 of K and of A's (with these two CTAs to an SM, but for RT = 8)
+    static constexpr int kX = DEEP ? 7 : RT == 4 ? 3 : 4, kA = RT == 4 && !DEEP ? 3 : 4;  // buffers of x's 64 of K and of A's
     static constexpr int kAOff = kX * 16384, kInboxOff = kAOff + kA * kABytes;
     static constexpr int kSmem = 1024 + kInboxOff + kTileRows * kRanks * 4;
     static constexpr int kAdapters = tile_adapters(kRanks), kTmemCols = kAdapters * kRanks;
     static_assert(kTileRows * kRanks * 4 <= kInboxOff && kInboxOff % 1024 == 0, "by groups: what the CTA has of u, in the rings' place");
-    static_assert(kSmem <= 232448 - 4096 && (RT == 8 || 2 * (kSmem + 4096) <= 232448), "shared memory");
+    static_assert(kSmem <= 232448 - 4096 && (RT == 8 || DEEP || 2 * (kSmem + 4096) <= 232448), "shared memory");
 };
 
 // CTAS: of a cluster, which share K.
-template <bool F16, int RT, int CTAS>
-__global__ void __launch_bounds__(kAdThreads, RT == 8 ? 1 : 2)
+template <bool F16, int RT, int CTAS, bool DEEP>
+__global__ void __launch_bounds__(kAdThreads, RT == 8 || DEEP ? 1 : 2)
 adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __grid_constant__ CUtensorMap tmap_a, const TileArgs ta) {
-    using S = ContractShape<RT>;
+    using S = ContractShape<RT, DEEP>;
     using namespace ptx;
     constexpr int kRanks = S::kRanks, kPer = kTileRows / CTAS;
     extern __shared__ uint8_t smem_raw[];
@@ -593,11 +594,13 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
         tmem_alloc(&tmem_slot, S::kTmemCols);
         tmem_relinquish();
     }
+    tc_fence_before_sync();
+    __syncthreads();  // the columns are allocated before another kernel may come to this SM and take some
+    tc_fence_after_sync();
     pdl_launch_dependents();
     pdl_wait();
     const int blocks = (a.K + 63) / 64, my_blocks = cta < blocks ? (blocks - cta + CTAS - 1) / CTAS : 0;
     const int early = min(my_blocks, S::kX);
-    __syncthreads();
     if (warp == 3 && elect_one()) {  // the first of x, whatever adapters it will meet
         for (int i = 0; i < early; ++i) {
             mbar_expect_tx(&x_full[i], 16384);
@@ -634,9 +637,7 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
             if (lane < min(n, S::kAdapters)) ta.list[tile * kListInts + 1 + lane] = several[lane];
         }
     }
-    tc_fence_before_sync();
     __syncthreads();
-    tc_fence_after_sync();
     const uint32_t tmem = tmem_slot;
     const int adapters = n_several;
     const bool tiled = adapters <= S::kAdapters;
@@ -1000,20 +1001,22 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
     if (warp == 9) tmem_dealloc(tmem, 2 * kTileCols);
 }
 
+template <bool F16, int RT, int CTAS, bool DEEP>
+int launch_contract(const CUtensorMap& tx, const CUtensorMap& ta, const TileArgs& t, long long tiles, cudaStream_t s) {
+    auto kernel = adapters_contract_kernel<F16, RT, CTAS, DEEP>;
+    constexpr int kSmem = ContractShape<RT, DEEP>::kSmem;
+    FORGE_SET_SMEM_ONCE(kernel, kSmem);
+    FORGE_CUDA_TRY(launch_pdl_cluster(kernel, dim3((unsigned)(tiles * CTAS)), dim3(kAdThreads), kSmem, CTAS, s, tx, ta, t));
+    return FORGE_OK;
+}
+
 template <bool F16, int RT>
 int launch_adapters_tiles(const AdapterArgs& a, void* workspace, cudaStream_t s) {
-    using C = ContractShape<RT>;
     using O = OutputShape<RT>;
-    const long long tiles = ((long long)a.T + kTileRows - 1) / kTileRows, chunks = tiles * ((a.N + kTileCols - 1) / kTileCols);
-    const int sms = sm_count();
-    // clusters of four where those of eight would not all run at a time (two CTAs to an SM, and SMs that no cluster fits on)
-    const bool wide = tiles * kAdCtas * (RT == 8 ? 2 : 1) <= sms * 3 / 2;
-    auto contract = wide ? adapters_contract_kernel<F16, RT, kAdCtas> : adapters_contract_kernel<F16, RT, kAdCtas / 2>;
+    constexpr int kRanks = RT * 16;
     auto output = adapters_output_kernel<F16, RT>;
-    FORGE_SET_SMEM_ONCE((adapters_contract_kernel<F16, RT, kAdCtas>), C::kSmem);
-    FORGE_SET_SMEM_ONCE((adapters_contract_kernel<F16, RT, kAdCtas / 2>), C::kSmem);
     FORGE_SET_SMEM_ONCE(output, O::kSmem);
-    const TileWorkspace w(a.T, C::kRanks);
+    const TileWorkspace w(a.T, kRanks);
     char* base = static_cast<char*>(workspace);
     TileArgs t = {a, reinterpret_cast<int*>(base), reinterpret_cast<int*>(base + w.list), reinterpret_cast<float*>(base + w.unit), reinterpret_cast<uint32_t*>(base + w.u)};
     CUtensorMap tx, ta, tu, ty, tb, to;
@@ -1022,12 +1025,20 @@ int launch_adapters_tiles(const AdapterArgs& a, void* workspace, cudaStream_t s)
         const uint32_t box[2] = {64, (uint32_t)box_rows};
         return encode_tmap_bf16_sw128(m, p, 2, dims, strides, box);
     };
-    if (!rows(&tx, a.x, a.K, a.T, a.xs, kTileRows) || !rows(&ta, a.a, a.K, (int64_t)a.n * a.rank, a.K, C::kRanks) ||
-        !rows(&tu, t.u, 2 * C::kRanks, a.T, 2 * C::kRanks, kTileRows) || !rows(&ty, a.y, a.N, a.T, a.ys, kTileRows) ||
+    if (!rows(&tx, a.x, a.K, a.T, a.xs, kTileRows) || !rows(&ta, a.a, a.K, (int64_t)a.n * a.rank, a.K, kRanks) ||
+        !rows(&tu, t.u, 2 * kRanks, a.T, 2 * kRanks, kTileRows) || !rows(&ty, a.y, a.N, a.T, a.ys, kTileRows) ||
         !rows(&tb, a.b, a.rank, (int64_t)a.n * a.N, a.rank, kTileCols) || !rows(&to, a.out, a.N, a.T, a.os, kTileRows))
         return FORGE_ERR_CUDA;
-    const int ctas = wide ? kAdCtas : kAdCtas / 2;
-    FORGE_CUDA_TRY(launch_pdl_cluster(contract, dim3((unsigned)(tiles * ctas)), dim3(kAdThreads), C::kSmem, ctas, s, tx, ta, t));
+    const long long tiles = ((long long)a.T + kTileRows - 1) / kTileRows, chunks = tiles * ((a.N + kTileCols - 1) / kTileCols);
+    const int sms = sm_count();
+    // Clusters of four where those of eight would not all run at a time (two CTAs to an SM, and SMs that no cluster fits on), with an SM for each CTA while
+    // there are enough, and more buffers (4000 tokens, 14336 x 4096, 64 ranks: 34.7 and 32.4 us; 9 requests, 4096 x 14336, both kernels 75 .. 78 and 73 .. 75).
+    constexpr int kHalf = kAdCtas / 2;
+    int st;
+    if (tiles * kAdCtas * (RT == 8 ? 2 : 1) <= sms * 3 / 2) st = launch_contract<F16, RT, kAdCtas, false>(tx, ta, t, tiles, s);
+    else if (RT <= 4 && tiles * kHalf <= sms) st = launch_contract<F16, RT, kHalf, (RT <= 4)>(tx, ta, t, tiles, s);
+    else st = launch_contract<F16, RT, kHalf, false>(tx, ta, t, tiles, s);
+    if (st != FORGE_OK) return st;
     FORGE_CUDA_TRY(launch_pdl(output, dim3((unsigned)(chunks < sms ? chunks : sms)), dim3(O::kThreads), O::kSmem, s, tu, ty, tb, to, t));
     return finish_launch(2);
 }

@@ -95,24 +95,25 @@ int attn_kv(const forge_kv_cache* cache, const forge_kv_pages* pages, const int3
     a.status = device_status_word();
     const int sms = sm_count();
     if (!a.status || sms <= 0) return FORGE_ERR_CUDA;
-    int ctas = sms < kKvMaxCtas ? sms : kKvMaxCtas;
-    if (tiles < ctas) ctas = (int)tiles;
+    const int most = sms < kKvMaxCtas ? sms : kKvMaxCtas;
+    auto ctas_for = [&](long long n) { return n < most ? (int)n : most; };
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (!pages) return run_format<false>(*cache, a, ctas, s);
+    if (!pages) return run_format<false>(*cache, a, ctas_for(tiles), s);
     a.page_heads = cache->Hkv;
-    if (const int parts = narrow_parts(*cache, G, T); parts > 1 && tiles * parts < (1LL << 31)) {
+    int parts = narrow_parts(*cache, G, T);
+    if (tiles * parts >= (1LL << 31)) parts = 1;
+    if (parts > 1) {
         a.Hkv *= parts;
         a.G /= parts;
         a.rows /= parts;
         a.part_mul = (unsigned)(((1ULL << 32) + parts - 1) / parts);
-        if (tiles * parts > ctas) ctas = tiles * parts < sms ? (int)(tiles * parts) : sms < kKvMaxCtas ? sms : kKvMaxCtas;
     }
     a.table = table;
     a.num_pages = pages->num_pages;
     a.max_pages = cache->Smax / pages->page_size;
     a.page_shift = log2_of(pages->page_size);
     const forge_kv_cache memory = {pages->k, pages->v, pages->k_scale, pages->v_scale, pages->num_pages, pages->Hkv, pages->page_size, pages->D, pages->format};
-    return run_format<true>(memory, a, ctas, s);
+    return run_format<true>(memory, a, ctas_for(tiles * parts), s);
 }
 
 int attn_cache(const forge_kv_cache* cache, const void* q, void* out, int dtype, int Hq, int T, bool own_rows, const int64_t* q_strides,
