@@ -165,11 +165,7 @@ __global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_append_kernel(const 
         src = a.rows[token];
         if (src < 0 || src >= a.S_src) return;
     }
-    int slot = 0;
-    if (FMT != kNoCache && a.slots) {
-        slot = a.slots[token];
-        if (slot < 0 || slot >= a.num_slots) return;
-    }
+    const int slot = FMT != kNoCache && a.slots ? a.slots[token] : 0;  // looked at when the first rows are on their way
     int64_t start = a.first ? a.first[b] : 0;
     if (FMT != kNoCache) start = min(max(start, (int64_t)0), (int64_t)a.Smax);
     const int64_t dst = start + s;  // the row of the cache
@@ -182,11 +178,6 @@ __global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_append_kernel(const 
     const bool in0 = d0 < a.D, in1 = d1 < a.D;
 
     const int iters = (H + RPW - 1) / RPW;
-    int64_t cache_row = 0, head_rows = 0;  // that of KV head 0; rows from a head to the next
-    if (FMT != kNoCache) {
-        head_rows = a.slots ? 1 << a.page_shift : a.Smax;
-        cache_row = a.slots ? ((int64_t)(slot >> a.page_shift) * a.Hkv << a.page_shift) + (slot & ((1 << a.page_shift) - 1)) : ((int64_t)b * a.Hkv) * a.Smax + dst;
-    }
     const T* const q_row = static_cast<const T*>(a.q) + b * a.qs.b + s * a.qs.s;
     const T* const k_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.k) + b * a.kst.b + src * a.kst.s;
     const T* const v_row = FMT == kNoCache ? nullptr : static_cast<const T*>(a.v) + b * a.vst.b + src * a.vst.s;
@@ -207,6 +198,12 @@ __global__ void __launch_bounds__(kRotWarps * 32, 5) rotate_append_kernel(const 
         }
     };
     load(part, then);
+    if (FMT != kNoCache && a.slots && (unsigned)slot >= (unsigned)a.num_slots) return;
+    int64_t cache_row = 0, head_rows = 0;  // that of KV head 0; rows from a head to the next
+    if (FMT != kNoCache) {
+        head_rows = a.slots ? 1 << a.page_shift : a.Smax;
+        cache_row = a.slots ? ((int64_t)(slot >> a.page_shift) * a.Hkv << a.page_shift) + (slot & ((1 << a.page_shift) - 1)) : ((int64_t)b * a.Hkv) * a.Smax + dst;
+    }
 
     // cosines and sines: of this lane's pairs, or (GENERIC) elements
     float cs[kAngles], sn[kAngles];
