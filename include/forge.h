@@ -510,7 +510,7 @@ int forge_attn_tree_pages(const forge_kv_pages* cache, const int32_t* table, int
  * any order is right.  x, y, out: rows of x_stride, y_stride, out_stride elements (0: dense), multiples of 8; out may be y
  * itself with the same stride, but may not overlap it otherwise, nor x.  K, N, rank: multiples of 8, rank up to 128.
  * Sums are kept in fp32, x A_i^T times the scale to within 2^-15 of itself (bf16) or 2^-21 (fp16), and out is rounded once.  The same inputs give
- * the same bits.  n * N and n * rank are below 2^31.
+ * the same bits.  T up to 2^30; n * N and n * rank below 2^31.
  * workspace: at least forge_linear_adapters_workspace_bytes(T, rank) bytes, 16-byte aligned, of any contents (none up to 512 tokens: NULL).  Two
  * calls that may overlap on the GPU must not share it.
  */

@@ -1092,7 +1092,7 @@ extern "C" int forge_linear_adapters(const forge_adapters* set, const void* x, c
     a.os = out_stride ? out_stride : set->N;
     if (a.xs < set->K || a.ys < set->N || a.os < set->N) return FORGE_ERR_INVALID_ARG;
     if (y == out && a.ys != a.os) return FORGE_ERR_INVALID_ARG;
-    if (set->K % 8 != 0 || set->N % 8 != 0 || set->rank % 8 != 0 || set->rank > 128) return FORGE_ERR_UNSUPPORTED;
+    if (set->K % 8 != 0 || set->N % 8 != 0 || set->rank % 8 != 0 || set->rank > 128 || T > 1 << 30) return FORGE_ERR_UNSUPPORTED;
     if (a.xs % 8 != 0 || a.ys % 8 != 0 || a.os % 8 != 0) return FORGE_ERR_UNSUPPORTED;
     if ((long long)set->n * set->N >= (1LL << 31) || (long long)set->n * set->rank >= (1LL << 31)) return FORGE_ERR_UNSUPPORTED;  // counted in 32 bits
     const size_t need = forge_linear_adapters_workspace_bytes(T, set->rank);

@@ -145,7 +145,7 @@ def test_adapters_refusals(lib):
                dict(xs=-64), dict(y=P, out=P, ys=128, os=64)):
         assert call(**kw) == BAD, kw
     for kw in (dict(dtype=2), dict(rank=12), dict(rank=136), dict(K=60), dict(N=68), dict(xs=68), dict(ys=70), dict(os=66),
-               dict(n=1 << 26), dict(n=1 << 28, N=8)):
+               dict(n=1 << 26), dict(n=1 << 28, N=8), dict(T=(1 << 30) + 1, ws=P, nws=1 << 60)):
         assert call(**kw) == UNS, kw
     # many tokens need a workspace
     need = lib.forge_linear_adapters_workspace_bytes(600, 16)

@@ -152,10 +152,28 @@ def test_fp16_products_beyond_its_range():
     assert (out[which == 0] == 0).all()
 
 
+def test_a_workspace_may_hold_anything():
+    g, x, y, a, b, scales = make(12, BF, 900, 12, 16, 256, 320)
+    which = (torch.arange(900, device="cuda") // 70 % 13 - 1).int()
+    which[256:384] = torch.arange(128, device="cuda").int() % 12  # a tile by groups of tokens
+    want = binding.linear_adapters(x, y, a, b, which, scales=scales)
+    need = binding.linear_adapters_workspace_bytes(900, 16)
+    for fill in (0, 255, 127):
+        buf = torch.full((need + 512,), fill, dtype=torch.uint8, device="cuda")
+        out = binding.linear_adapters(x, y, a, b, which, scales=scales, workspace=buf[256: 256 + need], out=torch.empty_like(y))
+        assert torch.equal(out, want)
+        assert (buf[:256] == fill).all() and (buf[-256:] == fill).all()
+    for short in (need - 1, 16):
+        with pytest.raises(binding.ForgeError) as e:
+            binding.linear_adapters(x, y, a, b, which, workspace=torch.zeros(short, dtype=torch.uint8, device="cuda"))
+        assert e.value.status == binding.ERR_WORKSPACE
+
+
 @TYPES
-def test_beside_a_projection_in_a_graph(dtype):
+@pytest.mark.parametrize("T", [37, 700])
+def test_beside_a_projection_in_a_graph(dtype, T):
     """linear_act, then the adapters in place, captured and replayed with other tokens and requests."""
-    T, K, N, n, rank = 37, 256, 512, 5, 16
+    K, N, n, rank = 256, 512, 5, 16
     g, x, _, a, b, scales = make(10, dtype, T, n, rank, K, N)
     w = ref.normal(g, (K, N), dtype, K ** -0.5)
     y = torch.empty((T, N), dtype=dtype, device="cuda")
