@@ -348,7 +348,7 @@ void set_rotary(RotArgs& a, const forge_rotary& r, int inverse) {
 bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
 
 // ------------------------------------------------------------------------------------------------- rows back
-constexpr int kReadThreads = 256, kReadUnroll = 4;
+constexpr int kReadThreads = 256, kFewReadThreads = 32, kReadUnroll = 4;  // few: where no more is to be read of a (batch, head)
 
 struct ReadArgs {
     const void *kc, *vc;
@@ -373,9 +373,9 @@ __device__ __forceinline__ uint32_t scaled_pair(uint32_t h2, float scale) {
     }
 }
 
-// A CTA takes kReadThreads * kReadUnroll pieces of 16 bytes of one (batch, head), of K (blockIdx.y 0) or V: a piece of 8-bit codes becomes 32 bytes.
-template <int FMT, bool F16>
-__global__ void __launch_bounds__(kReadThreads) read_rows_kernel(const ReadArgs a) {
+// A CTA takes THREADS * kReadUnroll pieces of 16 bytes of one (batch, head), of K (blockIdx.y 0) or V: a piece of 8-bit codes becomes 32 bytes.
+template <int FMT, bool F16, int THREADS>
+__global__ void __launch_bounds__(THREADS) read_rows_kernel(const ReadArgs a) {
     pdl_launch_dependents();
     const bool is_v = blockIdx.y != 0;
     const int bh = blockIdx.x / a.blocks, block = blockIdx.x - bh * a.blocks;
@@ -395,7 +395,7 @@ __global__ void __launch_bounds__(kReadThreads) read_rows_kernel(const ReadArgs 
     int entry[kReadUnroll];
 #pragma unroll
     for (int u = 0; u < kReadUnroll; ++u) {
-        const unsigned at = ((unsigned)block * kReadUnroll + u) * kReadThreads + threadIdx.x;
+        const unsigned at = ((unsigned)block * kReadUnroll + u) * THREADS + threadIdx.x;
         row[u] = (int)(at / (unsigned)a.pieces);
         piece[u] = (int)(at - (unsigned)row[u] * (unsigned)a.pieces);
         const int64_t src = first + row[u];
@@ -434,15 +434,21 @@ __global__ void __launch_bounds__(kReadThreads) read_rows_kernel(const ReadArgs 
     }
 }
 
+template <int FMT, bool F16, int THREADS>
+int launch_read(ReadArgs& a, int B, long long per_head, cudaStream_t s) {
+    const long long blocks = (per_head + THREADS * kReadUnroll - 1) / (THREADS * kReadUnroll);
+    if (blocks * B * a.Hkv > 0x7fffffffLL) return FORGE_ERR_UNSUPPORTED;
+    a.blocks = (int)blocks;
+    FORGE_CUDA_TRY(launch_pdl(read_rows_kernel<FMT, F16, THREADS>, dim3((unsigned)(blocks * B * a.Hkv), 2), dim3(THREADS), 0, s, a));
+    return finish_launch(1);
+}
+// A row of each of 64 x 8 heads, with the append before it: 7.7 us in CTAs of 256 threads, 5.9 of 32.
 template <int FMT, bool F16>
 int launch_read(ReadArgs& a, int B, cudaStream_t s) {
     const long long per_head = (long long)a.S * a.pieces;
-    const long long blocks = (per_head + kReadThreads * kReadUnroll - 1) / (kReadThreads * kReadUnroll);
     if (per_head >= (1LL << 31)) return FORGE_ERR_UNSUPPORTED;  // counted in 32 bits
-    if (blocks * B * a.Hkv > 0x7fffffffLL) return FORGE_ERR_UNSUPPORTED;
-    a.blocks = (int)blocks;
-    FORGE_CUDA_TRY(launch_pdl(read_rows_kernel<FMT, F16>, dim3((unsigned)(blocks * B * a.Hkv), 2), dim3(kReadThreads), 0, s, a));
-    return finish_launch(1);
+    return per_head <= kFewReadThreads * kReadUnroll ? launch_read<FMT, F16, kFewReadThreads>(a, B, per_head, s)
+                                                     : launch_read<FMT, F16, kReadThreads>(a, B, per_head, s);
 }
 
 // The cache's part of `a` is set, and the other arguments are checked but for the strides.
