@@ -507,8 +507,8 @@ int forge_attn_tree_pages(const forge_kv_pages* cache, const int32_t* table, int
  * x [T, K], y and out [T, N], a [n, rank, K], b [n, N, rank] of `dtype` FORGE_DTYPE_BF16 or _F16; scales fp32 [n] or NULL (1).  requests:
  * int32 [T], what forge_kv_assign_pages gives, and adapters int32 [R]; requests NULL: i = adapters[t] (R = T then).  A token whose request is outside
  * 0 .. R - 1, or its adapter outside 0 .. n - 1, has none: out[t,:] = y[t,:].  Neighbouring tokens of one adapter share its reads;
- * any order is right.  x, y, out: rows of x_stride, y_stride, out_stride elements (0: dense), multiples of 8; out may be y
- * itself with the same stride, but may not overlap it otherwise, nor x.  K, N, rank: multiples of 8, rank up to 128.
+ * any order is right.  x, y, out: rows of x_stride, y_stride, out_stride elements (0: dense, never the same row again), multiples of 8, no smaller
+ * than the row; out may be y itself with the same stride, but may not overlap it otherwise, nor x.  K, N, rank: multiples of 8, rank up to 128.
  * Sums are kept in fp32, x A_i^T times the scale to within 2^-15 of itself (bf16) or 2^-21 (fp16), and out is rounded once.  The same inputs give
  * the same bits.  T up to 2^30; n * N and n * rank below 2^31.
  * workspace: at least forge_linear_adapters_workspace_bytes(T, rank) bytes, 16-byte aligned, of any contents (none up to 512 tokens: NULL).  Two

@@ -988,6 +988,8 @@ def _rows(t: torch.Tensor, dtype, name: str, shape):
         raise ValueError(f"{name}: expected a CUDA tensor {list(shape)} of {dtype}")
     if t.stride(1) != 1 and shape[1] != 1:
         raise ValueError(f"{name}: the last dimension must be contiguous")
+    if shape[0] > 1 and t.stride(0) < shape[1]:  # 0, of a broadcast row, would say dense
+        raise ValueError(f"{name}: rows that do not overlap expected")
     return t.data_ptr(), t.stride(0) if shape[0] > 1 else 0
 
 
@@ -997,7 +999,7 @@ def linear_adapters_workspace_bytes(T, rank) -> int:
 
 def linear_adapters(x, y, a, b, adapters, requests=None, scales=None, out=None, workspace=None):
     """forge_linear_adapters: y + scales[i] * (x A_i^T) B_i^T with i = adapters[requests[t]] (requests None: adapters[t]); x [T,K] and
-    y, out [T,N] views with contiguous rows, a [n,rank,K], b [n,N,rank], all bf16 or fp16; adapters int32 [R], requests int32 [T], scales
+    y, out [T,N] views with contiguous rows that do not overlap, a [n,rank,K], b [n,N,rank], all bf16 or fp16; adapters int32 [R], requests int32 [T], scales
     fp32 [n] or None.  Tokens without an adapter (-1) keep y.  out may be y itself.  workspace: uint8, of any contents; without one,
     a fresh one is allocated where the call needs it."""
     if _host_calls is not None:

@@ -541,6 +541,7 @@ PyObject* py_adapters(PyObject*, PyObject* const* a, Py_ssize_t n) {
             !sized(r, T) || !sized(sc, d.n) || (!r && R != T) || !here({x, y, out, wa, wb, ad, r, sc, ws}) ||
             (!ws && pages.adapters_workspace(T, d.rank) > 0))
             return not_plain();
+        if (T > 1 && (xs[0] < d.K || ys[0] < d.N || os[0] < d.N)) return not_plain();  // 0, of a broadcast row, would say dense
         const int64_t sx = T > 1 ? xs[0] : 0, sy = T > 1 ? ys[0] : 0, so = T > 1 ? os[0] : 0;
         d.a = address(wa);
         d.b = address(wb);
