@@ -67,6 +67,21 @@ __device__ __forceinline__ float2 unpack16(uint32_t w) {
     if constexpr (F16) return __half22float2(*reinterpret_cast<const __half2*>(&w));
     return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
 }
+// Packed zeros while no element of the pairs so far was infinite or no number.
+template <bool F16>
+__device__ __forceinline__ uint32_t odd_pairs(uint32_t w, uint32_t so_far) {
+    uint32_t r;
+    if constexpr (F16) asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w), "r"(0u), "r"(so_far));
+    else asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(w), "r"(0u), "r"(so_far));
+    return r;
+}
+__device__ __forceinline__ bool is_odd(uint32_t pairs) { return (pairs & 0x7fff7fffu) != 0; }
+// A pair with what is no number, and what is infinite, taken as 0.
+template <bool F16>
+__device__ __forceinline__ uint32_t finite_pair(uint32_t w) {
+    constexpr uint32_t kTop = F16 ? 0x7c00u : 0x7f80u;
+    return ((w & kTop) == kTop ? 0u : w & 0xffffu) | ((w >> 16 & kTop) == kTop ? 0u : w & 0xffff0000u);
+}
 __device__ __forceinline__ uint4 load16(const void* p, bool there) { return there ? *static_cast<const uint4*>(p) : make_uint4(0, 0, 0, 0); }
 __device__ __forceinline__ uint2 load8(const void* p, bool there) { return there ? *static_cast<const uint2*>(p) : make_uint2(0, 0); }
 
@@ -352,7 +367,34 @@ struct AdShare {
     }
 };
 
-// out^T = y^T + unit B u^T.  `even`: the first piece's first group, if EARLY.  Up to 32 ranks the next group's y and B are on their way while one is worked
+// The same products anew where what comes out is not all finite (see expand_groups), B from memory once more, where up to 32 ranks leave it in no register.
+template <bool F16, int RT>
+__device__ __forceinline__ void multiply_finite_rests(float (&acc)[4][4], const AdapterArgs& a, int adapter, int col, const uint16_t* u_hi,
+                                                      const uint16_t* u_lo, int c) {
+    const uint16_t* const bp = static_cast<const uint16_t*>(a.b) + ((int64_t)adapter * a.N + col) * a.rank;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
+#pragma unroll 1
+    for (int r = 0; r < RT * 16; r += 16) {
+        const uint2 hi = *reinterpret_cast<const uint2*>(u_hi + r), lo = *reinterpret_cast<const uint2*>(u_lo + r);
+        const bool there = col < a.N && r + 4 * c < a.rank;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint2 b0 = load8(bp + 2 * i * a.rank + r + 4 * c, there), b1 = load8(bp + (2 * i + 1) * a.rank + r + 4 * c, there);
+            const uint32_t f[4] = {b0.x, b1.x, b0.y, b1.y};
+            const uint32_t f_rest[4] = {finite_pair<F16>(f[0]), finite_pair<F16>(f[1]), finite_pair<F16>(f[2]), finite_pair<F16>(f[3])};
+            mma_16816<F16>(acc[i], f, hi.x, hi.y);
+            mma_16816<F16>(acc[i], f_rest, lo.x, lo.y);
+        }
+    }
+}
+
+// out^T = y^T + unit B u^T.  An infinite element of B is multiplied by the rounded u alone: with what rounding left it would come to an infinity of the
+// other sign, or to no number, and so would the sum.  Where the products (up to 32 ranks: the outputs, once they have left) turn out not to be finite, they are made
+// anew in that way; looking costs nothing that can be measured here.
+// `even`: the first piece's first group, if EARLY.  Up to 32 ranks the next group's y and B are on their way while one is worked
 // on, in two sets of registers in turns; more ranks have one set, and B is kept while the adapter stays.
 template <bool F16, int RT, bool EARLY>
 __device__ __forceinline__ void expand_groups(const AdapterArgs& a, const AdGroup* groups, const uint16_t* u_hi, const uint16_t* u_lo, const float* unit,
@@ -365,37 +407,69 @@ __device__ __forceinline__ void expand_groups(const AdapterArgs& a, const AdGrou
         const int col = col0 + 8 * g, ta = gr.token[2 * c], tb = gr.token[2 * c + 1];
         const bool has_a = col < a.N && 2 * c < gr.n, has_b = col < a.N && 2 * c + 1 < gr.n;
         uint4 oa = at.ya, ob = at.yb;
+        auto put = [&]() {
+            if (has_a) *reinterpret_cast<uint4*>(op + ta * a.os + col) = oa;
+            if (has_b) *reinterpret_cast<uint4*>(op + tb * a.os + col) = ob;
+        };
         if (gr.adapter >= 0) {
             float acc[4][4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
             const int row = gr.token[min(g, gr.n - 1)] * kRow + 4 * c;
+            auto multiply = [&](auto rest) {  // rest: what a pair of B is for what rounding left of u
 #pragma unroll
-            for (int s = 0; s < RT; ++s) {
-                const uint2 hi = *reinterpret_cast<const uint2*>(u_hi + row + 16 * s), lo = *reinterpret_cast<const uint2*>(u_lo + row + 16 * s);
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) acc[i][k] = 0.f;
+#pragma unroll
+                for (int s = 0; s < RT; ++s) {
+                    const uint2 hi = *reinterpret_cast<const uint2*>(u_hi + row + 16 * s), lo = *reinterpret_cast<const uint2*>(u_lo + row + 16 * s);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t f[4] = {at.b[s][i][0].x, at.b[s][i][1].x, at.b[s][i][0].y, at.b[s][i][1].y};
+                        const uint32_t f_rest[4] = {rest(f[0]), rest(f[1]), rest(f[2]), rest(f[3])};
+                        mma_16816<F16>(acc[i], f, hi.x, hi.y);
+                        mma_16816<F16>(acc[i], f_rest, lo.x, lo.y);
+                    }
+                }
+            };
+            multiply([](uint32_t w) { return w; });
+            const float ua = has_a ? unit[ta] : 0.f, ub = has_b ? unit[tb] : 0.f;
+            auto add = [&]() {
+                const uint32_t wa[4] = {at.ya.x, at.ya.y, at.ya.z, at.ya.w}, wb[4] = {at.yb.x, at.yb.y, at.yb.z, at.yb.w};
+                uint32_t ra[4], rb[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {  // columns 2 i, 2 i + 1 of the lane's 8
+                    const float2 fa = unpack16<F16>(wa[i]), fb = unpack16<F16>(wb[i]);
+                    ra[i] = pack16<F16>(fmaf(acc[i][0], ua, fa.x), fmaf(acc[i][2], ua, fa.y));
+                    rb[i] = pack16<F16>(fmaf(acc[i][1], ub, fb.x), fmaf(acc[i][3], ub, fb.y));
+                }
+                oa = make_uint4(ra[0], ra[1], ra[2], ra[3]);
+                ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+            };
+            if constexpr (RT > 2) {
+                float2 odd[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const uint32_t f[4] = {at.b[s][i][0].x, at.b[s][i][1].x, at.b[s][i][0].y, at.b[s][i][1].y};
-                    mma_16816<F16>(acc[i], f, hi.x, hi.y);
-                    mma_16816<F16>(acc[i], f, lo.x, lo.y);
+                    const float2 none = make_float2(0.f, 0.f);
+                    odd[i] = ffma2(make_float2(acc[i][0], acc[i][1]), none, ffma2(make_float2(acc[i][2], acc[i][3]), none, none));
+                }
+                const float2 any = fadd2(fadd2(odd[0], odd[1]), fadd2(odd[2], odd[3]));
+                if (__builtin_expect(__any_sync(0xffffffffu, any.x + any.y != 0.f), 0)) multiply([](uint32_t w) { return finite_pair<F16>(w); });
+                add();
+                put();
+            } else {
+                add();
+                put();
+                const uint32_t odd = odd_pairs<F16>(oa.w, odd_pairs<F16>(oa.z, odd_pairs<F16>(oa.y, odd_pairs<F16>(oa.x, 0u)))) |
+                                     odd_pairs<F16>(ob.w, odd_pairs<F16>(ob.z, odd_pairs<F16>(ob.y, odd_pairs<F16>(ob.x, 0u))));
+                if (__builtin_expect(__any_sync(0xffffffffu, is_odd(odd)), 0)) {
+                    multiply_finite_rests<F16, RT>(acc, a, gr.adapter, col, u_hi + row, u_lo + row, c);
+                    add();
+                    put();
                 }
             }
-            const float ua = has_a ? unit[ta] : 0.f, ub = has_b ? unit[tb] : 0.f;
-            const uint32_t wa[4] = {oa.x, oa.y, oa.z, oa.w}, wb[4] = {ob.x, ob.y, ob.z, ob.w};
-            uint32_t ra[4], rb[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {  // columns 2 i, 2 i + 1 of the lane's 8
-                const float2 fa = unpack16<F16>(wa[i]), fb = unpack16<F16>(wb[i]);
-                ra[i] = pack16<F16>(fmaf(acc[i][0], ua, fa.x), fmaf(acc[i][2], ua, fa.y));
-                rb[i] = pack16<F16>(fmaf(acc[i][1], ub, fb.x), fmaf(acc[i][3], ub, fb.y));
-            }
-            oa = make_uint4(ra[0], ra[1], ra[2], ra[3]);
-            ob = make_uint4(rb[0], rb[1], rb[2], rb[3]);
+        } else {
+            put();
         }
-        if (has_a) *reinterpret_cast<uint4*>(op + ta * a.os + col) = oa;
-        if (has_b) *reinterpret_cast<uint4*>(op + tb * a.os + col) = ob;
     };
     struct At { int un, gi; } at = {share.piece, share.g0}, next = at;
     auto step_on = [&](At& x) {
@@ -759,6 +833,61 @@ struct OutputShape {
     static_assert(kSmem <= 232448 - 4096, "shared memory");
 };
 
+// Whether one of the half's 128 threads has it; a barrier for them.
+__device__ __forceinline__ bool any_of_half(int half, bool has) {
+    uint32_t any;
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 q, %2, 0;\n\tbar.red.or.pred p, %1, 128, q;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                 : "=r"(any) : "r"(1 + half), "r"((uint32_t)has) : "memory");
+    return any != 0;
+}
+
+// 64 columns from `col0` on of the warp's 32 tokens (a lane's from `row` on, in shared memory), of which some are not finite (odd): the ones whose row of B is
+// not either are made anew, with the products of what rounding left of u taking B's finite elements alone (see expand_groups).  The lanes share the odd tokens'
+// columns.  Out's columns have not left yet, so that y's are there, even if they are the same.  What looking costs where all is finite: 4000 tokens of one
+// adapter, 4096 x 14336, 64 ranks, 61.1 -> 62.2 us for both kernels; of nine requests 74.6 .. 77.2 -> 73.7 .. 77.6.
+template <bool F16, int RT>
+__device__ __forceinline__ void redo_columns(const TileArgs& ta, bool odd, uint8_t* row, int token, int own, float unit, int col0, int lane) {
+    const AdapterArgs& a = ta.a;
+    constexpr uint32_t kTop = F16 ? 0x7c00u : 0x7f80u;
+    for (int r = 0; r < RT * 8 && odd; r += 4) {
+        const uint4 w = __ldcg(reinterpret_cast<const uint4*>(ta.u + (int64_t)token * (RT * 16) + r));
+        for (uint32_t x : {w.x, w.y, w.z, w.w}) odd = odd && (x & 0x7fffu) <= kTop && (x >> 16 & 0x7fffu) <= kTop;  // else no column is a number, whatever B has
+    }
+    __syncwarp();
+    const unsigned rows = __ballot_sync(0xffffffffu, odd);
+    if (rows == 0) return;
+    int lanes = 32;  // to a token
+    while (lanes * __popc(rows) > 32) lanes /= 2;
+    unsigned left = rows;
+    for (int k = lane / lanes; k > 0; --k) left &= left - 1;
+    const int r0 = left ? __ffs(left) - 1 : lane, adapter = __shfl_sync(0xffffffffu, own, r0);
+    const float mul = __shfl_sync(0xffffffffu, unit, r0);
+    if (left) {
+        token += r0 - lane;
+        row += (r0 - lane) * 128;
+        const uint32_t* u = ta.u + (int64_t)token * (RT * 16);
+#pragma unroll 1
+        for (int i = lane % lanes; i < 64 && col0 + i < a.N; i += lanes) {
+            uint16_t* at = reinterpret_cast<uint16_t*>(row + (((i >> 3) ^ (r0 & 7)) << 4)) + (i & 7);
+            if (!is_odd(odd_pairs<F16>(*at, 0u))) continue;
+            const uint16_t* b = static_cast<const uint16_t*>(a.b) + ((int64_t)adapter * a.N + col0 + i) * a.rank;
+            float sum = 0.f;
+            bool finite = true;
+#pragma unroll 4
+            for (int r = 0; r < a.rank; r += 2) {
+                const uint32_t w = *reinterpret_cast<const uint32_t*>(b + r), w_rest = finite_pair<F16>(w);
+                const float2 hi = unpack16<F16>(__ldcg(u + r / 2)), lo = unpack16<F16>(__ldcg(u + RT * 8 + r / 2)), f = unpack16<F16>(w), rest = unpack16<F16>(w_rest);
+                finite = finite && w == w_rest;
+                sum = fmaf(hi.x, f.x, fmaf(hi.y, f.y, fmaf(lo.x, rest.x, fmaf(lo.y, rest.y, sum))));
+            }
+            const uint16_t* y = static_cast<const uint16_t*>(a.y) + (int64_t)token * a.ys + col0 + i;
+            if (!finite) *at = (uint16_t)pack16<F16>(fmaf(sum, mul, unpack16<F16>(*y).x), 0.f);
+        }
+    }
+    __syncwarp();
+}
+
 template <bool F16, int RT>
 __global__ void __launch_bounds__(OutputShape<RT>::kThreads, 1)
 adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_constant__ CUtensorMap tmap_y, const __grid_constant__ CUtensorMap tmap_b,
@@ -931,6 +1060,7 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
                 const int yb = nn % S::kY;
                 uint8_t* half_ring = y_ring + yb * S::kYBytes + half * 16384;
                 uint8_t* y = half_ring + row * 128;
+                bool odd = false;
                 if (!failed && !warp_wait(&y_full[yb], (nn / S::kY) & 1)) failed = true;
 #pragma unroll
                 for (int j = 0; j < S::kAdapters; ++j) {
@@ -946,6 +1076,10 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
                         tmem_ld_x32(lanes + db * kTileCols + 32, d[1]);
                         tmem_ld_wait();
                         if (hit) {
+                            float2 o[4] = {};  // zeros while D is finite; sums side by side
+#pragma unroll
+                            for (int i = 0; i < 64; i += 2)
+                                o[i / 2 & 3] = ffma2(make_float2(__uint_as_float(d[i >> 5][i & 31]), __uint_as_float(d[i >> 5][(i & 31) + 1])), make_float2(0.f, 0.f), o[i / 2 & 3]);
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
                                 uint4* at16 = reinterpret_cast<uint4*>(y + ((i ^ (row & 7)) << 4));
@@ -954,12 +1088,14 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
                                 uint32_t out[4];
 #pragma unroll
                                 for (int k = 0; k < 4; ++k) {
-                                    const float2 f = unpack16<F16>(in[k]);
-                                    out[k] = pack16<F16>(fmaf(__uint_as_float(d[i >> 2][(i & 3) * 8 + 2 * k]), mul, f.x),
-                                                         fmaf(__uint_as_float(d[i >> 2][(i & 3) * 8 + 2 * k + 1]), mul, f.y));
+                                    const float2 p = make_float2(__uint_as_float(d[i >> 2][(i & 3) * 8 + 2 * k]), __uint_as_float(d[i >> 2][(i & 3) * 8 + 2 * k + 1]));
+                                    const float2 f = ffma2(p, make_float2(mul, mul), unpack16<F16>(in[k]));
+                                    out[k] = pack16<F16>(f.x, f.y);
                                 }
                                 *at16 = make_uint4(out[0], out[1], out[2], out[3]);
                             }
+                            const float2 all = fadd2(fadd2(o[0], o[1]), fadd2(o[2], o[3]));
+                            odd = all.x + all.y != 0.f;
                         }
                         tc_fence_before_sync();
                     }
@@ -968,8 +1104,11 @@ adapters_output_kernel(const __grid_constant__ CUtensorMap tmap_u, const __grid_
                     ++mm;
                 }
                 fence_proxy_async_smem();
-                if (half == 0) asm volatile("bar.sync 1, 128;" ::: "memory");
-                else asm volatile("bar.sync 2, 128;" ::: "memory");
+                if (__builtin_expect(any_of_half(half, odd), 0)) {
+                    redo_columns<F16, RT>(ta, odd, y, t0 + row, own, mul, q * kTileCols + half * 64, lane);
+                    fence_proxy_async_smem();
+                    any_of_half(half, false);
+                }
                 if ((threadIdx.x & 127) == 0 && !failed) {
                     if (q * kTileCols + half * 64 < a.N) tma_store_2d(&tmap_out, half_ring, q * kTileCols + half * 64, t0);
                     tma_store_commit();
