@@ -86,7 +86,8 @@ __device__ __forceinline__ void bulk_load(uint32_t smem_dst, const void* src, ui
                  : "memory");
 }
 
-__device__ __forceinline__ int kv_past(const KvAttnArgs& a, int b) { return min(max(__ldg(a.lens + b), 0), a.Smax); }
+// From L2, like the table: the kernels before this one, which may have made room for more rows, may still run while its CTAs already do.
+__device__ __forceinline__ int kv_past(const KvAttnArgs& a, int b) { return min(max(__ldcg(a.lens + b), 0), a.Smax); }
 // Rows that any token of the sequence may see.
 __device__ __forceinline__ int kv_rows(const KvAttnArgs& a, int past) { return min(past + a.T, a.Smax); }
 // Tiles of KEYS keys of a (sequence, KV head): one at least, so that a sequence without rows gets its zeros.
