@@ -92,14 +92,15 @@ def _try_host_calls() -> None:
 
 def build(force: bool = False, verbose: bool = False) -> str:
     lib, host = force or _stale(), force or _host_calls_stale()
-    if host:  # before the library, not beside it: whoever stands in for subprocess.run sees one command after the other
-        _try_host_calls()
     if lib:
-        _build_lib(verbose)
+        _build_lib(verbose, beside=[_try_host_calls] if host else [])
+    elif host:
+        _try_host_calls()
     return LIB
 
 
-def _build_lib(verbose: bool) -> None:
+def _build_lib(verbose: bool, beside=()) -> None:
+    """Compiles the sources side by side, and what is given in `beside` with them, as the first of them: one after the other where there is one source."""
     os.makedirs(OBJ_DIR, exist_ok=True)
     sources = sorted(glob.glob(os.path.join(CSRC, "*.cu")))
     objs = [os.path.join(OBJ_DIR, os.path.basename(s)[:-3] + ".o") for s in sources]
@@ -114,8 +115,10 @@ def _build_lib(verbose: bool) -> None:
         if verbose:
             sys.stderr.write(r.stderr)
 
-    with ThreadPoolExecutor(max_workers=min(8, len(sources))) as pool:
-        list(pool.map(compile_one, zip(sources, objs)))
+    with ThreadPoolExecutor(max_workers=max(1, min(8, len(sources)))) as pool:
+        jobs = [pool.submit(job) for job in beside] + [pool.submit(compile_one, pair) for pair in zip(sources, objs)]
+        for job in jobs:
+            job.result()
     tmp = LIB + f".tmp{os.getpid()}"
     r = subprocess.run([_nvcc(), "-shared", "-o", tmp, *objs, "-gencode", "arch=compute_100a,code=sm_100a"],
                        capture_output=True, text=True)
