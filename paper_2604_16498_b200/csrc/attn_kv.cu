@@ -28,15 +28,18 @@ size_t counter_bytes(size_t items) {
 }
 
 // A cache in pages: the query heads of a KV head that are worked on in parts of up to 8 rows each, on the kernel for those, although it then reads K
-// and V once for each part (all but the first from L2): how many parts, 1 where the other kernel is the one.  Measured, parts and tile of 128 rows:
-//   8-bit rows, 2 parts, 16/1 heads of 128: 2 x up to 65,536 rows 36.9 and 65.5 us, 64 x 128/8 x up to 1024 59.4 and 127; 3 parts, 8 x 96/4 x up to
-//     4096 30.7 and 34.9; 4 parts, 4 x 32/8 x 5 tokens behind up to 512 14.4 and 20.5, 4 x 256/8 x up to 4096 36.9 and 34.8
-//   16-bit rows of 64, 2 parts: 2 x 16/1 x up to 65,536 26.6 and 43.0, 64 x 128/8 x up to 1024 49.2 and 69.6; 4 parts, 4 x 256/8 x up to 4096 28.7 and 24.6
-//   16-bit rows of 128, 2 parts: 2 x 16/1 x up to 65,536 38.9 and 47.1; but 16 x 128/8 x up to 2048 43.0 and 38.9, and with 4 x 32/8 x 4 tokens
-//     45.1 and 36.9: there the rows bound it, and only few KV heads leave SMs for the parts
+// and V once for each part (all but the first from L2): how many parts, 1 where the other kernel is the one.  How long the requests are is not known here, so
+// the rule goes by the number of parts and the rows' type alone.  Measured with 1 to 512 KV heads in all, 256 to 65,536 rows each (and down to a quarter of
+// that), single tokens of 12 to 32 heads to a KV head and trees of 4 to 8 tokens; the tile of 128 rows takes, in times of what the parts take (means are geometric):
+//   8-bit rows of 64     2 parts 1.02 .. 3.9, 3 parts 1.03 .. 2.6, 4 parts 0.89 .. 2.4 (mean 1.41)
+//   8-bit rows of 128    2 parts 1.03 .. 2.7, 3 parts 1.06 .. 2.3, 4 parts 0.82 .. 2.1 (mean 1.21; below 1 from 8 KV heads of long requests on: 64 x 32/1 heads,
+//     1024 rows, 20.5 us in parts and 19.3; 32, 4096 rows 28.5 and 27.0; but 512, 1024 rows 89 and 107, 1, 4096 rows 14.8 and 20.7)
+//   16-bit rows of 64    2 parts 0.88 .. 2.4 (mean 1.40); 4 parts 0.59 .. 1.9 (mean 1.04)
+//   16-bit rows of 128   2 parts 0.83 .. 2.2 (mean 1.31; below 1 from 16,384 rows and 32 KV heads on, whose K and V leave L2 between the parts: 32 x 16/1 heads,
+//     16,384 rows 50.9 us in parts and 42.4; but 64, 4096 rows 28.3 and 35.7, 128, 4096 rows 38.6 and 59.4, 1, 4096 rows 10.3 and 18.8); 4 parts 0.47 .. 1.8 (mean 0.98)
 int narrow_parts(const forge_kv_cache& c, int G, int T) {
     if (G * T <= kNarrowRows) return 1;
-    const int most = eight_bit(c.format) ? 4 : c.D <= 64 || (long long)c.B * c.Hkv <= 32 ? 2 : 1;
+    const int most = eight_bit(c.format) ? 4 : 2;
     for (int parts = 2; parts <= most; ++parts)
         if (G % parts == 0 && G / parts * T <= kNarrowRows) return parts;
     return 1;
