@@ -493,7 +493,8 @@ int forge_kv_read_pages(const forge_kv_pages* cache, const int32_t* table, int B
 /*
  * forge_attn_decode_kv and forge_attn_tree over a cache in pages: request b's rows are those of its row of the table, lens clamped to
  * 0 .. max_pages * page_size; a tree's own rows lie behind the lens[b] ones, in the table's order too.  Everything else, the
- * workspace and its size included, as there: one workspace serves calls of both kinds, one after the other.
+ * workspace and its size included, as there: one workspace serves calls of both kinds, one after the other.  B * Hkv * max_pages * page_size is
+ * below 2^35, with more than 128 query rows (Hq / Hkv * T) to a KV head divided by the groups of 128 rows that these make.
  */
 int forge_attn_decode_pages(const forge_kv_pages* cache, const int32_t* table, int B, int max_pages, const void* q, void* out, int dtype,
                             int Hq, const int32_t* lens, float scale, void* workspace, size_t workspace_bytes, void* stream);
@@ -509,8 +510,9 @@ int forge_attn_tree_pages(const forge_kv_pages* cache, const int32_t* table, int
  * 0 .. R - 1, or its adapter outside 0 .. n - 1, has none: out[t,:] = y[t,:].  Neighbouring tokens of one adapter share its reads;
  * any order is right.  x, y, out: rows of x_stride, y_stride, out_stride elements (0: dense, never the same row again), multiples of 8, no smaller
  * than the row; out may be y itself with the same stride, but may not overlap it otherwise, nor x.  K, N, rank: multiples of 8, rank up to 128.
- * Sums are kept in fp32, x A_i^T times the scale to within 2^-15 of itself (bf16) or 2^-21 (fp16), and out is rounded once.  The same inputs give
- * the same bits.  T up to 2^30; n * N and n * rank below 2^31.
+ * Sums are kept in fp32, an element of x A_i^T times the scale to within 2^-15 of itself and 2^-134 (bf16), or 2^-21 of itself and 2^-39 of the token's
+ * largest (fp16): smaller ones count as 0.  out is rounded once.  The same inputs give the same bits.  Infinities and what is no number come out where the
+ * formula takes them to, and nowhere else.  T up to 2^30; n * N and n * rank below 2^31.
  * workspace: at least forge_linear_adapters_workspace_bytes(T, rank) bytes, 16-byte aligned, of any contents (none up to 512 tokens: NULL).  Two
  * calls that may overlap on the GPU must not share it.
  */

@@ -30,9 +30,13 @@ namespace {
 constexpr int kAdCtas = 8;                 // of a cluster
 constexpr int kAdWarps = 8, kAdThreads = kAdWarps * 32;
 constexpr int kAdMost = 16;                // tokens of a tile of the kernel for few of them
-// From how many tokens on the tensor cores' tiles of 128 are the faster ones: when more than 32 tiles of 16 are too many to run at a time.  Groups and
-// tiles, 4096 x 4096, 16 ranks: one adapter, 512 tokens 19.5 and 23.6 us, 592 30.7 and 23.6, 2000 59.4 and 29.7; 8 adapters in runs of 16 tokens, 512 tokens
-// 22.6 and 42, 1000 35.8 and 46.1, 2000 63.6 and 56.3; in turns, 512 tokens 25.7 and 42, 1000 45.1 and 50.2, 2000 82.9 and 60.5.
+// From how many tokens on tiles of 128 on the tensor cores: when more than 32 tiles of 16 are too many to run at a time (which adapters the tokens have is not
+// known on the host).  That favours long runs of one adapter and many ranks; short runs of few adapters pay for a pass over the tile for each of them.  Groups and
+// tiles, us, 4096 x 4096:
+//   16 ranks: one adapter, 512 tokens 10 and 14, 600 19 and 15, 2000 39 and 18; runs of 100 of 8 adapters 11 and 19, 18 and 19, 40 and 25; runs of 16 of 8 adapters
+//     10 and 32, 18 and 35, 39 and 47; 8 adapters in turns 21 and 34, 33 and 38, 69 and 50; 40 in turns 29 and 41, 50 and 47, 110 and 68
+//   64 ranks: one adapter 15 and 17, 27 and 16, 57 and 21; runs of 16 of 8 adapters 15 and 50, 26 and 55, 57 and 69; 40 in turns 87 and 109, 125 and 111, 281 and 189
+//   128 ranks (tiles are the faster ones from 200 tokens on where runs are long): one adapter 48 and 18, 49 and 20, 146 and 28; 40 in turns 224 and 229, 228 and 261, 677 and 439
 constexpr int kTileTokens = 513;
 
 struct AdapterArgs {
@@ -597,8 +601,8 @@ __global__ void __launch_bounds__(kAdThreads, RT <= 4 ? 2 : 1) adapters_kernel(c
 //   u[128 x ranks] = x A_i^T for each adapter i that the tile has, a cluster of eight CTAs to a tile; a row takes its own adapter's
 //   D[128 x 128 columns] = [u, what rounding left] [B_i, B_i]^T; the rows of y, which lie in shared memory, get their own adapter's D added there and
 //     leave by TMA
-// What bounds them: the second kernel HBM (4000 tokens, 4096 x 14336, 64 ranks, 229 MB of y and out: 41.4 us, 5.5 TB/s, with one adapter), the first one its fixed
-// steps and the copies (33 MB of x: 17 us); the same with 9 requests of 5 adapters 73 to 75 us for both.
+// What bounds them: the second kernel HBM where tiles have one adapter (4000 tokens, 4096 x 14336, 64 ranks, 229 MB of y and out: 45 us, 5.1 TB/s), else its passes
+// and how evenly they are shared out (9 requests of 5 adapters: 49 to 57 us, by where the requests begin); the first one its fixed steps and the copies (33 MB of x: 17 us); both together 62 and 74 to 78 us.
 // A tile of more than tile_adapters() adapters, each of which takes a pass over the tile, goes by groups of 8 tokens like small ones.
 constexpr int kTileRows = 128, kTileCols = 128;
 constexpr int tile_adapters(int ranks) { return ranks <= 32 ? 8 : 4; }  // their u lie side by side in tensor memory, of two CTAs to an SM
@@ -817,7 +821,9 @@ adapters_contract_kernel(const __grid_constant__ CUtensorMap tmap_x, const __gri
 }
 
 // What a chunk of a tile's columns takes, in quarters of one with one adapter: each further adapter costs a product, its B and a pass of the warps whose rows
-// have it; by groups a chunk takes about five times as long.
+// have it; by groups it depends on how many tokens a group has.  Measured with 37 tiles of 14336 columns, all with the same number of adapters in turns, K of 64 (so that the first
+// kernel is next to nothing), 16 / 64 ranks: one 66 / 68 us, two 75 / 78, three 93 / 98, four 115 / 121, eight 195 by passes (16 ranks); by groups nine 189 / 247, twelve 232 / 308,
+// twenty 206 / 304, forty 355 / 523: 4, 4.5, 5.6, 7 and 11.8 quarters, and 11.5 to 31.
 __device__ __forceinline__ int chunk_cost(int adapters, int most) { return adapters > most ? 20 : 3 + max(adapters, 1); }
 
 template <int RT>
@@ -845,7 +851,7 @@ __device__ __forceinline__ bool any_of_half(int half, bool has) {
 // 64 columns from `col0` on of the warp's 32 tokens (a lane's from `row` on, in shared memory), of which some are not finite (odd): the ones whose row of B is
 // not either are made anew, with the products of what rounding left of u taking B's finite elements alone (see expand_groups).  The lanes share the odd tokens'
 // columns.  Out's columns have not left yet, so that y's are there, even if they are the same.  What looking costs where all is finite: 4000 tokens of one
-// adapter, 4096 x 14336, 64 ranks, 61.1 -> 62.2 us for both kernels; of nine requests 74.6 .. 77.2 -> 73.7 .. 77.6.
+// adapter, 4096 x 14336, 64 ranks, 61.0 -> 62.3 us for both kernels; of nine requests 72.9 .. 75.5 -> 74.3 .. 77.9.
 template <bool F16, int RT>
 __device__ __forceinline__ void redo_columns(const TileArgs& ta, bool odd, uint8_t* row, int token, int own, float unit, int col0, int lane) {
     const AdapterArgs& a = ta.a;
@@ -1244,8 +1250,9 @@ extern "C" int forge_linear_adapters(const forge_adapters* set, const void* x, c
     a.adapters = adapters;
     a.T = T; a.R = R;
     a.n = set->n; a.rank = set->rank; a.K = set->K; a.N = set->N;
-    // A tile's tokens: so many that all clusters run at a time, two CTAs to an SM (one for more than 64 ranks) but for the SMs that no whole cluster
-    // fits on (200 tokens of 200 requests of 40 adapters, 4096 x 4096, 16 ranks: 24.6 us in 34 clusters, 21.6 in 29); from 9 on 16, which the warps share.
+    // A tile's tokens: so many that all clusters run at a time, two CTAs to an SM but for the SMs that no whole cluster fits on (200 tokens of 200 requests of
+    // 40 adapters, 4096 x 4096, 16 ranks: 24.6 us in 34 clusters, 21.6 in 29); from 9 on 16, which the warps share.  With more than 64 ranks, one CTA to an SM, that
+    // holds up to 256 tokens: more go in two rounds.
     const int sms = sm_count();
     a.status = device_status_word();
     if (sms <= 0 || !a.status) return FORGE_ERR_CUDA;
